@@ -462,6 +462,204 @@ DSA_API dsa_status dsa_select(const dsa_params* p, const dsa_shape* s, const int
                               const void* d_plan, const float* d_window_logits, void* d_state,
                               hipStream_t stream);
 
+/* ---- several tokens of a request at once ----------------------------------- */
+
+/*
+ * A step that looks at several new tokens of every request: drafted tokens in
+ * a tree (or a chain) that the model is about to check, or a chunk of known
+ * tokens (a prompt, the start of an image).  Its calls are
+ *
+ *     dsa_tree_plan       depth and ancestors of every node (trees only;
+ *                         once per step, shared by all layers)
+ *     dsa_tree_attention  attention of every node over the cache and its
+ *                         ancestors among the new tokens (each layer)
+ *     dsa_tree_verify     the drafted tokens that the target's probabilities
+ *                         accept, and the token that follows them
+ *     dsa_kv_append       K/V rows of the accepted tokens into the caches
+ *
+ * The new tokens' K and V are not in the cache during the step: they are read
+ * where the projection left them, so drafts that are not accepted leave no
+ * trace, also in a ring.
+ *
+ * Node i < N of request b is the token at decode position base_b + depth(i).
+ * Position j < 0 is prompt row L_p + j (a chunk of a prompt has base_b < 0; the
+ * first is base_b = -L_p).  The cache holds the positions before base_b.
+ *   nodes    N >= 1, at most DSA_MAX_TREE_NODES where d_plan is given and in
+ *            dsa_tree_verify, else at most 1 << 20
+ *   d_base   int32 [B]: base_b.  A request with base_b < -L_p is an unused
+ *            slot (as one with count 0); base_b > H*W is taken as H*W.
+ *            dsa_tree_verify does not read it (may be NULL there).
+ *   d_count  int32 [B]: request b has nodes 0 .. d_count[b] - 1 (clamped to
+ *            [0, N]); NULL: all N.  Nothing is read or written for the others.
+ *   d_plan   buffer filled by dsa_tree_plan from the nodes' parents, or NULL:
+ *            a chain, node i follows node i - 1
+ */
+typedef struct dsa_tree {
+  int32_t nodes;
+  const int32_t* d_base;
+  const int32_t* d_count;
+  const void* d_plan;
+} dsa_tree;
+
+#define DSA_MAX_TREE_NODES 256
+
+/* Element strides of per-node rows: row (layer l, request b, node i, head h)
+ * starts at l * stride_layer + b * stride_batch + i * stride_node +
+ * h * stride_head and holds head_dim contiguous bf16 elements.  Strides are
+ * >= 0 and multiples of 8 elements, the arrays 16-byte aligned.
+ * stride_layer is read by dsa_kv_append only. */
+typedef struct dsa_node_rows {
+  int64_t stride_batch;
+  int64_t stride_node;
+  int64_t stride_head;
+  int64_t stride_layer;
+} dsa_node_rows;
+
+/* dsa_tree_plan flag bits (per request). */
+#define DSA_TREE_FLAG_BAD_PARENT 1 /* a parent outside [-1, i - 1], taken as -1 */
+
+/* Byte offsets of the arrays inside a tree plan (int32, but ancestors uint32):
+ *   flags     [B]            DSA_TREE_FLAG_* bits
+ *   max_depth [B]            largest depth of the request's nodes
+ *   depth     [B][N]         0 for a node without a parent
+ *   parent    [B][N]         the parents, -1 for none; -1 past the count
+ *   ancestors [B][N][words]  bit m of node i's words: m is i or an ancestor
+ * words = ceil(N / 32). */
+typedef struct dsa_tree_plan_layout {
+  size_t flags_offset;
+  size_t max_depth_offset;
+  size_t depth_offset;
+  size_t parent_offset;
+  size_t ancestors_offset;
+  int32_t words;
+  size_t bytes;
+} dsa_tree_plan_layout;
+
+/* How dsa_tree_attention is launched (for reports and tests): a function of
+ * parameters, shape and nodes. */
+typedef struct dsa_tree_launch_info {
+  int32_t rows_per_tile;   /* query rows (nodes x group) of a workgroup         */
+  int32_t row_tiles;       /* row tiles per (request, KV head)                  */
+  int32_t splits;          /* workgroups that share a row tile's keys, at most  */
+  int32_t workgroups;
+  size_t workspace_bytes;  /* fp32 partials for the combine (0 with one split)  */
+} dsa_tree_launch_info;
+
+DSA_API dsa_status dsa_get_tree_plan_layout(int32_t batch, int32_t nodes,
+                                            dsa_tree_plan_layout* out);
+DSA_API size_t dsa_tree_plan_bytes(int32_t batch, int32_t nodes);
+DSA_API dsa_status dsa_get_tree_launch_info(const dsa_params* p, const dsa_shape* s,
+                                            int32_t nodes, dsa_tree_launch_info* out);
+/* Workspace of dsa_tree_attention (0 when the arguments are invalid). */
+DSA_API size_t dsa_tree_workspace_bytes(const dsa_params* p, const dsa_shape* s, int32_t nodes);
+
+/*
+ * Depths and ancestors of the nodes of B trees.
+ *   d_parent  int32 [B][N]: parent of node i, an earlier node of the same
+ *             request, or -1 for none (depth 0); any other value is taken as
+ *             -1 and flagged
+ *   d_count   int32 [B] or NULL, as in dsa_tree
+ *   d_plan    output, plan_bytes >= dsa_tree_plan_bytes(batch, nodes)
+ * Errors: INVALID_ARG (batch < 1, nodes outside [1, DSA_MAX_TREE_NODES], NULL
+ * pointers), WORKSPACE (plan_bytes too small), HIP.
+ */
+DSA_API dsa_status dsa_tree_plan(int32_t batch, int32_t nodes, const int32_t* d_parent,
+                                 const int32_t* d_count, void* d_plan, size_t plan_bytes,
+                                 hipStream_t stream);
+
+/* Element types of dsa_tree_attention's output. */
+#define DSA_OUT_FP32 0 /* weights kept to fp32 in the product with V           */
+#define DSA_OUT_BF16 1 /* weights rounded to bf16 for that product             */
+
+/*
+ * Attention of every node of every request in dense or window mode.  Node i
+ * at position p attends the cached position j (prompt rows included) where
+ * j < S or p - j < W, and node m where m is i or one of its ancestors (a chain:
+ * m <= i) and the same holds for m's position: W = N_att - S in window mode;
+ * no bound and S = 0 in dense mode.  That is what dsa_decode_attention gives for
+ * a token whose predecessors are all in the cache.  A prompt's rows attend the
+ * prompt up to themselves in every mode.  What a mask hides does not reach the
+ * output, NaN and infinities included.
+ *   d_q              bf16 rows (q_rows), query head h of node i
+ *   d_k_new, d_v_new bf16 rows (new_rows), KV head h of node i
+ *   d_k, d_v, kv     caches as for dsa_decode_attention, holding the positions
+ *                    before base_b that a node can attend
+ *   d_out            [B][N][Hq][d] in out_type, 16-byte aligned; rows of nodes
+ *                    past a request's count are left as they are
+ *   d_ws, ws_bytes   dsa_tree_workspace_bytes() bytes
+ * Algorithm 1 chooses what a token keeps from the step before it, one token
+ * at a time: DSA_MODE_DIAGONAL is refused (a prompt goes in dense mode).
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
+ */
+DSA_API dsa_status dsa_tree_attention(const dsa_params* p, const dsa_shape* s,
+                                      const dsa_tree* tree, const void* d_q,
+                                      const dsa_node_rows* q_rows, const void* d_k_new,
+                                      const void* d_v_new, const dsa_node_rows* new_rows,
+                                      const void* d_k, const void* d_v, const dsa_kv_layout* kv,
+                                      float sm_scale, void* d_out, int32_t out_type, void* d_ws,
+                                      size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Which drafted tokens stand, by rejection sampling from given random numbers,
+ * so that the tokens kept are distributed as the target's.  Node 0 is the
+ * last token already chosen; its children are drafts for the next position, and
+ * so on.  From c = 0, with P = target[c]: the children of c are tried in index
+ * order; child i with token x is accepted where
+ *     uniform[i] * draft[c][x] < P(x),
+ * and c = i; a rejected one leaves P <- max(P - draft[c], 0), scaled to sum 1
+ * (children are independent samples of the parent's draft row).  Without draft
+ * rows each child is certain: accepted where uniform[i] < P(x), else P(x) <- 0
+ * and P is scaled by 1 / (1 - what was taken out).  Where no child is left, the
+ * next token is the first v with P(0) + .. + P(v) > uniform[N] * sum P.  All
+ * sums and comparisons are in fp64.
+ *   batch, vocab  B >= 1, V in [1, 1 << 24]
+ *   tree          nodes, d_count, d_plan; at most DSA_MAX_TREE_NODES nodes
+ *   d_tokens      int32 [B][N]; a token outside [0, V) is never accepted and
+ *                 takes nothing out of P where there are no draft rows
+ *   d_target      fp32 [B][N][V]: row i is the target's distribution of the
+ *                 token after node i (read for accepted nodes only)
+ *   d_draft       fp32 [B][N][V], or NULL: row c is the distribution that the
+ *                 children of node c were drawn from
+ *   d_uniform     fp32 [B][N + 1] in [0, 1): one per node, one for the next token
+ *   d_path        int32 [B][N], out: the accepted nodes, node 0 first, then -1
+ *   d_accepted    int32 [B], out: how many (0 for an unused slot)
+ *   d_next        int32 [B], out: the next token (-1 for an unused slot, or a
+ *                 target row without any mass)
+ * Where max(P - draft, 0) has no mass left, P keeps its last value with mass
+ * for the next token, and no further child of c is accepted.  Negative and NaN
+ * probabilities count as 0.
+ * Errors: INVALID_ARG, HIP.
+ */
+DSA_API dsa_status dsa_tree_verify(int32_t batch, int32_t vocab, const dsa_tree* tree,
+                                   const int32_t* d_tokens, const float* d_target,
+                                   const float* d_draft, const float* d_uniform, int32_t* d_path,
+                                   int32_t* d_accepted, int32_t* d_next, hipStream_t stream);
+
+/*
+ * K/V rows of new tokens into the caches of `layers` layers: row e of request b
+ * (0 <= e < d_accepted[b]) is node d_path[b][e], and goes to position
+ * base_b + e.  bf16 rows are copied; for an fp8 cache each element is divided
+ * by its scale (1 where the pointer is NULL), clamped to +-448 and rounded to
+ * the nearest E4M3 value, ties to even (NaN stays NaN).
+ *   tree        nodes, d_base, d_count (d_plan is not read)
+ *   d_k_new ..  bf16 rows (new_rows, with stride_layer)
+ *   d_path      int32 [B][N], or NULL: node e (a chain, or a chunk).  An entry
+ *               outside the request's nodes is skipped.
+ *   d_accepted  int32 [B] (clamped to the request's count), or NULL: the count
+ *   d_k, d_v    caches; layer l starts l * stride_layer elements in.  kv's
+ *               scales are [layers][B*Hkv].
+ * In a ring, of rows that share a slot the last is written.  Positions at or
+ * past H*W and unused slots write nothing.
+ * All modes are allowed (a decode step appends its token with N = 1).
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+DSA_API dsa_status dsa_kv_append(const dsa_params* p, const dsa_shape* s, const dsa_tree* tree,
+                                 const void* d_k_new, const void* d_v_new,
+                                 const dsa_node_rows* new_rows, const int32_t* d_path,
+                                 const int32_t* d_accepted, int32_t layers, void* d_k, void* d_v,
+                                 const dsa_kv_layout* kv, int64_t stride_layer,
+                                 hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,6 +33,9 @@ Sparse Attention", Algorithm 1 and the "Detailed explanation" paragraph):
                    (``oracle/c/dsa_oracle.c``, fp64, OpenMP over KV heads),
                    for long selection histories and the timed CPU baseline;
                    pinned to the Python oracle and the worked example.
+* ``tree``      -- several new tokens of a request at once: what a node of a
+                   tree (or a chunk) attends, the verification of drafted
+                   tokens by rejection sampling, and rounding to E4M3.
 * ``tieband``   -- bounds of the fp32 rounding of the phase-2 scores, which
                    decide when a device's different argmin is still a
                    correct pick (a near tie); pinned by simulating the fp32
@@ -45,4 +48,4 @@ reduction to the paper's per-head rule at group size 1 is pinned, the rest is
 "parity unpinned".
 """
 
-from . import alg1, attention, fp8, params, step, tieband  # noqa: F401
+from . import alg1, attention, fp8, params, step, tieband, tree  # noqa: F401

@@ -31,6 +31,8 @@ FLAG_POS_CLAMPED = 2
 FLAG_STATE_BEHIND = 4
 FLAG_BAD_OFFSET = 8
 FLAG_COUNT = 16
+TREE_FLAG_BAD_PARENT = 1
+MAX_TREE_NODES = 256
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = 0, -1, -2, -3, -4
 
@@ -82,8 +84,30 @@ class LaunchInfo(C.Structure):
                 ("kept_read", C.c_int32)]
 
 
+class TreeRequest(C.Structure):  # dsa_tree
+    _fields_ = [("nodes", C.c_int32), ("d_base", C.c_void_p), ("d_count", C.c_void_p),
+                ("d_plan", C.c_void_p)]
+
+
+class NodeRows(C.Structure):
+    _fields_ = [("stride_batch", C.c_int64), ("stride_node", C.c_int64),
+                ("stride_head", C.c_int64), ("stride_layer", C.c_int64)]
+
+
+class TreePlanLayout(C.Structure):
+    _fields_ = [("flags_offset", C.c_size_t), ("max_depth_offset", C.c_size_t),
+                ("depth_offset", C.c_size_t), ("parent_offset", C.c_size_t),
+                ("ancestors_offset", C.c_size_t), ("words", C.c_int32), ("bytes", C.c_size_t)]
+
+
+class TreeLaunchInfo(C.Structure):
+    _fields_ = [("rows_per_tile", C.c_int32), ("row_tiles", C.c_int32), ("splits", C.c_int32),
+                ("workgroups", C.c_int32), ("workspace_bytes", C.c_size_t)]
+
+
 # name -> (restype, argtypes); mirrors include/dsa.h
 _P, _S = C.POINTER(Params), C.POINTER(Shape)
+_T, _R = C.POINTER(TreeRequest), C.POINTER(NodeRows)
 _VP = C.c_void_p
 SIGNATURES = {
     "dsa_abi_version": (C.c_int32, []),
@@ -112,6 +136,17 @@ SIGNATURES = {
     "dsa_decode_step_noalloc": (C.c_int32, [_P, _S, _VP, _VP, _VP, C.POINTER(KVLayout), _VP, _VP,
                                             _VP, C.c_size_t, C.c_float, _VP, _VP, _VP]),
     "dsa_select": (C.c_int32, [_P, _S, _VP, _VP, _VP, _VP, _VP]),
+    "dsa_get_tree_plan_layout": (C.c_int32, [C.c_int32, C.c_int32, C.POINTER(TreePlanLayout)]),
+    "dsa_tree_plan_bytes": (C.c_size_t, [C.c_int32, C.c_int32]),
+    "dsa_get_tree_launch_info": (C.c_int32, [_P, _S, C.c_int32, C.POINTER(TreeLaunchInfo)]),
+    "dsa_tree_workspace_bytes": (C.c_size_t, [_P, _S, C.c_int32]),
+    "dsa_tree_plan": (C.c_int32, [C.c_int32, C.c_int32, _VP, _VP, _VP, C.c_size_t, _VP]),
+    "dsa_tree_attention": (C.c_int32, [_P, _S, _T, _VP, _R, _VP, _VP, _R, _VP, _VP,
+                                       C.POINTER(KVLayout), C.c_float, _VP, C.c_int32, _VP,
+                                       C.c_size_t, _VP]),
+    "dsa_tree_verify": (C.c_int32, [C.c_int32, C.c_int32, _T] + [_VP] * 8),
+    "dsa_kv_append": (C.c_int32, [_P, _S, _T, _VP, _VP, _R, _VP, _VP, C.c_int32, _VP, _VP,
+                                  C.POINTER(KVLayout), C.c_int64, _VP]),
 }
 
 NOALLOC_SCRATCH_BYTES = 16 << 20  # DSA_NOALLOC_SCRATCH_BYTES
@@ -400,6 +435,218 @@ def select(p, s, decode_pos, plan_buf, window_logits, state, stream=None):
         _need(state, "state", None, z[3])
     _check(lib().dsa_select(C.byref(p), C.byref(s), _ptr(decode_pos), _ptr(plan_buf),
                             _ptr(window_logits), _ptr(state), _stream(stream)), "dsa_select")
+
+
+# ---- several tokens of a request at once ----------------------------------------
+
+_OUT_TYPES = {torch.float32: 0, torch.bfloat16: 1}  # DSA_OUT_FP32, DSA_OUT_BF16
+
+
+class Tree:
+    """New tokens of every request (``dsa_tree``): ``nodes`` per request at
+    most, ``base`` the decode position of each request's first (int32 [B]),
+    ``count`` how many of them each has (int32 [B]; all), ``plan`` a buffer
+    filled by ``tree_plan`` (a chain).  Keeps the tensors it points to."""
+
+    def __init__(self, nodes, base=None, count=None, plan=None):
+        _need(base, "base", torch.int32)
+        _need(count, "count", torch.int32)
+        _need(plan, "plan")
+        if plan is not None and nodes > MAX_TREE_NODES:
+            raise ValueError(f"a tree has at most {MAX_TREE_NODES} nodes, got {nodes}")
+        self.nodes, self.base, self.count, self.plan = int(nodes), base, count, plan
+        self.c = TreeRequest(self.nodes, _ptr(base), _ptr(count), _ptr(plan))
+        self._batch = None  # the batch these tensors were last checked for
+
+    def check(self, batch, where, base=True):
+        if base and self.base is None:
+            raise ValueError(f"{where} needs the tree's base positions")
+        if batch != self._batch:
+            _need(self.base, "base", torch.int32, batch * 4)
+            _need(self.count, "count", torch.int32, batch * 4)
+            if self.plan is not None:
+                _need(self.plan, "plan", None, tree_plan_bytes(batch, self.nodes))
+            self._batch = batch
+
+
+def make_tree(nodes, base=None, count=None, plan=None) -> Tree:
+    return Tree(nodes, base, count, plan)
+
+
+def tree_plan_layout(batch: int, nodes: int) -> TreePlanLayout:
+    out = TreePlanLayout()
+    _check(lib().dsa_get_tree_plan_layout(batch, nodes, C.byref(out)), "dsa_get_tree_plan_layout")
+    return out
+
+
+def tree_plan_bytes(batch: int, nodes: int) -> int:
+    return lib().dsa_tree_plan_bytes(batch, nodes)
+
+
+def tree_launch_info(p: Params, s: Shape, nodes: int) -> TreeLaunchInfo:
+    out = TreeLaunchInfo()
+    _check(lib().dsa_get_tree_launch_info(C.byref(p), C.byref(s), nodes, C.byref(out)),
+           "dsa_get_tree_launch_info")
+    return out
+
+
+def tree_workspace_bytes(p: Params, s: Shape, nodes: int) -> int:
+    return lib().dsa_tree_workspace_bytes(C.byref(p), C.byref(s), nodes)
+
+
+def _on_device(*tensors):
+    """Every tensor is on the current device, whose stream the call takes."""
+    at = torch.cuda.current_device()
+    for x in tensors:
+        if x is not None and x.device.index != at:
+            raise ValueError(f"a tensor is on {x.device}, the current device is cuda:{at}")
+
+
+def _need_shape(x, name, dtype, shape):
+    _need(x, name, dtype)
+    if tuple(x.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(x.shape)}")
+
+
+def _node_rows(x, name, shape):
+    """Strides of a bf16 tensor of rows ``[(layers,) B, nodes, heads, d]``, the
+    rows themselves dense."""
+    if x.dtype is not torch.bfloat16 or not x.is_cuda:
+        _need(x, name, torch.bfloat16, contiguous=False)
+    if tuple(x.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(x.shape)}")
+    st = x.stride()
+    if st[-1] != 1:
+        raise ValueError(f"{name}: head_dim must be contiguous")
+    return NodeRows(st[-4], st[-3], st[-2], st[0] if len(st) == 5 else 0)
+
+
+def _new_rows(k_new, v_new, shape):
+    rows = _node_rows(k_new, "k_new", shape)
+    _node_rows(v_new, "v_new", shape)
+    if k_new.stride() != v_new.stride():
+        raise ValueError("k_new and v_new must share strides")
+    return rows
+
+
+def _check_caches(p, s, k, v, layout, rows_needed, layers=None):
+    _need(k, "k", _KV_DTYPES, contiguous=False)
+    _need(v, "v", _KV_DTYPES, contiguous=False)
+    if k.dtype != v.dtype or k.shape != v.shape or k.stride() != v.stride():
+        raise ValueError("k and v must share element type, shape and strides")
+    if (layout.dtype == KV_BF16) != (k.dtype is torch.bfloat16):
+        raise ValueError(f"the layout is not of a {k.dtype} cache")
+    if layers is not None and (k.dim() != 5 or k.shape[0] != layers):
+        raise ValueError(f"the caches must be of {layers} layers, got shape {tuple(k.shape)}")
+    if k.dim() >= 4 and layout.d_row_base is None:
+        nb, nh, rows, nd = k.shape[-4:]
+        if (nb < s.batch or nh < s.num_kv_heads or nd != s.head_dim or rows < rows_needed
+                or (layout.stride_batch, layout.stride_head, layout.stride_row)
+                != tuple(k.stride()[-4:-1])):
+            raise ValueError(f"cache of shape {tuple(k.shape)} does not hold {s.batch} requests x "
+                             f"{s.num_kv_heads} KV heads x {rows_needed}+ rows of {s.head_dim} "
+                             "elements as the layout says")
+
+
+def tree_plan(parent, count, plan_buf, stream=None):
+    """Depths and ancestors of trees: ``parent`` int32 [B, nodes], -1 for none."""
+    _need(parent, "parent", torch.int32)
+    if parent.dim() != 2:
+        raise ValueError(f"parent must be [B, nodes], got {tuple(parent.shape)}")
+    batch, nodes = parent.shape
+    _need(count, "count", torch.int32, batch * 4)
+    _need(plan_buf, "plan")
+    _on_device(parent, count, plan_buf)
+    _check(lib().dsa_tree_plan(batch, nodes, _ptr(parent), _ptr(count), _ptr(plan_buf),
+                               _nbytes(plan_buf), _stream(stream)), "dsa_tree_plan")
+
+
+def tree_attention(p, s, tree: Tree, q, k_new, v_new, k, v, layout: KVLayout, sm_scale, out,
+                   workspace=None, stream=None):
+    """Attention of every node over the caches and its ancestors.  ``q``
+    bf16 [B, nodes, Hq, d], ``k_new`` and ``v_new`` bf16 [B, nodes, Hkv, d]
+    (any strides with dense rows, as slices of a fused projection), ``out``
+    [B, nodes, Hq, d] in fp32 or bf16."""
+    B_, Hq, Hkv, d = s.batch, s.num_q_heads, s.num_kv_heads, s.head_dim
+    n = tree.nodes
+    tree.check(B_, "tree_attention")
+    q_rows = _node_rows(q, "q", (B_, n, Hq, d))
+    new_rows = _new_rows(k_new, v_new, (B_, n, Hkv, d))
+    out_type = _OUT_TYPES.get(out.dtype)
+    if out_type is None:
+        raise ValueError(f"out must be fp32 or bf16, got {out.dtype}")
+    _need_shape(out, "out", out.dtype, (B_, n, Hq, d))
+    _check_caches(p, s, k, v, layout,
+                  p.prompt_len + layout.ring_rows)
+    _need(workspace, "workspace")
+    _on_device(tree.base, q, k_new, v_new, k, v, out, workspace)
+    _check(lib().dsa_tree_attention(
+        C.byref(p), C.byref(s), C.byref(tree.c), _ptr(q), C.byref(q_rows), _ptr(k_new),
+        _ptr(v_new), C.byref(new_rows), _ptr(k), _ptr(v), C.byref(layout), float(sm_scale),
+        _ptr(out), out_type, _ptr(workspace), 0 if workspace is None else _nbytes(workspace),
+        _stream(stream)), "dsa_tree_attention")
+
+
+def tree_verify(tree: Tree, tokens, target, draft, uniform, path, accepted, next_token,
+                stream=None):
+    """Which drafted tokens stand, and the token after them.  ``tokens`` int32
+    [B, nodes], ``target`` fp32 [B, nodes, V], ``draft`` the same or None
+    (certain drafts), ``uniform`` fp32 [B, nodes + 1]; out: ``path`` int32
+    [B, nodes], ``accepted`` and ``next_token`` int32 [B]."""
+    _need(target, "target", torch.float32)
+    if target.dim() != 3:
+        raise ValueError(f"target must be [B, nodes, V], got {tuple(target.shape)}")
+    batch, n, vocab = target.shape
+    if n != tree.nodes:
+        raise ValueError(f"target has {n} nodes, the tree {tree.nodes}")
+    tree.check(batch, "tree_verify", base=False)
+    _need_shape(tokens, "tokens", torch.int32, (batch, n))
+    if draft is not None:
+        _need_shape(draft, "draft", torch.float32, (batch, n, vocab))
+    _need_shape(uniform, "uniform", torch.float32, (batch, n + 1))
+    _need_shape(path, "path", torch.int32, (batch, n))
+    _need_shape(accepted, "accepted", torch.int32, (batch,))
+    _need_shape(next_token, "next_token", torch.int32, (batch,))
+    _on_device(tokens, target, draft, uniform, path, accepted, next_token, tree.count, tree.plan)
+    _check(lib().dsa_tree_verify(batch, vocab, C.byref(tree.c), _ptr(tokens), _ptr(target),
+                                 _ptr(draft), _ptr(uniform), _ptr(path), _ptr(accepted),
+                                 _ptr(next_token), _stream(stream)), "dsa_tree_verify")
+
+
+def kv_append(p, s, tree: Tree, k_new, v_new, k, v, layout: KVLayout, path=None, accepted=None,
+              stream=None):
+    """K/V rows of new tokens into the caches, from the tree's base positions on:
+    ``accepted[b]`` rows (all), the e-th node ``path[b, e]`` (node e).  One
+    layer (``k_new`` [B, nodes, Hkv, d], ``k`` [B, Hkv, rows, d]) or all of
+    them (both with layers in front, ``layout`` of one layer's cache but with
+    the scales of all, [layers, B * Hkv])."""
+    B_, Hkv, d, n = s.batch, s.num_kv_heads, s.head_dim, tree.nodes
+    tree.check(B_, "kv_append")
+    layers = k_new.shape[0] if k_new.dim() == 5 else None
+    lead = () if layers is None else (layers,)
+    rows = _new_rows(k_new, v_new, lead + (B_, n, Hkv, d))
+    _check_caches(p, s, k, v, layout,
+                  p.prompt_len + (layout.ring_rows or p.grid_h * p.grid_w), layers)
+    if path is not None:
+        _need_shape(path, "path", torch.int32, (B_, n))
+    _need(accepted, "accepted", torch.int32, B_ * 4)
+    _on_device(tree.base, k_new, v_new, k, v, path, accepted)
+    _check(lib().dsa_kv_append(
+        C.byref(p), C.byref(s), C.byref(tree.c), _ptr(k_new), _ptr(v_new), C.byref(rows),
+        _ptr(path), _ptr(accepted), layers or 1, _ptr(k), _ptr(v), C.byref(layout),
+        k.stride(0) if layers else 0, _stream(stream)), "dsa_kv_append")
+
+
+def tree_plan_views(batch: int, nodes: int, plan_buf: torch.Tensor):
+    """(flags [B], max_depth [B], depth [B, nodes], parent [B, nodes], ancestors
+    [B, nodes, words]) int32 views of a tree plan."""
+    L = tree_plan_layout(batch, nodes)
+    i32 = lambda off, n: plan_buf[off:off + 4 * n].view(torch.int32)
+    bn = batch * nodes
+    return (i32(L.flags_offset, batch), i32(L.max_depth_offset, batch),
+            i32(L.depth_offset, bn).view(batch, nodes),
+            i32(L.parent_offset, bn).view(batch, nodes),
+            i32(L.ancestors_offset, bn * L.words).view(batch, nodes, L.words))
 
 
 # ---- buffers (torch allocations) and views --------------------------------------

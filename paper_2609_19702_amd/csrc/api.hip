@@ -4,6 +4,7 @@
 #include <mutex>
 
 #include "internal.h"
+#include "tree.h"
 
 namespace dsa {
 namespace {
@@ -186,6 +187,29 @@ dsa_status derive(const dsa_params* p, const dsa_shape* s, Derived* d) {
     d->NW_fp8 = waves_for(d->MF ? kMfmaTile : 2 * rows_per_instr * unroll_for(G, d->D, 1));
   }
   return DSA_OK;
+}
+
+// What every call that takes a cache layout checks of it.
+dsa_status check_kv(const dsa_kv_layout* kv, const Derived& d) {
+  if (kv->dtype != DSA_KV_BF16 && kv->dtype != DSA_KV_FP8_E4M3) return DSA_ERR_INVALID_ARG;
+  if (kv->dtype == DSA_KV_BF16 && (kv->d_k_scale || kv->d_v_scale)) return DSA_ERR_INVALID_ARG;
+  if (kv->stride_row < d.D || kv->stride_head < 0 || kv->stride_batch < 0)
+    return DSA_ERR_INVALID_ARG;
+  if ((kv->stride_row | kv->stride_head | kv->stride_batch) & 7) return DSA_ERR_INVALID_ARG;
+  if (kv->ring_rows < 0 || kv->ring_rows > (int64_t(1) << 30)) return DSA_ERR_INVALID_ARG;
+  // The ring must hold every row a step can read: the sinks plus the window
+  // (sparse modes), or every decode row (dense mode).
+  if (kv->ring_rows > 0 && kv->ring_rows < (d.mode != DSA_MODE_DENSE ? int64_t(d.Ns) + d.Nr
+                                                                     : int64_t(d.Ldec)))
+    return DSA_ERR_INVALID_ARG;
+  return DSA_OK;
+}
+
+// No ring (0), or a ring of at least L_dec slots, maps every position to
+// itself; otherwise ring_slots >= N_r > 0 slots rotate after the sinks.
+int ring_slots(const dsa_kv_layout* kv, const Derived& d) {
+  return (kv->ring_rows == 0 || kv->ring_rows >= d.Ldec) ? 0
+                                                         : static_cast<int>(kv->ring_rows - d.Ns);
 }
 
 }  // namespace dsa
@@ -373,18 +397,8 @@ static dsa_status decode_impl(const dsa_params* p, const dsa_shape* s, const voi
     if (d.state_cap > 0 && d.Nr > dsa::kMaxFusedWindow) return DSA_ERR_UNSUPPORTED;
   }
   if (!std::isfinite(sm_scale)) return DSA_ERR_INVALID_ARG;
-  if (kv->dtype != DSA_KV_BF16 && kv->dtype != DSA_KV_FP8_E4M3) return DSA_ERR_INVALID_ARG;
-  if (kv->dtype == DSA_KV_BF16 && (kv->d_k_scale || kv->d_v_scale)) return DSA_ERR_INVALID_ARG;
+  if ((st = dsa::check_kv(kv, d)) != DSA_OK) return st;
   const int64_t esz = kv->dtype == DSA_KV_BF16 ? 2 : 1;
-  if (kv->stride_row < d.D || kv->stride_head < 0 || kv->stride_batch < 0)
-    return DSA_ERR_INVALID_ARG;
-  if ((kv->stride_row | kv->stride_head | kv->stride_batch) & 7) return DSA_ERR_INVALID_ARG;
-  if (kv->ring_rows < 0 || kv->ring_rows > (int64_t(1) << 30)) return DSA_ERR_INVALID_ARG;
-  // The ring must hold every row a step can read: the sinks plus the window
-  // (sparse modes), or every decode row (dense mode).
-  if (kv->ring_rows > 0 &&
-      kv->ring_rows < (sparse ? int64_t(d.Ns) + d.Nr : int64_t(d.Ldec)))
-    return DSA_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(d_k) | reinterpret_cast<uintptr_t>(d_v) |
        reinterpret_cast<uintptr_t>(d_q)) & 15)
     return DSA_ERR_INVALID_ARG;
@@ -421,11 +435,7 @@ static dsa_status decode_impl(const dsa_params* p, const dsa_shape* s, const voi
   a.wl_rows = std::min(d.C, (d.plan_cap + 3) & ~3);  // C is a multiple of the tile
   a.sel_lds = d.state_cap > 0 ? dsa::sel_lds_bytes(d.G, d.plan_cap - d.Ns, int64_t{d.B} * d.Hkv)
                             : 0u;
-  // No ring (0), or a ring of at least L_dec slots, maps every position to
-  // itself; otherwise a.ring >= N_r > 0 slots rotate after the sinks.
-  a.ring = (kv->ring_rows == 0 || kv->ring_rows >= d.Ldec)
-               ? 0
-               : static_cast<int>(kv->ring_rows - d.Ns);
+  a.ring = dsa::ring_slots(kv, d);
   a.Ns = d.Ns;
   a.Nr = d.Nr;
   a.Natt = d.Natt;

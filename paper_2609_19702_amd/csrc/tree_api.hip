@@ -1,0 +1,304 @@
+// Host side of the calls that take several tokens per request: argument
+// checks, the tree plan's layout and the launch of the attention.
+#include <algorithm>
+#include <cmath>
+
+#include "tree.h"
+
+namespace dsa {
+namespace {
+
+constexpr int kMostNodes = 1 << 20;
+constexpr int64_t kMostGrid = (int64_t(1) << 31) - 1;
+
+size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+
+dsa_status hip_status(hipError_t e) { return e == hipSuccess ? DSA_OK : DSA_ERR_HIP; }
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+dsa_status tree_plan_layout(int batch, int nodes, dsa_tree_plan_layout* l) {
+  if (batch < 1 || nodes < 1 || nodes > DSA_MAX_TREE_NODES) return DSA_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(batch) * nodes > (int64_t(1) << 30)) return DSA_ERR_INVALID_ARG;
+  const size_t b = batch, bn = b * nodes;
+  l->words = (nodes + 31) / 32;
+  l->flags_offset = 0;
+  l->max_depth_offset = align256(4 * b);
+  l->depth_offset = l->max_depth_offset + align256(4 * b);
+  l->parent_offset = l->depth_offset + align256(4 * bn);
+  l->ancestors_offset = l->parent_offset + align256(4 * bn);
+  l->bytes = l->ancestors_offset + align256(4 * bn * l->words);
+  return DSA_OK;
+}
+
+dsa_status check_tree(const dsa_tree* t, int batch, int most) {
+  if (!t || t->nodes < 1 || t->nodes > most) return DSA_ERR_INVALID_ARG;
+  if (t->d_plan && t->nodes > DSA_MAX_TREE_NODES) return DSA_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(batch) * t->nodes > (int64_t(1) << 30)) return DSA_ERR_INVALID_ARG;
+  return DSA_OK;
+}
+
+dsa_status check_rows(const dsa_node_rows* r) {
+  if (!r || r->stride_batch < 0 || r->stride_node < 0 || r->stride_head < 0)
+    return DSA_ERR_INVALID_ARG;
+  if ((r->stride_batch | r->stride_node | r->stride_head) & 7) return DSA_ERR_INVALID_ARG;
+  return DSA_OK;
+}
+
+// derive() for the calls that need no plan of kept rows, so that their modes
+// and nodes bound nothing but their own launch.
+dsa_status tree_derive(const dsa_params* p, const dsa_shape* s, int nodes, Derived* d,
+                       TreeLaunch* l) {
+  const dsa_status st = derive(p, s, d);
+  if (st != DSA_OK) return st;
+  if (nodes < 1 || nodes > kMostNodes) return DSA_ERR_INVALID_ARG;
+  if (d->mode == DSA_MODE_DIAGONAL) return DSA_ERR_UNSUPPORTED;
+  *l = tree_launch(*d, nodes);
+  if (l->workgroups + 8 > kMostGrid || static_cast<int64_t>(d->B) * nodes > (int64_t(1) << 30))
+    return DSA_ERR_INVALID_ARG;
+  return DSA_OK;
+}
+
+}  // namespace
+
+TreeLaunch tree_launch(const Derived& d, int nodes) {
+  constexpr int kRows = 128, kKeys = 64;
+  TreeLaunch l{};
+  l.rows = kRows;
+  const int64_t rows = static_cast<int64_t>(nodes) * d.G;
+  l.row_tiles = static_cast<int>((rows + kRows - 1) / kRows);
+  const int64_t wgs = static_cast<int64_t>(d.B) * d.Hkv * l.row_tiles;
+  const int64_t keys = d.Lp + (d.mode == DSA_MODE_WINDOW ? std::min(d.Natt, d.Ldec) : d.Ldec) +
+                       int64_t{nodes};
+  const int64_t most = std::max<int64_t>(1, keys / (2 * kKeys));
+  l.splits = static_cast<int>(std::min<int64_t>({(512 + wgs - 1) / wgs, most, 64}));
+  l.workgroups = wgs * l.splits;
+  l.ws_bytes = l.splits > 1 ? static_cast<size_t>(l.workgroups) * l.rows * (d.D + 4) * 4 : 0;
+  return l;
+}
+
+}  // namespace dsa
+
+using dsa::Derived;
+using dsa::TreeLaunch;
+
+extern "C" {
+
+DSA_API dsa_status dsa_get_tree_plan_layout(int32_t batch, int32_t nodes,
+                                            dsa_tree_plan_layout* out) {
+  dsa_tree_plan_layout l;
+  const dsa_status st = dsa::tree_plan_layout(batch, nodes, &l);
+  if (st != DSA_OK) return st;
+  if (!out) return DSA_ERR_INVALID_ARG;
+  *out = l;
+  return DSA_OK;
+}
+
+DSA_API size_t dsa_tree_plan_bytes(int32_t batch, int32_t nodes) {
+  dsa_tree_plan_layout l;
+  return dsa::tree_plan_layout(batch, nodes, &l) == DSA_OK ? l.bytes : 0;
+}
+
+DSA_API dsa_status dsa_get_tree_launch_info(const dsa_params* p, const dsa_shape* s, int32_t nodes,
+                                            dsa_tree_launch_info* out) {
+  Derived d;
+  TreeLaunch l;
+  const dsa_status st = dsa::tree_derive(p, s, nodes, &d, &l);
+  if (st != DSA_OK) return st;
+  if (!out) return DSA_ERR_INVALID_ARG;
+  out->rows_per_tile = l.rows;
+  out->row_tiles = l.row_tiles;
+  out->splits = l.splits;
+  out->workgroups = static_cast<int32_t>(l.workgroups);
+  out->workspace_bytes = l.ws_bytes;
+  return DSA_OK;
+}
+
+DSA_API size_t dsa_tree_workspace_bytes(const dsa_params* p, const dsa_shape* s, int32_t nodes) {
+  Derived d;
+  TreeLaunch l;
+  return dsa::tree_derive(p, s, nodes, &d, &l) == DSA_OK ? l.ws_bytes : 0;
+}
+
+DSA_API dsa_status dsa_tree_plan(int32_t batch, int32_t nodes, const int32_t* d_parent,
+                                 const int32_t* d_count, void* d_plan, size_t plan_bytes,
+                                 hipStream_t stream) {
+  dsa_tree_plan_layout l;
+  const dsa_status st = dsa::tree_plan_layout(batch, nodes, &l);
+  if (st != DSA_OK) return st;
+  if (!d_parent || !d_plan) return DSA_ERR_INVALID_ARG;
+  if (plan_bytes < l.bytes) return DSA_ERR_WORKSPACE;
+  char* pb = static_cast<char*>(d_plan);
+  dsa::TreePlanArgs a{};
+  a.parent = d_parent;
+  a.count = d_count;
+  a.flags = reinterpret_cast<int32_t*>(pb + l.flags_offset);
+  a.max_depth = reinterpret_cast<int32_t*>(pb + l.max_depth_offset);
+  a.depth = reinterpret_cast<int32_t*>(pb + l.depth_offset);
+  a.out_parent = reinterpret_cast<int32_t*>(pb + l.parent_offset);
+  a.anc = reinterpret_cast<uint32_t*>(pb + l.ancestors_offset);
+  a.B = batch;
+  a.N = nodes;
+  a.words = l.words;
+  return dsa::hip_status(dsa::launch_tree_plan(a, stream));
+}
+
+DSA_API dsa_status dsa_tree_attention(const dsa_params* p, const dsa_shape* s,
+                                      const dsa_tree* tree, const void* d_q,
+                                      const dsa_node_rows* q_rows, const void* d_k_new,
+                                      const void* d_v_new, const dsa_node_rows* new_rows,
+                                      const void* d_k, const void* d_v, const dsa_kv_layout* kv,
+                                      float sm_scale, void* d_out, int32_t out_type, void* d_ws,
+                                      size_t ws_bytes, hipStream_t stream) {
+  Derived d;
+  TreeLaunch l;
+  dsa_status st = dsa::derive(p, s, &d);
+  if (st != DSA_OK) return st;
+  if ((st = dsa::check_tree(tree, d.B, dsa::kMostNodes)) != DSA_OK) return st;
+  if ((st = dsa::tree_derive(p, s, tree->nodes, &d, &l)) != DSA_OK) return st;
+  if (!tree->d_base || !d_q || !d_k_new || !d_v_new || !d_k || !d_v || !kv || !d_out)
+    return DSA_ERR_INVALID_ARG;
+  if ((st = dsa::check_rows(q_rows)) != DSA_OK) return st;
+  if ((st = dsa::check_rows(new_rows)) != DSA_OK) return st;
+  if (!std::isfinite(sm_scale)) return DSA_ERR_INVALID_ARG;
+  if (out_type != DSA_OUT_FP32 && out_type != DSA_OUT_BF16) return DSA_ERR_INVALID_ARG;
+  if ((st = dsa::check_kv(kv, d)) != DSA_OK) return st;
+  for (const void* x : {d_q, d_k_new, d_v_new, d_k, d_v, static_cast<const void*>(d_out)})
+    if (!dsa::aligned16(x)) return DSA_ERR_INVALID_ARG;
+  if (l.ws_bytes && (!d_ws || ws_bytes < l.ws_bytes)) return DSA_ERR_WORKSPACE;
+  if (l.ws_bytes && !dsa::aligned16(d_ws)) return DSA_ERR_INVALID_ARG;
+
+  const int64_t esz = kv->dtype == DSA_KV_BF16 ? 2 : 1;
+  dsa::TreeArgs a{};
+  a.q = static_cast<const uint16_t*>(d_q);
+  a.kn = static_cast<const uint16_t*>(d_k_new);
+  a.vn = static_cast<const uint16_t*>(d_v_new);
+  a.k = static_cast<const uint8_t*>(d_k);
+  a.v = static_cast<const uint8_t*>(d_v);
+  a.qsb = q_rows->stride_batch;
+  a.qsn = q_rows->stride_node;
+  a.qsh = q_rows->stride_head;
+  a.nsb = new_rows->stride_batch;
+  a.nsn = new_rows->stride_node;
+  a.nsh = new_rows->stride_head;
+  a.row_base = kv->d_row_base;
+  a.sb = kv->stride_batch * esz;
+  a.sh = kv->stride_head * esz;
+  a.sr = kv->stride_row * esz;
+  a.ks = kv->d_k_scale;
+  a.vs = kv->d_v_scale;
+  a.base = tree->d_base;
+  a.count = tree->d_count;
+  if (tree->d_plan) {
+    dsa_tree_plan_layout pl;
+    dsa::tree_plan_layout(d.B, tree->nodes, &pl);
+    const char* pb = static_cast<const char*>(tree->d_plan);
+    a.max_depth = reinterpret_cast<const int32_t*>(pb + pl.max_depth_offset);
+    a.depth = reinterpret_cast<const int32_t*>(pb + pl.depth_offset);
+    a.anc = reinterpret_cast<const uint32_t*>(pb + pl.ancestors_offset);
+    a.words = pl.words;
+  }
+  a.scale_log2 = std::max(std::fabs(sm_scale) * 1.4426950408889634f, dsa::kTreeMinScale);
+  a.q_sign = std::signbit(sm_scale) ? 0x80008000u : 0u;
+  a.out = d_out;
+  a.part = static_cast<float*>(d_ws);
+  a.B = d.B;
+  a.Hq = d.Hq;
+  a.Hkv = d.Hkv;
+  a.G = d.G;
+  a.N = tree->nodes;
+  a.Lp = d.Lp;
+  a.Ldec = d.Ldec;
+  a.S = d.Ns;
+  a.W = d.mode == DSA_MODE_WINDOW ? d.Nr : dsa::kTreeNone;
+  a.ring = dsa::ring_slots(kv, d);
+  a.row_tiles = l.row_tiles;
+  a.splits = l.splits;
+  const bool f32 = out_type == DSA_OUT_FP32;
+  return dsa::hip_status(kv->dtype == DSA_KV_BF16 ? dsa::launch_tree_bf16(d, l, a, f32, stream)
+                                                  : dsa::launch_tree_fp8(d, l, a, f32, stream));
+}
+
+DSA_API dsa_status dsa_tree_verify(int32_t batch, int32_t vocab, const dsa_tree* tree,
+                                   const int32_t* d_tokens, const float* d_target,
+                                   const float* d_draft, const float* d_uniform, int32_t* d_path,
+                                   int32_t* d_accepted, int32_t* d_next, hipStream_t stream) {
+  if (batch < 1 || vocab < 1 || vocab > (1 << 24)) return DSA_ERR_INVALID_ARG;
+  const dsa_status st = dsa::check_tree(tree, batch, DSA_MAX_TREE_NODES);
+  if (st != DSA_OK) return st;
+  if (!d_tokens || !d_target || !d_uniform || !d_path || !d_accepted || !d_next)
+    return DSA_ERR_INVALID_ARG;
+  dsa::VerifyArgs a{};
+  a.count = tree->d_count;
+  if (tree->d_plan) {
+    dsa_tree_plan_layout pl;
+    dsa::tree_plan_layout(batch, tree->nodes, &pl);
+    a.parent = reinterpret_cast<const int32_t*>(static_cast<const char*>(tree->d_plan) +
+                                                pl.parent_offset);
+  }
+  a.tokens = d_tokens;
+  a.target = d_target;
+  a.draft = d_draft;
+  a.uniform = d_uniform;
+  a.path = d_path;
+  a.accepted = d_accepted;
+  a.next = d_next;
+  a.N = tree->nodes;
+  a.V = vocab;
+  return dsa::hip_status(dsa::launch_verify(a, batch, stream));
+}
+
+DSA_API dsa_status dsa_kv_append(const dsa_params* p, const dsa_shape* s, const dsa_tree* tree,
+                                 const void* d_k_new, const void* d_v_new,
+                                 const dsa_node_rows* new_rows, const int32_t* d_path,
+                                 const int32_t* d_accepted, int32_t layers, void* d_k, void* d_v,
+                                 const dsa_kv_layout* kv, int64_t stride_layer,
+                                 hipStream_t stream) {
+  Derived d;
+  dsa_status st = dsa::derive(p, s, &d);
+  if (st != DSA_OK) return st;
+  if ((st = dsa::check_tree(tree, d.B, dsa::kMostNodes)) != DSA_OK) return st;
+  if (!tree->d_base || !d_k_new || !d_v_new || !d_k || !d_v || !kv) return DSA_ERR_INVALID_ARG;
+  if ((st = dsa::check_rows(new_rows)) != DSA_OK) return st;
+  if (layers < 1 || stride_layer < 0 || new_rows->stride_layer < 0 ||
+      ((stride_layer | new_rows->stride_layer) & 7))
+    return DSA_ERR_INVALID_ARG;
+  if ((st = dsa::check_kv(kv, d)) != DSA_OK) return st;
+  for (const void* x : {d_k_new, d_v_new, static_cast<const void*>(d_k),
+                        static_cast<const void*>(d_v)})
+    if (!dsa::aligned16(x)) return DSA_ERR_INVALID_ARG;
+  const int64_t per = (static_cast<int64_t>(tree->nodes) * d.Hkv * (d.D / 8) + 255) / 256;
+  if (per > dsa::kMostGrid / layers / d.B) return DSA_ERR_INVALID_ARG;
+  const int64_t esz = kv->dtype == DSA_KV_BF16 ? 2 : 1;
+  dsa::AppendArgs a{};
+  a.kn = static_cast<const uint16_t*>(d_k_new);
+  a.vn = static_cast<const uint16_t*>(d_v_new);
+  a.nsl = new_rows->stride_layer;
+  a.nsb = new_rows->stride_batch;
+  a.nsn = new_rows->stride_node;
+  a.nsh = new_rows->stride_head;
+  a.base = tree->d_base;
+  a.count = tree->d_count;
+  a.path = d_path;
+  a.accepted = d_accepted;
+  a.k = static_cast<uint8_t*>(d_k);
+  a.v = static_cast<uint8_t*>(d_v);
+  a.row_base = kv->d_row_base;
+  a.sl = stride_layer * esz;
+  a.sb = kv->stride_batch * esz;
+  a.sh = kv->stride_head * esz;
+  a.sr = kv->stride_row * esz;
+  a.ks = kv->d_k_scale;
+  a.vs = kv->d_v_scale;
+  a.layers = layers;
+  a.B = d.B;
+  a.Hkv = d.Hkv;
+  a.N = tree->nodes;
+  a.Lp = d.Lp;
+  a.Ldec = d.Ldec;
+  a.S = d.Ns;
+  a.ring = dsa::ring_slots(kv, d);
+  return dsa::hip_status(dsa::launch_append(a, d.D, kv->dtype, stream));
+}
+
+}  // extern "C"
