@@ -175,11 +175,6 @@ struct SkipSet {
   int flags;
 };
 
-__device__ __forceinline__ void fence_wave() {
-  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // What a wave that may own window rows loads ahead of the decode position
 // (kPre 16-bit values per lane), by the build:
 //   without kept lists (KL false): the first kPre*64 stored skip offsets,

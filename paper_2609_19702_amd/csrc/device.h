@@ -89,6 +89,12 @@ __device__ __forceinline__ void xor_pair(float x, float& first, float& second) {
   }
 }
 
+// What the wave wrote to LDS before is there for what it reads after.
+__device__ __forceinline__ void fence_wave() {
+  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 __device__ __forceinline__ float shfl_xor(float x, int mask) { return __shfl_xor(x, mask, 64); }
 
 template <int CTRL>

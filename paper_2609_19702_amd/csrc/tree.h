@@ -51,11 +51,15 @@ struct TreeArgs {
   int S, W;          // sinks, recent window (kTreeNone: none)
   int ring;          // positions >= S rotate through this many slots (0: linear)
   int row_tiles, splits;
+  int split_tiles;   // key tiles of a split, at least (but the last)
 };
 
 // Launch of dsa_tree_attention.
 struct TreeLaunch {
   int rows;       // query rows per workgroup
+  int waves;      // waves per workgroup
+  int keys;       // keys per tile
+  int split_tiles;  // tiles per split, at least
   int row_tiles;  // per (request, KV head)
   int splits;
   int64_t workgroups;

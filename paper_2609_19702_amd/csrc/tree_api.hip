@@ -62,16 +62,22 @@ dsa_status tree_derive(const dsa_params* p, const dsa_shape* s, int nodes, Deriv
 }  // namespace
 
 TreeLaunch tree_launch(const Derived& d, int nodes) {
-  constexpr int kRows = 128, kKeys = 64;
   TreeLaunch l{};
-  l.rows = kRows;
   const int64_t rows = static_cast<int64_t>(nodes) * d.G;
-  l.row_tiles = static_cast<int>((rows + kRows - 1) / kRows);
-  const int64_t wgs = static_cast<int64_t>(d.B) * d.Hkv * l.row_tiles;
+  const int64_t pairs = static_cast<int64_t>(d.B) * d.Hkv;
+  const bool stream = rows <= 64;
+  l.rows = stream ? (rows <= 32 ? 32 : 64) : 128;
+  l.keys = stream ? 32 : 64;
+  l.row_tiles = static_cast<int>((rows + l.rows - 1) / l.rows);
+  l.waves = l.rows == 32 && pairs <= 256 ? 8 : 4;
   const int64_t keys = d.Lp + (d.mode == DSA_MODE_WINDOW ? std::min(d.Natt, d.Ldec) : d.Ldec) +
                        int64_t{nodes};
-  const int64_t most = std::max<int64_t>(1, keys / (2 * kKeys));
-  l.splits = static_cast<int>(std::min<int64_t>({(512 + wgs - 1) / wgs, most, 64}));
+  const int64_t tiles = (keys + l.keys - 1) / l.keys + 2;
+  const int64_t wgs = pairs * l.row_tiles;
+  const int least = stream ? 4 * l.waves : 4;
+  const int64_t want = std::min<int64_t>((512 + wgs - 1) / wgs, 64);
+  l.split_tiles = static_cast<int>(std::max<int64_t>(least, (tiles + want - 1) / want));
+  l.splits = static_cast<int>((tiles + l.split_tiles - 1) / l.split_tiles);
   l.workgroups = wgs * l.splits;
   l.ws_bytes = l.splits > 1 ? static_cast<size_t>(l.workgroups) * l.rows * (d.D + 4) * 4 : 0;
   return l;
@@ -214,6 +220,7 @@ DSA_API dsa_status dsa_tree_attention(const dsa_params* p, const dsa_shape* s,
   a.ring = dsa::ring_slots(kv, d);
   a.row_tiles = l.row_tiles;
   a.splits = l.splits;
+  a.split_tiles = l.split_tiles;
   const bool f32 = out_type == DSA_OUT_FP32;
   return dsa::hip_status(kv->dtype == DSA_KV_BF16 ? dsa::launch_tree_bf16(d, l, a, f32, stream)
                                                   : dsa::launch_tree_fp8(d, l, a, f32, stream));

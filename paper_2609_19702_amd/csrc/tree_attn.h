@@ -15,10 +15,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kTreeMin = -3.0e38f;  // "no score yet": finite, below every finite score in use
 
-
-constexpr int kTileRows = 128;  // query rows of a workgroup: four waves of 32
-constexpr int kTileKeys = 64;   // keys of a tile
-
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {  // nearest even
   const f32x2 x = {a, b};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
@@ -29,13 +25,15 @@ __device__ __forceinline__ uint32_t high_halves(float a, float b) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
 
-__device__ __forceinline__ bool has_nonfinite(const uint4& x) {
+// Bit 15 of the result: any of eight bf16 values is infinite or NaN (an exponent
+// of ones carries into the bit above it).
+__device__ __forceinline__ uint32_t nonfinite_bit(const uint4& x) {
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  bool bad = false;
+  uint32_t carry = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    bad |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
-  return bad;
+    carry |= ((w[i] & 0x7f80u) + 0x80u) | (((w[i] >> 16) & 0x7f80u) + 0x80u);
+  return carry;
 }
 
 // Sixteen E4M3 values as bf16 (exact: 4 significant bits, exponents -9 .. 8).
@@ -87,24 +85,338 @@ __device__ __forceinline__ void store4(void* out, int64_t at, float a, float b, 
         make_uint2(pack_bf16(a, b), pack_bf16(c, d));
 }
 
+// What a wave needs of one query row (node, query head): its lane's row.
+struct TreeRow {
+  int node, dep;  // the node and its depth (a chain: the same)
+  int thr;        // cached entries past the prefix are seen above this one
+  int64_t out;    // element offset of the output row
+};
+
+__device__ __forceinline__ TreeRow tree_row(const TreeArgs& a, const TreeReq& rq,
+                                            const TreeKeys& ks, int b, int h, int row) {
+  TreeRow r;
+  r.node = row / a.G;
+  const int head = h * a.G + row % a.G;
+  r.dep = a.depth ? a.depth[static_cast<int64_t>(b) * a.N + r.node] : r.node;
+  r.thr = ks.pre + rq.base + r.dep - a.W - ks.j0;
+  r.out = (static_cast<int64_t>(b) * a.N + r.node) * a.Hq + head;
+  return r;
+}
+
+// Which of 32 cached entries from e on the row sees.
+__device__ __forceinline__ uint32_t see_cached(const TreeKeys& ks, const TreeRow& r, int e) {
+  return low_bits(ks.nold - e) & (low_bits(ks.pre - e) | ~low_bits(r.thr + 1 - e));
+}
+
+// Which of 32 new entries from e on the row sees.  sink: nodes of smaller depth
+// stand at sink positions; deep: some node is a window or more deep.
+__device__ __forceinline__ uint32_t see_new(const TreeArgs& a, const TreeKeys& ks, const TreeRow& r,
+                                            int b, int e, int sink, bool deep) {
+  uint32_t see = low_bits(ks.nnew - e);
+  if (!a.depth) {  // nodes from a1 on follow the first a0, which every node sees
+    const int f = ks.a0 - ks.a1 - e;
+    return see & low_bits(r.node + 1 + f) &
+           (low_bits(ks.a0 - e) | low_bits(sink + f) | ~low_bits(r.node - a.W + 1 + f));
+  }
+  const int64_t at = static_cast<int64_t>(b) * a.N;
+  see &= e / 32 < a.words ? a.anc[(at + r.node) * a.words + e / 32] : 0u;
+  if (deep)
+    for (uint32_t m = see; m; m &= m - 1) {
+      const int i = __builtin_ctz(m), de = a.depth[at + e + i];
+      if (de >= sink && r.dep - de >= a.W) see &= ~(1u << i);
+    }
+  return see;
+}
+
+// Whether some row of nodes n0 .. n1 (the deepest at depth `deepest`) must not
+// see some of the `keys` cached (new) entries from e on.
+__device__ __forceinline__ bool hides_cached(const TreeArgs& a, const TreeReq& rq,
+                                             const TreeKeys& ks, int e, int keys, int deepest) {
+  const int thr = ks.pre + rq.base + deepest - a.W - ks.j0;
+  return e + keys > ks.nold || (e + keys > ks.pre && max(e, ks.pre) <= thr);
+}
+__device__ __forceinline__ bool hides_new(const TreeArgs& a, const TreeKeys& ks, int e, int keys,
+                                          int n0, int n1) {
+  return a.depth || !(e + keys <= ks.a0 ||
+                      (e >= ks.a0 && e + keys <= ks.nnew && ks.node(e + keys - 1) <= n0 &&
+                       ks.node(e) > n1 - a.W));
+}
+
+// Elements of a K or V row in LDS.  Padded so that neither the K operand's
+// reads (16 rows, 16 bytes each, side by side) nor the transposed V reads
+// (8 rows, 32 bytes each) meet in a bank; addresses are then a lane's base and
+// constants (swizzled rows without padding cost a register per address).
+template <int D>
+constexpr int kKRow = D + 8;
+template <int D>
+constexpr int kVRow = D + 16;
+
+// A wave's NB blocks of 32 query rows against tiles of keys in LDS.
+//
+// Both products run on the matrix cores with the keys as rows, S^T = K Q^T and
+// O^T = V^T P^T (v_mfma_f32_32x32x16_bf16).  A lane then holds scores, weights
+// and outputs of one query row of each block (lane % 32) only: the running
+// maximum and the rescale need one exchange, with the lane's other half, and the
+// weights are the second product's operand where they are.  V comes back from
+// LDS transposed (ds_read_b64_tr_b16) in the order of keys the weights have.
+template <int D, bool F32, int NB>
+struct TreeWave {
+  bf16x8 qf[NB][D / 16];
+  f32x16 o[NB][D / 32];
+  float m[NB], l[NB];
+
+  // Queries: the second operand of S^T, elements 16 s + 8 hh .. of the row.
+  __device__ __forceinline__ void start(const TreeArgs& a, int lane, int nb, const uint16_t* q) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      uint4 x = *reinterpret_cast<const uint4*>(q + 16 * s + 8 * (lane >> 5));
+      x.x ^= a.q_sign;
+      x.y ^= a.q_sign;
+      x.z ^= a.q_sign;
+      x.w ^= a.q_sign;
+      qf[nb][s] = __builtin_bit_cast(bf16x8, x);
+    }
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[nb][c][i] = 0.f;
+    m[nb] = kTreeMin;
+    l[nb] = 0.f;
+  }
+
+  // Four keys from `key` on, 16 columns of block c: see kernels above.
+  static __device__ __forceinline__ uint2 vread(const uint16_t* lv, int lane, int key, int c) {
+    const int s16 = lane & 15, r = key + (s16 >> 2);
+    return __builtin_bit_cast(
+        uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                   (__attribute__((address_space(3))) s16x4*)(
+                       lv + r * kVRow<D> + 32 * c + 16 * ((lane >> 4) & 1) + 4 * (s16 & 3))));
+  }
+
+  // A tile of 32 KB keys.  sl: score scale (positive), flip: of negated scores;
+  // vs: scale of V; see: the keys each row sees, used where `hides`.
+  template <int KB>
+  __device__ __forceinline__ void tile(int lane, const uint16_t* lk, const uint16_t* lv, float sl,
+                                       bool flip, float vs, bool hides,
+                                       const uint32_t (&see)[NB][KB]) {
+    const int lq = lane & 31, hh = lane >> 5;
+    f32x16 sc[NB][KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[nb][kb][i] = 0.f;
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) {
+        const bf16x8 kf =
+            *reinterpret_cast<const bf16x8*>(lk + (32 * kb + lq) * kKRow<D> + 16 * s + 8 * hh);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+          sc[nb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[nb][s], sc[nb][kb], 0, 0, 0);
+      }
+    }
+    // Lane (lq, hh) holds row lq's scores of keys 32 kb + 8 (i / 4) + 4 hh + i % 4.
+    if (flip) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[nb][kb][i] = -sc[nb][kb][i];
+    }
+    if (hides) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const uint32_t w = see[nb][kb] >> (4 * hh);
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            sc[nb][kb][i] =
+                w & (1u << (8 * (i / 4) + i % 4)) ? sc[nb][kb][i] : -__builtin_inff();
+        }
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float mx = sc[nb][0][0];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[nb][kb][i]);
+      float x1, x2;
+      xor_pair<32>(mx, x1, x2);
+      const float mnew = fmaxf(m[nb], fmaxf(x1, x2) * sl);
+      if (__ballot(mnew > m[nb])) {
+        const float alpha = fast_exp2(m[nb] - mnew);
+        l[nb] *= alpha;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[nb][c][i] *= alpha;
+        m[nb] = mnew;
+      }
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          sc[nb][kb][i] = fast_exp2(fmaf(sc[nb][kb][i], sl, -m[nb]));
+          l[nb] += sc[nb][kb][i];
+          if (vs != 1.f) sc[nb][kb][i] *= vs;
+        }
+    }
+    // P.V, 16 keys a step.  Half hh's eight operand slots are the keys 4 hh ..
+    // + 3 and 8 + 4 hh .. + 3 of the step, and V is read in that order.  For
+    // fp32 outputs the weights go in as three bf16 terms, which hold all their
+    // 24 bits; for bf16 outputs rounded to one, off by half a step as the
+    // outputs are.
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        constexpr int NE = F32 ? 3 : 1;
+        bf16x8 pf[NB][NE];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          uint32_t w[NE][4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float u = sc[nb][kb][8 * s + 2 * j], v = sc[nb][kb][8 * s + 2 * j + 1];
+            if constexpr (F32) {
+#pragma unroll
+              for (int e = 0; e < NE; ++e) {
+                w[e][j] = high_halves(u, v);
+                u -= __uint_as_float(__float_as_uint(u) & 0xffff0000u);
+                v -= __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+              }
+            } else {
+              w[0][j] = pack_bf16(u, v);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < NE; ++e)
+            pf[nb][e] = __builtin_bit_cast(bf16x8, make_uint4(w[e][0], w[e][1], w[e][2], w[e][3]));
+        }
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          const uint2 va = vread(lv, lane, 32 * kb + 16 * s + 4 * hh, c);
+          const uint2 vb = vread(lv, lane, 32 * kb + 16 * s + 8 + 4 * hh, c);
+          const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(va.x, va.y, vb.x, vb.y));
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < NE; ++e)
+              o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[nb][e], o[nb][c], 0, 0, 0);
+        }
+      }
+  }
+
+  // Adds the infinities and NaN of V row v to the rows that see its key: as
+  // products of 1 and the largest bf16 values, whose sum overflows where it is
+  // added, and of 0 where the key is hidden.  A NaN is both infinities.
+  __device__ __forceinline__ void add_nonfinite(int lane, const uint16_t* v,
+                                                const bool (&mine)[NB]) {
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      const uint32_t x = v[32 * c + (lane & 31)], size = x & 0x7fffu;
+      const uint32_t up = x == 0x7f80u || size > 0x7f80u ? 0x7f7f7f7fu : 0u;
+      const uint32_t down = x == 0xff80u || size > 0x7f80u ? 0xff7fff7fu : 0u;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const uint32_t one = mine[nb] ? 0x3f803f80u : 0u;
+        const bf16x8 p = __builtin_bit_cast(bf16x8, make_uint4(one, one, one, one));
+        o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, make_uint4(up, up, up, up)), p, o[nb][c], 0, 0, 0);
+        o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, make_uint4(down, down, down, down)), p, o[nb][c], 0, 0, 0);
+      }
+    }
+  }
+};
+
+// Scales of the scores and of V over the cache.  Scores are compared before they
+// are scaled, so the scale is positive: a negative one flips the scores, a
+// zero one is as good as the smallest.
+struct CacheScale {
+  float sl, vs;
+  bool flip;
+};
+template <bool FP8>
+__device__ __forceinline__ CacheScale cache_scale(const TreeArgs& a, int pair) {
+  CacheScale c{a.scale_log2, 1.f, false};
+  if constexpr (FP8) {
+    if (a.ks) c.sl *= a.ks[pair];
+    if (a.vs) c.vs = a.vs[pair];
+    c.flip = c.sl < 0.f;
+    c.sl = fmaxf(fabsf(c.sl), kTreeMinScale);
+  }
+  return c;
+}
+
+// In a tile with hidden keys a V row's infinity or NaN would reach queries that
+// must not see it, as 0 times it.  Such elements become 0 in LDS, and
+// add_nonfinite adds them where they are seen.  Each lane takes the N chunks of 16
+// bytes it has just stored, chunk i at `v` + i * step, D / 8 lanes to a row;
+// returns the rows that had any: bit i * (512 / D) + g for row g of pass i.  (A
+// loop over LDS: the same on the registers before they are stored costs 20 more.)
+template <int D>
+__device__ __forceinline__ uint32_t clean_rows(uint16_t* v, int n, int step) {
+  constexpr int CPR = D / 8, RPW = 64 / CPR;
+  uint32_t rows = 0;
+#pragma unroll 1
+  for (int i = 0; i < n; ++i, v += step) {
+    const uint4 x = *reinterpret_cast<const uint4*>(v);
+    const bool mine = (nonfinite_bit(x) & 0x8000u) != 0;
+    const uint64_t who = __ballot(mine);
+    if (!who) continue;
+    if (mine)
+      *reinterpret_cast<uint4*>(v) =
+          make_uint4(finite_pair(x.x), finite_pair(x.y), finite_pair(x.z), finite_pair(x.w));
+#pragma unroll
+    for (int g = 0; g < RPW; ++g)
+      rows |= (who >> (g * CPR) & ((1ull << CPR) - 1)) ? 1u << (i * RPW + g) : 0u;
+  }
+  return rows;
+}
+
+// Outputs of a finished block of 32 rows, or its partial result.
+template <int D, bool F32>
+__device__ __forceinline__ void tree_write(const TreeArgs& a, int lane, const f32x16 (&o)[D / 32],
+                                           float inv, int64_t out) {
+  const int64_t at = out * D + 4 * (lane >> 5);
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      store4<F32>(a.out, at + 32 * c + 2 * i, o[c][i] * inv, o[c][i + 1] * inv, o[c][i + 2] * inv,
+                  o[c][i + 3] * inv);
+}
+
+// Splits of a row tile that have keys, and the tiles of 'part' of 'parts'.
+__device__ __forceinline__ int tree_splits(const TreeArgs& a, int tiles) {
+  return min(a.splits, (tiles + a.split_tiles - 1) / a.split_tiles);
+}
+__device__ __forceinline__ int tree_cut(int tiles, int part, int parts) {
+  return static_cast<int>(static_cast<int64_t>(tiles) * part / parts);
+}
+
+// ---- many query rows -----------------------------------------------------------
+
+constexpr int kTileRows = 128;  // query rows of a workgroup: four waves of 32
+constexpr int kTileKeys = 64;   // keys of a tile
+
 // A workgroup of four waves takes 128 query rows (node, query head of the KV
 // head's group) of one request and KV head, and a share of the keys.  Tiles of
-// 64 keys go through LDS, two buffers in turn.  Both products run on the matrix
-// cores with the keys as rows, S^T = K Q^T and O^T = V^T P^T
-// (v_mfma_f32_32x32x16_bf16): a lane then holds scores, weights and outputs of
-// one query row (lane % 32) only, so the running maximum and the rescale need
-// no exchange but one with the lane's other half, and the weights are the second
-// product's operand where they are.  V comes back from LDS transposed
-// (ds_read_b64_tr_b16) in the key order the weights have.
+// 64 keys go through LDS for all four waves, two buffers in turn.
 template <bool FP8, int D, bool F32>
-__global__ __launch_bounds__(256, FP8 && D == 128 ? 1 : 2) void tree_tile_kernel(TreeArgs a) {
+__global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
   constexpr int CPR = D / 8;           // 16-byte chunks of a bf16 row
   constexpr int NP = CPR * kTileKeys / 256;
   constexpr int RPP = 256 / CPR;       // rows per pass of the workgroup
   constexpr int CP8 = D / 16, NP8 = CP8 * kTileKeys / 256, RP8 = 256 / CP8;
-  __shared__ __align__(16) uint16_t lk[2][kTileKeys * D];
-  __shared__ __align__(16) uint16_t lv[2][kTileKeys * D];
-  __shared__ uint64_t lbad[2][4];  // keys of a tile whose V row is not finite, by wave
+  __shared__ __align__(16) uint16_t lk[2][kTileKeys * kKRow<D>];
+  __shared__ __align__(16) uint16_t lv[2][kTileKeys * kVRow<D>];
+  __shared__ uint32_t lbad[2][4];  // V rows of a tile that are not finite, by wave (clean_rows)
 
   const int per_pair = a.row_tiles * a.splits;
   const int item = xcd_item(a.B * a.Hkv * per_pair);
@@ -119,352 +431,372 @@ __global__ __launch_bounds__(256, FP8 && D == 128 ? 1 : 2) void tree_tile_kernel
   const TreeKeys ks = tree_keys(a, rq, n0, n1);
   const int t_old = (ks.nold + kTileKeys - 1) / kTileKeys;
   const int tiles = t_old + (ks.nnew + kTileKeys - 1) / kTileKeys;
-  const int nsp = min(a.splits, tiles);
+  const int nsp = tree_splits(a, tiles);
   if (sp >= nsp) return;
-  const int t0 = static_cast<int>(static_cast<int64_t>(tiles) * sp / nsp);
-  const int t1 = static_cast<int>(static_cast<int64_t>(tiles) * (sp + 1) / nsp);
+  const int t0 = tree_cut(tiles, sp, nsp), t1 = tree_cut(tiles, sp + 1, nsp);
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int lq = lane & 31, hh = lane >> 5;
-  const int row = r0 + 32 * wave + lq;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int row = r0 + 32 * wave + (lane & 31);
   const bool wave_on = r0 + 32 * wave < rows;
-  const int node = min(row, rows - 1) / a.G, head = h * a.G + min(row, rows - 1) % a.G;
-  const bool chain = a.depth == nullptr;
-  const int dep = chain ? node : a.depth[b * a.N + node];
-  const int deepest = chain ? n1 : a.max_depth[b];
-  const int p = rq.base + dep;
-  const int thr = ks.pre + p - a.W - ks.j0;                       // cached entries past pre: visible above
-  const int thr_max = ks.pre + rq.base + deepest - a.W - ks.j0;
-  const int sink_node = a.S - rq.base;                            // depths below stand at sink positions
-  const uint32_t* anc = chain ? nullptr : a.anc + (static_cast<int64_t>(b) * a.N + node) * a.words;
-  const int32_t* depths = chain ? nullptr : a.depth + static_cast<int64_t>(b) * a.N;
-
-  // Scores are compared before they are scaled, so scales are positive here: a
-  // negative one flips the scores, a zero one is as good as the smallest.
-  float kscale = a.scale_log2, vscale = 1.f;
-  bool flip = false;
-  if constexpr (FP8) {
-    if (a.ks) kscale *= a.ks[pair];
-    if (a.vs) vscale = a.vs[pair];
-    flip = kscale < 0.f;
-    kscale = fmaxf(fabsf(kscale), kTreeMinScale);
-  }
-
-  // Queries: the second operand of S^T, lane (row lq, elements 16 s + 8 hh ..).
-  bf16x8 qf[D / 16];
-  {
-    const uint16_t* q = a.q + b * a.qsb + node * a.qsn + head * a.qsh;
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      uint4 x = *reinterpret_cast<const uint4*>(q + 16 * s + 8 * hh);
-      x.x ^= a.q_sign;
-      x.y ^= a.q_sign;
-      x.z ^= a.q_sign;
-      x.w ^= a.q_sign;
-      qf[s] = __builtin_bit_cast(bf16x8, x);
-    }
-  }
+  const TreeRow my = tree_row(a, rq, ks, b, h, min(row, rows - 1));
+  const int deepest = a.depth ? a.max_depth[b] : n1;
+  const int sink = a.S - rq.base;
+  const CacheScale cs = cache_scale<FP8>(a, pair);
+  TreeWave<D, F32, 1> w;
+  w.start(a, lane, 0,
+          a.q + b * a.qsb + my.node * a.qsn + (h * a.G + min(row, rows - 1) % a.G) * a.qsh);
 
   const int64_t cbase = tree_cache_base(a, b, h, FP8 ? 1 : 2);
   const uint16_t* kn = a.kn + b * a.nsb + h * a.nsh;
   const uint16_t* vn = a.vn + b * a.nsb + h * a.nsh;
   uint4 rk[NP], rv[NP];
-  const uint4 zero = make_uint4(0, 0, 0, 0);
-  auto load = [&](int t) {
-    if (t < t_old) {
-      if constexpr (FP8) {
+
+  // A tile of bf16 rows (new ones, or the cache's) into LDS.
+  auto put = [&](int buf, bool hides) {
+    const int c = tid % CPR;
 #pragma unroll
-        for (int i = 0; i < NP8; ++i) {
-          const int r = t * kTileKeys + i * RP8 + tid / CP8;
-          rk[i] = rv[i] = zero;
-          if (r < ks.nold) {
-            const int64_t at = cbase + ks.row(r) * a.sr + (tid % CP8) * 16;
-            rk[i] = load_stream16(a.k + at);
-            rv[i] = load_stream16(a.v + at);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          const int r = t * kTileKeys + i * RPP + tid / CPR;
-          rk[i] = rv[i] = zero;
-          if (r < ks.nold) {
-            const int64_t at = cbase + ks.row(r) * a.sr + (tid % CPR) * 16;
-            rk[i] = load_stream16(a.k + at);
-            rv[i] = load_stream16(a.v + at);
-          }
-        }
+    for (int i = 0; i < NP; ++i) {
+      const int r = i * RPP + tid / CPR;
+      *reinterpret_cast<uint4*>(lk[buf] + r * kKRow<D> + (c) * 8) = rk[i];
+      *reinterpret_cast<uint4*>(lv[buf] + r * kVRow<D> + (c) * 8) = rv[i];
+    }
+    uint32_t bad = 0;
+    if (hides) bad = clean_rows<D>(lv[buf] + (tid / CPR) * kVRow<D> + c * 8, NP, RPP * kVRow<D>);
+    if (lane == 0) lbad[buf][wave] = bad;
+  };
+  auto add_hidden = [&](int buf, const uint32_t (&see)[1][2], auto&& row_of) {
+    constexpr int RPW = 64 / CPR;  // rows of a wave's pass
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i)
+#pragma unroll 1
+      for (uint32_t bad = lbad[buf][i]; bad; bad &= bad - 1) {
+        const int at = __builtin_ctz(bad), e = at / RPW * RPP + i * RPW + at % RPW;
+        const bool mine[1] = {static_cast<bool>((see[0][e >> 5] >> (e & 31)) & 1u)};
+        w.add_nonfinite(lane, row_of(e), mine);
       }
-    } else {
+  };
+
+  // The cache's tiles.
+  auto load_old = [&](int t) {
+    constexpr int N = FP8 ? NP8 : NP, R = FP8 ? RP8 : RPP, C = FP8 ? CP8 : CPR;
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const int x = (t - t_old) * kTileKeys + i * RPP + tid / CPR;
-        rk[i] = rv[i] = zero;
-        if (x < ks.nnew) {
-          const int64_t at = ks.node(x) * a.nsn + (tid % CPR) * 8;
-          rk[i] = *reinterpret_cast<const uint4*>(kn + at);
-          rv[i] = *reinterpret_cast<const uint4*>(vn + at);
-        }
-      }
+    for (int i = 0; i < N; ++i) {
+      const int r = min(t * kTileKeys + i * R + tid / C, ks.nold - 1);
+      const int64_t at = cbase + ks.row(r) * a.sr + (tid % C) * 16;
+      rk[i] = load_stream16(a.k + at);
+      rv[i] = load_stream16(a.v + at);
     }
   };
-  // Chunk c of row r lies at chunk c ^ (r mod CPR) of its row: rows start at
-  // the same banks, and the lanes of a read go down the rows.
-  auto put = [&](uint16_t* buf, int r, int c, const uint4& x) {
-    *reinterpret_cast<uint4*>(buf + r * D + ((c ^ (r & (CPR - 1))) * 8)) = x;
+  auto hides_old = [&](int t) {
+    return hides_cached(a, rq, ks, t * kTileKeys, kTileKeys, deepest);
   };
-  // Whether some query of the workgroup must not see some key of tile t.
-  auto masked = [&](int t) {
-    if (t < t_old) {
-      const int r = t * kTileKeys;
-      return r + kTileKeys > ks.nold || (r + kTileKeys > ks.pre && max(r, ks.pre) <= thr_max);
-    }
-    const int x = (t - t_old) * kTileKeys;
-    return !chain || !(x + kTileKeys <= ks.a0 ||
-                       (x >= ks.a0 && x + kTileKeys <= ks.nnew &&
-                        ks.node(x + kTileKeys - 1) <= n0 && ks.node(x) > n1 - a.W));
-  };
-  auto store = [&](int t, int buf) {
-    if (FP8 && t < t_old) {
+  auto put_old = [&](int t, int buf) {
+    if constexpr (FP8) {
 #pragma unroll
       for (int i = 0; i < NP8; ++i) {
         const int r = i * RP8 + tid / CP8, c = 2 * (tid % CP8);
         uint4 lo, hi;
         widen_fp8(rk[i], lo, hi);
-        put(lk[buf], r, c, lo);
-        put(lk[buf], r, c + 1, hi);
+        *reinterpret_cast<uint4*>(lk[buf] + r * kKRow<D> + (c) * 8) = lo;
+        *reinterpret_cast<uint4*>(lk[buf] + r * kKRow<D> + (c + 1) * 8) = hi;
         widen_fp8(rv[i], lo, hi);
-        put(lv[buf], r, c, lo);
-        put(lv[buf], r, c + 1, hi);
+        *reinterpret_cast<uint4*>(lv[buf] + r * kVRow<D> + (c) * 8) = lo;
+        *reinterpret_cast<uint4*>(lv[buf] + r * kVRow<D> + (c + 1) * 8) = hi;
       }
-      if (lane == 0) lbad[buf][wave] = 0;
-      return;
+    } else {
+      put(buf, hides_old(t));
     }
-    // In a tile with hidden keys a V row's infinity or NaN would reach queries
-    // that must not see it, as 0 times it.  Such elements go in as 0, and
-    // compute() adds them where they are seen.
-    uint64_t bad = 0;
-    if (masked(t)) {
-#pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const bool mine = has_nonfinite(rv[i]);
-        const uint64_t who = __ballot(mine);
-        if (who) {
-          if (mine)
-            rv[i] = make_uint4(finite_pair(rv[i].x), finite_pair(rv[i].y), finite_pair(rv[i].z),
-                               finite_pair(rv[i].w));
-#pragma unroll 1
-          for (int g = 0; g < 64 / CPR; ++g)
-            if (who >> (g * CPR) & ((1ull << CPR) - 1))
-              bad |= 1ull << (i * RPP + wave * (64 / CPR) + g);
+  };
+  int t = t0, buf = 0;
+  const int e_old = min(t1, t_old);
+  if (t < e_old) {
+    load_old(t);
+    put_old(t, 0);
+    __syncthreads();
+    for (; t < e_old; ++t, buf ^= 1) {
+      if (t + 1 < e_old) load_old(t + 1);
+      if (wave_on) {
+        const bool hides = hides_old(t);
+        uint32_t see[1][2] = {};
+        if (hides) {
+          see[0][0] = see_cached(ks, my, t * kTileKeys);
+          see[0][1] = see_cached(ks, my, t * kTileKeys + 32);
         }
+        w.template tile<2>(lane, lk[buf], lv[buf], cs.sl, FP8 && cs.flip, FP8 ? cs.vs : 1.f, hides,
+                           see);
+        if (!FP8 && hides)
+          add_hidden(buf, see, [&](int e) {
+            return reinterpret_cast<const uint16_t*>(a.v + cbase + ks.row(t * kTileKeys + e) * a.sr);
+          });
       }
+      if (t + 1 < e_old) put_old(t + 1, buf ^ 1);
+      __syncthreads();
     }
+  }
+
+  // The new tokens' tiles.
+  auto load_new = [&](int x0) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int r = i * RPP + tid / CPR, c = tid % CPR;
-      put(lk[buf], r, c, rk[i]);
-      put(lv[buf], r, c, rv[i]);
-    }
-    if (lane == 0) lbad[buf][wave] = bad;
-  };
-
-  f32x16 o[D / 32];
-#pragma unroll
-  for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
-  float m = kTreeMin, l = 0.f;
-
-  // Transposed V reads: see the two row orders in the comment above pv.
-  const int s16 = lane & 15;
-  auto vread = [&](const uint16_t* buf, int key, int c) {  // 4 keys from `key`, 16 columns
-    const int r = key + (s16 >> 2);
-    const int ch = 4 * c + 2 * ((lane >> 4) & 1) + ((s16 & 3) >> 1);
-    return __builtin_bit_cast(
-        uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                   (__attribute__((address_space(3))) s16x4*)(
-                       buf + r * D + ((ch ^ (r & (CPR - 1))) * 8) + 4 * (s16 & 1))));
-  };
-
-  auto compute = [&](int t, int buf) {
-    f32x16 sc[2];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
-      const int r = 32 * kb + lq;
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(
-            lk[buf] + r * D + (((2 * s + hh) ^ (r & (CPR - 1))) * 8));
-        sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], sc[kb], 0, 0, 0);
-      }
-    }
-    // Lane (lq, hh) holds row lq's scores of keys 32 kb + 8 (i / 4) + 4 hh + i % 4.
-    const bool old = t < t_old;
-    const float sl = FP8 && old ? kscale : a.scale_log2;
-    const bool hides = masked(t);
-    if (FP8 && old && flip) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[kb][i] = -sc[kb][i];
-    }
-    uint32_t see[2] = {~0u, ~0u};
-    if (hides) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        if (old) {
-          const int e = t * kTileKeys + 32 * kb;
-          see[kb] = low_bits(ks.nold - e) & (low_bits(ks.pre - e) | ~low_bits(thr + 1 - e));
-        } else {
-          const int e = (t - t_old) * kTileKeys + 32 * kb;
-          see[kb] = low_bits(ks.nnew - e);
-          if (chain) {  // nodes from a1 on follow the first a0, which every node sees
-            const int f = ks.a0 - ks.a1 - e;
-            see[kb] &= low_bits(node + 1 + f) & (low_bits(ks.a0 - e) | low_bits(sink_node + f) |
-                                                 ~low_bits(node - a.W + 1 + f));
-          } else {
-            uint32_t m = e / 32 < a.words ? anc[e / 32] : 0u;
-            see[kb] &= m;
-            if (deepest >= a.W) {
-              m = see[kb];
-              while (m) {
-                const int i = __builtin_ctz(m), de = depths[e + i];
-                m &= m - 1;
-                if (de >= sink_node && dep - de >= a.W) see[kb] &= ~(1u << i);
-              }
-            }
-          }
-        }
-        const uint32_t w = see[kb] >> (4 * hh);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          sc[kb][i] = w & (1u << (8 * (i / 4) + i % 4)) ? sc[kb][i] : -__builtin_inff();
-      }
-    }
-    float mx = sc[0][0];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[kb][i]);
-    float x1, x2;
-    xor_pair<32>(mx, x1, x2);
-    const float mnew = fmaxf(m, fmaxf(x1, x2) * sl);
-    if (__ballot(mnew > m)) {
-      const float alpha = fast_exp2(m - mnew);
-      l *= alpha;
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[c][i] *= alpha;
-      m = mnew;
-    }
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[kb][i] = fast_exp2(fmaf(sc[kb][i], sl, -m));
-        l += sc[kb][i];
-        if (FP8) sc[kb][i] *= old ? vscale : 1.f;
-      }
-    // P.V.  A step takes 16 keys; the weights' order gives half hh's eight
-    // operand slots the keys 4 hh .. + 3 and 8 + 4 hh .. + 3 of the step, and V
-    // is read in the same order.
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        bf16x8 pf[F32 ? 3 : 1];
-        if constexpr (F32) {
-          uint32_t w[3][4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float u = sc[kb][8 * s + 2 * j], v = sc[kb][8 * s + 2 * j + 1];
-#pragma unroll
-            for (int e = 0; e < 3; ++e) {
-              w[e][j] = high_halves(u, v);
-              u -= __uint_as_float(__float_as_uint(u) & 0xffff0000u);
-              v -= __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-            }
-          }
-#pragma unroll
-          for (int e = 0; e < 3; ++e)
-            pf[e] = __builtin_bit_cast(bf16x8, make_uint4(w[e][0], w[e][1], w[e][2], w[e][3]));
-        } else {
-          uint32_t w[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            w[j] = pack_bf16(sc[kb][8 * s + 2 * j], sc[kb][8 * s + 2 * j + 1]);
-          pf[0] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-        }
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          const uint2 va = vread(lv[buf], 32 * kb + 16 * s + 4 * hh, c);
-          const uint2 vb = vread(lv[buf], 32 * kb + 16 * s + 8 + 4 * hh, c);
-          const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(va.x, va.y, vb.x, vb.y));
-#pragma unroll
-          for (int e = 0; e < (F32 ? 3 : 1); ++e)
-            o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[e], o[c], 0, 0, 0);
-        }
-      }
-    if (!hides) return;
-    uint64_t bad = lbad[buf][0] | lbad[buf][1] | lbad[buf][2] | lbad[buf][3];
-#pragma unroll 1
-    for (; bad; bad &= bad - 1) {
-      const int e = __builtin_ctzll(bad), at = (old ? t : t - t_old) * kTileKeys + e;
-      const bool mine = (see[e >> 5] >> (e & 31)) & 1u;
-      const uint16_t* vr = old ? reinterpret_cast<const uint16_t*>(a.v + cbase + ks.row(at) * a.sr)
-                               : vn + ks.node(at) * a.nsn;
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const uint2 x = *reinterpret_cast<const uint2*>(vr + 32 * c + 2 * i + 4 * hh);
-          const float f[4] = {bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y)};
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            o[c][i + j] += mine && !__builtin_isfinite(f[j]) ? f[j] : 0.f;
-        }
+      const int x = min(x0 + i * RPP + tid / CPR, ks.nnew - 1);
+      const int64_t at = ks.node(x) * a.nsn + (tid % CPR) * 8;
+      rk[i] = *reinterpret_cast<const uint4*>(kn + at);
+      rv[i] = *reinterpret_cast<const uint4*>(vn + at);
     }
   };
-
-  load(t0);
-  store(t0, 0);
-  __syncthreads();
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
-    if (t + 1 < t1) load(t + 1);
-    if (wave_on) compute(t, buf);
-    if (t + 1 < t1) store(t + 1, buf ^ 1);
+  auto hides_at = [&](int x) { return hides_new(a, ks, x, kTileKeys, n0, n1); };
+  if (t < t1) {
+    const int end = (t1 - t_old) * kTileKeys;
+    int x = (t - t_old) * kTileKeys;
+    load_new(x);
+    put(buf, hides_at(x));
     __syncthreads();
+    for (; x < end; x += kTileKeys, buf ^= 1) {
+      if (x + kTileKeys < end) load_new(x + kTileKeys);
+      if (wave_on) {
+        const bool hides = hides_at(x);
+        uint32_t see[1][2] = {};
+        if (hides) {
+          see[0][0] = see_new(a, ks, my, b, x, sink, deepest >= a.W);
+          see[0][1] = see_new(a, ks, my, b, x + 32, sink, deepest >= a.W);
+        }
+        w.template tile<2>(lane, lk[buf], lv[buf], a.scale_log2, false, 1.f, hides, see);
+        if (hides)
+          add_hidden(buf, see, [&](int e) { return vn + ks.node(x + e) * a.nsn; });
+      }
+      if (x + kTileKeys < end) put(buf ^ 1, hides_at(x + kTileKeys));
+      __syncthreads();
+    }
   }
 
   float l1, l2;
-  xor_pair<32>(l, l1, l2);
-  l = l1 + l2;
+  xor_pair<32>(w.l[0], l1, l2);
+  const float l = l1 + l2;
   if (row >= rows) return;
   if (nsp == 1) {
-    const float inv = 1.f / l;
-    const int64_t at = ((static_cast<int64_t>(b) * a.N + node) * a.Hq + head) * D + 4 * hh;
+    tree_write<D, F32>(a, lane, w.o[0], 1.f / l, my.out);
+    return;
+  }
+  float* part = a.part + ((static_cast<int64_t>(pair) * a.row_tiles + qt) * a.splits + sp) *
+                             kTileRows * kPartRow<D> +
+                (row - r0) * kPartRow<D>;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      *reinterpret_cast<float4*>(part + 32 * c + 2 * i + 4 * (lane >> 5)) =
+          make_float4(w.o[0][c][i], w.o[0][c][i + 1], w.o[0][c][i + 2], w.o[0][c][i + 3]);
+  if (lane < 32) *reinterpret_cast<float2*>(part + D) = make_float2(w.m[0], l);
+}
+
+// ---- few query rows --------------------------------------------------------------
+
+constexpr int kStreamKeys = 32;  // keys of a wave's tile
+
+template <int D>
+constexpr uint32_t kStreamLds = kStreamKeys * (kKRow<D> + kVRow<D>) * 2;  // a wave's K and V tile, bytes
+
+// At most 32 NB query rows per (request, KV head): bound by the cache's bytes.
+// Every wave streams tiles of 32 keys of its own for all rows, through registers
+// (the next tiles are on their way while one is computed) and an LDS region of
+// its own, so the waves of a workgroup wait for each other only to join
+// their results at the end.
+template <bool FP8, int D, bool F32, int NB, int NW>
+__global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeArgs a) {
+  constexpr int CPR = D / 8, RPP = 64 / CPR, NP = kStreamKeys / RPP;  // bf16 rows
+  constexpr int C = FP8 ? D / 16 : CPR, R = 64 / C, N = kStreamKeys / R;  // the cache's
+  constexpr int PF = N > 4 ? 1 : 2;  // tiles in flight ahead of the one at hand
+  __shared__ __align__(16) uint16_t lds[NW * (kStreamLds<D> / 2)];
+  __shared__ float lm[NW][32], ll[NW][32];
+
+  const int item = xcd_item(a.B * a.Hkv * a.splits);
+  if (item < 0) return;
+  const int pair = item / a.splits, sp = item % a.splits;
+  const int b = pair / a.Hkv, h = pair % a.Hkv;
+  const TreeReq rq = tree_request(a.base, a.count, b, a.N, a.Lp, a.Ldec);
+  const int rows = rq.n * a.G;
+  if (rows == 0) return;
+  const int n1 = rq.n - 1;
+  const TreeKeys ks = tree_keys(a, rq, 0, n1);
+  const int t_old = (ks.nold + kStreamKeys - 1) / kStreamKeys;
+  const int tiles = t_old + (ks.nnew + kStreamKeys - 1) / kStreamKeys;
+  const int nsp = tree_splits(a, tiles);
+  if (sp >= nsp) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t0 = tree_cut(tiles, sp * NW + wave, nsp * NW);
+  const int t1 = tree_cut(tiles, sp * NW + wave + 1, nsp * NW);
+
+  uint16_t* lk = lds + wave * (kStreamLds<D> / 2);
+  uint16_t* lv = lk + kStreamKeys * kKRow<D>;
+  const int64_t cbase = tree_cache_base(a, b, h, FP8 ? 1 : 2);
+  uint4 rk[PF][N], rv[PF][N];
+  auto load_old = [&](int t, uint4 (&k)[N], uint4 (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = min(t * kStreamKeys + i * R + lane / C, ks.nold - 1);
+      const int64_t at = cbase + ks.row(r) * a.sr + (lane % C) * 16;
+      k[i] = load_stream16(a.k + at);
+      v[i] = load_stream16(a.v + at);
+    }
+  };
+  const int e_old = min(t1, t_old);
+#pragma unroll
+  for (int j = 0; j < PF; ++j)
+    if (t0 + j < e_old) load_old(t0 + j, rk[j], rv[j]);
+
+  TreeRow my[NB];
+  TreeWave<D, F32, NB> w;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int row = min(32 * nb + (lane & 31), rows - 1);
+    my[nb] = tree_row(a, rq, ks, b, h, row);
+    w.start(a, lane, nb,
+            a.q + b * a.qsb + my[nb].node * a.qsn + (h * a.G + row % a.G) * a.qsh);
+  }
+  const int deepest = a.depth ? a.max_depth[b] : n1;
+  const CacheScale cs = cache_scale<FP8>(a, pair);
+
+  auto add_hidden = [&](uint32_t bad, const uint32_t (&see)[NB][1], auto&& row_of) {
+#pragma unroll 1
+    for (; bad; bad &= bad - 1) {
+      const int e = __builtin_ctz(bad);
+      bool mine[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) mine[nb] = (see[nb][0] >> e) & 1u;
+      w.add_nonfinite(lane, row_of(e), mine);
+    }
+  };
+
+  for (int t = t0; t < e_old; t += PF) {
+#pragma unroll
+    for (int j = 0; j < PF; ++j) {
+      if (t + j >= e_old) break;
+      const int e0 = (t + j) * kStreamKeys;
+      const bool hides = hides_cached(a, rq, ks, e0, kStreamKeys, deepest);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int r = i * R + lane / C;
+        if constexpr (FP8) {
+          const int c = 2 * (lane % C);
+          uint4 lo, hi;
+          widen_fp8(rk[j][i], lo, hi);
+          *reinterpret_cast<uint4*>(lk + r * kKRow<D> + (c) * 8) = lo;
+          *reinterpret_cast<uint4*>(lk + r * kKRow<D> + (c + 1) * 8) = hi;
+          widen_fp8(rv[j][i], lo, hi);
+          *reinterpret_cast<uint4*>(lv + r * kVRow<D> + (c) * 8) = lo;
+          *reinterpret_cast<uint4*>(lv + r * kVRow<D> + (c + 1) * 8) = hi;
+        } else {
+          *reinterpret_cast<uint4*>(lk + r * kKRow<D> + (lane % C) * 8) = rk[j][i];
+          *reinterpret_cast<uint4*>(lv + r * kVRow<D> + (lane % C) * 8) = rv[j][i];
+        }
+      }
+      if (t + j + PF < e_old) load_old(t + j + PF, rk[j], rv[j]);
+      uint32_t bad = 0;
+      if (!FP8 && hides) bad = clean_rows<D>(lv + (lane / C) * kVRow<D> + (lane % C) * 8, N, R * kVRow<D>);
+      fence_wave();
+      uint32_t see[NB][1] = {};
+      if (hides)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) see[nb][0] = see_cached(ks, my[nb], e0);
+      w.template tile<1>(lane, lk, lv, cs.sl, FP8 && cs.flip, FP8 ? cs.vs : 1.f, hides, see);
+      if (!FP8 && bad)
+        add_hidden(bad, see, [&](int e) {
+          return reinterpret_cast<const uint16_t*>(a.v + cbase + ks.row(e0 + e) * a.sr);
+        });
+      fence_wave();
+    }
+  }
+
+  const uint16_t* kn = a.kn + b * a.nsb + h * a.nsh;
+  const uint16_t* vn = a.vn + b * a.nsb + h * a.nsh;
+  for (int t = max(t0, t_old); t < t1; ++t) {
+    const int x0 = (t - t_old) * kStreamKeys;
+    uint4 k[NP], v[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int x = min(x0 + i * RPP + lane / CPR, ks.nnew - 1);
+      const int64_t at = ks.node(x) * a.nsn + (lane % CPR) * 8;
+      k[i] = *reinterpret_cast<const uint4*>(kn + at);
+      v[i] = *reinterpret_cast<const uint4*>(vn + at);
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int r = i * RPP + lane / CPR;
+      *reinterpret_cast<uint4*>(lk + r * kKRow<D> + (lane % CPR) * 8) = k[i];
+      *reinterpret_cast<uint4*>(lv + r * kVRow<D> + (lane % CPR) * 8) = v[i];
+    }
+    const uint32_t bad =
+        clean_rows<D>(lv + (lane / CPR) * kVRow<D> + (lane % CPR) * 8, NP, RPP * kVRow<D>);
+    fence_wave();
+    uint32_t see[NB][1];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+      see[nb][0] = see_new(a, ks, my[nb], b, x0, a.S - rq.base, deepest >= a.W);
+    w.template tile<1>(lane, lk, lv, a.scale_log2, false, 1.f, true, see);
+    add_hidden(bad, see, [&](int e) { return vn + ks.node(x0 + e) * a.nsn; });
+    fence_wave();
+  }
+
+  // Join the waves' results, a block of rows at a time: every wave scales its own
+  // to the common maximum and leaves them in its LDS region, 32 columns of a row
+  // per step, then the workgroup's threads add them up.
+  const bool split = nsp > 1;
+  float* part = a.part + (static_cast<int64_t>(pair) * a.splits + sp) * (32 * NB) * kPartRow<D>;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    float l1, l2;
+    xor_pair<32>(w.l[nb], l1, l2);
+    if (lane < 32) {
+      lm[wave][lane] = w.m[nb];
+      ll[wave][lane] = l1 + l2;
+    }
+    __syncthreads();
+    float M = kTreeMin;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) M = fmaxf(M, lm[i][lane & 31]);
+    const float mine = fast_exp2(w.m[nb] - M);
+    float* red = reinterpret_cast<float*>(lk);  // [32 rows][D], groups of 4 columns swizzled
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        store4<F32>(a.out, at + 32 * c + 2 * i, o[c][i] * inv, o[c][i + 1] * inv,
-                    o[c][i + 2] * inv, o[c][i + 3] * inv);
-  } else {
-    float* part = a.part + ((static_cast<int64_t>(pair) * a.row_tiles + qt) * a.splits + sp) *
-                               kTileRows * kPartRow<D> +
-                  (row - r0) * kPartRow<D>;
+      for (int i = 0; i < 16; i += 4) {
+        const int g = 8 * c + i / 2 + (lane >> 5), r = lane & 31;
+        *reinterpret_cast<float4*>(red + r * D + ((g ^ (r & 15)) * 4)) =
+            make_float4(w.o[nb][c][i] * mine, w.o[nb][c][i + 1] * mine, w.o[nb][c][i + 2] * mine,
+                        w.o[nb][c][i + 3] * mine);
+      }
+    __syncthreads();
+    for (int at = threadIdx.x; at < 32 * (D / 4); at += 64 * NW) {
+      const int r = at / (D / 4), g = at % (D / 4), row = 32 * nb + r;
+      if (row >= rows) break;
+      float mr = kTreeMin, lr = 0.f;
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c)
+      for (int i = 0; i < NW; ++i) mr = fmaxf(mr, lm[i][r]);
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<float4*>(part + 32 * c + 2 * i + 4 * hh) =
-            make_float4(o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]);
-    if (hh == 0) *reinterpret_cast<float2*>(part + D) = make_float2(m, l);
+      for (int i = 0; i < NW; ++i) lr = fmaf(ll[i][r], fast_exp2(lm[i][r] - mr), lr);
+      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < NW; ++i) {
+        const float4 x = *reinterpret_cast<const float4*>(
+            reinterpret_cast<const float*>(lds + i * (kStreamLds<D> / 2)) + r * D +
+            ((g ^ (r & 15)) * 4));
+        s.x += x.x;
+        s.y += x.y;
+        s.z += x.z;
+        s.w += x.w;
+      }
+      if (split) {
+        float* p = part + row * kPartRow<D>;
+        *reinterpret_cast<float4*>(p + 4 * g) = s;
+        if (g == 0) *reinterpret_cast<float2*>(p + D) = make_float2(mr, lr);
+      } else {
+        const float inv = 1.f / lr;
+        const int64_t out = (static_cast<int64_t>(b) * a.N + row / a.G) * a.Hq + h * a.G + row % a.G;
+        store4<F32>(a.out, out * D + 4 * g, s.x * inv, s.y * inv, s.z * inv, s.w * inv);
+      }
+    }
+    if (nb + 1 < NB) __syncthreads();
   }
 }
 
@@ -485,7 +817,7 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a, int tile_
   if (row >= rows) return;
   const TreeKeys ks = tree_keys(a, rq, r0 / a.G, (min(r0 + tile_rows, rows) - 1) / a.G);
   const int tiles = (ks.nold + tile_keys - 1) / tile_keys + (ks.nnew + tile_keys - 1) / tile_keys;
-  const int nsp = min(a.splits, tiles);
+  const int nsp = tree_splits(a, tiles);
   if (nsp <= 1) return;
   const int64_t step = static_cast<int64_t>(tile_rows) * kPartRow<D>;
   const float* part = a.part + (static_cast<int64_t>(pair) * a.row_tiles + qt) * a.splits * step +
@@ -514,15 +846,30 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a, int tile_
   }
 }
 
+template <bool FP8, int D, bool F32, int NB, int NW>
+hipError_t launch_stream(const TreeLaunch& l, const TreeArgs& a, hipStream_t st) {
+  tree_stream_kernel<FP8, D, F32, NB, NW><<<dim3(static_cast<uint32_t>((l.workgroups + 7) / 8 * 8)),
+                                            dim3(64 * NW), 0, st>>>(a);
+  return hipGetLastError();
+}
+
 template <bool FP8, int D, bool F32>
 hipError_t launch_one(const TreeLaunch& l, const TreeArgs& a, hipStream_t st) {
-  tree_tile_kernel<FP8, D, F32><<<dim3(static_cast<uint32_t>((l.workgroups + 7) / 8 * 8)),
-                                  dim3(256), 0, st>>>(a);
-  const hipError_t e = hipGetLastError();
+  hipError_t e;
+  if (l.rows > 64) {
+    tree_tile_kernel<FP8, D, F32><<<dim3(static_cast<uint32_t>((l.workgroups + 7) / 8 * 8)),
+                                    dim3(256), 0, st>>>(a);
+    e = hipGetLastError();
+  } else if (l.rows > 32) {
+    e = launch_stream<FP8, D, F32, 2, 4>(l, a, st);
+  } else {
+    e = l.waves == 8 ? launch_stream<FP8, D, F32, 1, 8>(l, a, st)
+                     : launch_stream<FP8, D, F32, 1, 4>(l, a, st);
+  }
   if (e != hipSuccess || l.splits == 1) return e;
   const int64_t waves = static_cast<int64_t>(a.B) * a.Hkv * a.row_tiles * l.rows;
   tree_combine_kernel<D, F32><<<dim3(static_cast<uint32_t>((waves + 3) / 4)), dim3(256), 0, st>>>(
-      a, l.rows, kTileKeys);
+      a, l.rows, l.keys);
   return hipGetLastError();
 }
 
