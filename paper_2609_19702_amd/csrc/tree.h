@@ -121,22 +121,26 @@ __device__ __forceinline__ TreeReq tree_request(const int32_t* base, const int32
   return r;
 }
 
-// The keys that nodes n0 .. n1 of a request can attend, as two lists.
+// A list of keys: entries 0 .. pre - 1 are rows 0 .. pre - 1 of an array, the ones
+// after them consecutive rows from pre + shift on, which pass the end of a ring
+// of rows (`wrap`: the row after its last) once at most.
+struct KeyList {
+  int n, pre, shift, wrap, ring;
+  __device__ __forceinline__ int row(int e) const {
+    const int x = e + shift;
+    return e < pre ? e : x >= wrap ? x - ring : x;
+  }
+};
+
+// The keys that nodes n0 .. n1 of a request can attend.
 //   cached: rows 0 .. pre - 1 of the cache (prompt and sinks), which every node
-//           attends, then the positions j0 .. j0 + (nold - pre) - 1
-//   new:    nodes 0 .. a0 - 1 (at prompt or sink positions), then a1 .. n1
+//           attends, then the positions from j0 on
+//   fresh:  nodes 0 .. pre - 1 (at prompt or sink positions), then the last
+//           fresh.n - fresh.pre up to n1
 // Positions that the window of the lowest node hides from all are left out.
 struct TreeKeys {
-  int pre, j0, nold;
-  int a0, a1, nnew;
-  int shift, wrap, ring;  // cache rows of the cached list's second part
-  __device__ __forceinline__ int node(int x) const { return x < a0 ? x : a1 + x - a0; }
-  // Cache row of entry r of the cached list.  The window fits in the ring, so it
-  // passes the ring's end once at most.
-  __device__ __forceinline__ int row(int r) const {
-    const int x = r + shift;
-    return r < pre ? r : x >= wrap ? x - ring : x;
-  }
+  KeyList cached, fresh;
+  int j0;
 };
 
 __device__ __forceinline__ TreeKeys tree_keys(const TreeArgs& a, const TreeReq& r, int n0, int n1) {
@@ -144,22 +148,21 @@ __device__ __forceinline__ TreeKeys tree_keys(const TreeArgs& a, const TreeReq& 
   const bool chain = a.depth == nullptr;
   const int low = r.base + (chain ? n0 : 0);  // lowest position of the nodes
   const int first = low - a.W + 1;            // lowest position of their windows
-  if (r.base < 0) {
-    k.pre = a.Lp + r.base;
-    k.j0 = 0;
-    k.nold = k.pre;
-  } else {
-    const int s = min(a.S, r.base);
-    k.pre = a.Lp + s;
-    k.j0 = min(max(s, first), r.base);
-    k.nold = k.pre + r.base - k.j0;
-  }
-  k.a1 = chain ? min(max(first - r.base, 0), n0) : 0;
-  k.a0 = min(max(a.S - r.base, 0), k.a1);
-  k.nnew = k.a0 + n1 + 1 - k.a1;
-  k.ring = a.ring;
-  k.wrap = a.ring ? a.Lp + a.S + a.ring : 0x7fffffff;
-  k.shift = a.Lp - k.pre + (a.ring && k.j0 >= a.S ? a.S + (k.j0 - a.S) % a.ring : k.j0);
+  const int s = r.base < 0 ? r.base : min(a.S, r.base);
+  k.j0 = r.base < 0 ? 0 : min(max(s, first), r.base);
+  k.cached.pre = a.Lp + s;
+  k.cached.n = k.cached.pre + (r.base < 0 ? 0 : r.base - k.j0);
+  // The window fits in the ring (check_kv).
+  k.cached.ring = a.ring;
+  k.cached.wrap = a.ring ? a.Lp + a.S + a.ring : 0x7fffffff;
+  k.cached.shift =
+      a.Lp - k.cached.pre + (a.ring && k.j0 >= a.S ? a.S + (k.j0 - a.S) % a.ring : k.j0);
+  const int a1 = chain ? min(max(first - r.base, 0), n0) : 0;
+  k.fresh.pre = min(max(a.S - r.base, 0), a1);
+  k.fresh.n = k.fresh.pre + n1 + 1 - a1;
+  k.fresh.shift = a1 - k.fresh.pre;
+  k.fresh.wrap = 0x7fffffff;
+  k.fresh.ring = 0;
   return k;
 }
 

@@ -61,21 +61,28 @@ dsa_status tree_derive(const dsa_params* p, const dsa_shape* s, int nodes, Deriv
 
 }  // namespace
 
+// Up to 64 query rows per (request, KV head) stream the keys for 32 rows at a
+// time (tree_stream_kernel); more go through LDS for 128 at a time
+// (tree_tile_kernel; 64 rows of d = 128 over fp8, 32 requests: 70 us a layer
+// streamed, 98 through it).  The keys of a row tile are split where the row tiles
+// alone would leave CUs without a workgroup, but not finer than four tiles of
+// keys per wave: a split costs a second kernel and a row of partial results.
 TreeLaunch tree_launch(const Derived& d, int nodes) {
   TreeLaunch l{};
   const int64_t rows = static_cast<int64_t>(nodes) * d.G;
   const int64_t pairs = static_cast<int64_t>(d.B) * d.Hkv;
   const bool stream = rows <= 64;
-  l.rows = stream ? (rows <= 32 ? 32 : 64) : 128;
+  l.rows = stream ? 32 : 128;
   l.keys = stream ? 32 : 64;
   l.row_tiles = static_cast<int>((rows + l.rows - 1) / l.rows);
-  l.waves = l.rows == 32 && pairs <= 256 ? 8 : 4;
   const int64_t keys = d.Lp + (d.mode == DSA_MODE_WINDOW ? std::min(d.Natt, d.Ldec) : d.Ldec) +
                        int64_t{nodes};
   const int64_t tiles = (keys + l.keys - 1) / l.keys + 2;
   const int64_t wgs = pairs * l.row_tiles;
-  const int least = stream ? 4 * l.waves : 4;
-  const int64_t want = std::min<int64_t>((512 + wgs - 1) / wgs, 64);
+  // Twice the waves on the keys where at most one workgroup per CU has work.
+  l.waves = stream && wgs <= 256 ? 8 : 4;
+  const int64_t want = std::max<int64_t>(1, 256 / wgs);
+  const int64_t least = 4 * (stream ? l.waves : 1);
   l.split_tiles = static_cast<int>(std::max<int64_t>(least, (tiles + want - 1) / want));
   l.splits = static_cast<int>((tiles + l.split_tiles - 1) / l.split_tiles);
   l.workgroups = wgs * l.splits;

@@ -14,6 +14,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kTreeMin = -3.0e38f;  // "no score yet": finite, below every finite score in use
+constexpr float kTreeSlack = 8.f;
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {  // nearest even
   const f32x2 x = {a, b};
@@ -34,6 +35,11 @@ __device__ __forceinline__ uint32_t nonfinite_bit(const uint4& x) {
   for (int i = 0; i < 4; ++i)
     carry |= ((w[i] & 0x7f80u) + 0x80u) | (((w[i] >> 16) & 0x7f80u) + 0x80u);
   return carry;
+}
+
+// K/V rows that other workgroups read too: without the hint of load_stream16.
+__device__ __forceinline__ uint4 load16(const uint8_t* p) {
+  return *reinterpret_cast<const uint4*>(p);
 }
 
 // Sixteen E4M3 values as bf16 (exact: 4 significant bits, exponents -9 .. 8).
@@ -85,61 +91,64 @@ __device__ __forceinline__ void store4(void* out, int64_t at, float a, float b, 
         make_uint2(pack_bf16(a, b), pack_bf16(c, d));
 }
 
-// What a wave needs of one query row (node, query head): its lane's row.
+// What a lane needs of its query row (node, query head).
 struct TreeRow {
   int node, dep;  // the node and its depth (a chain: the same)
   int thr;        // cached entries past the prefix are seen above this one
-  int64_t out;    // element offset of the output row
 };
 
 __device__ __forceinline__ TreeRow tree_row(const TreeArgs& a, const TreeReq& rq,
-                                            const TreeKeys& ks, int b, int h, int row) {
+                                            const TreeKeys& ks, int b, int row) {
   TreeRow r;
   r.node = row / a.G;
-  const int head = h * a.G + row % a.G;
   r.dep = a.depth ? a.depth[static_cast<int64_t>(b) * a.N + r.node] : r.node;
-  r.thr = ks.pre + rq.base + r.dep - a.W - ks.j0;
-  r.out = (static_cast<int64_t>(b) * a.N + r.node) * a.Hq + head;
+  r.thr = ks.cached.pre + rq.base + r.dep - a.W - ks.j0;
   return r;
 }
 
+// What is the same for all rows of a row tile.
+struct TreeTile {
+  int n0, n1, deepest, sink;  // nodes, largest depth; smaller depths stand at sink positions
+};
+
 // Which of 32 cached entries from e on the row sees.
 __device__ __forceinline__ uint32_t see_cached(const TreeKeys& ks, const TreeRow& r, int e) {
-  return low_bits(ks.nold - e) & (low_bits(ks.pre - e) | ~low_bits(r.thr + 1 - e));
+  return low_bits(ks.cached.n - e) & (low_bits(ks.cached.pre - e) | ~low_bits(r.thr + 1 - e));
 }
 
-// Which of 32 new entries from e on the row sees.  sink: nodes of smaller depth
-// stand at sink positions; deep: some node is a window or more deep.
-__device__ __forceinline__ uint32_t see_new(const TreeArgs& a, const TreeKeys& ks, const TreeRow& r,
-                                            int b, int e, int sink, bool deep) {
-  uint32_t see = low_bits(ks.nnew - e);
-  if (!a.depth) {  // nodes from a1 on follow the first a0, which every node sees
-    const int f = ks.a0 - ks.a1 - e;
+// Which of 32 new entries from e on the row sees.
+__device__ __forceinline__ uint32_t see_fresh(const TreeArgs& a, const TreeKeys& ks,
+                                              const TreeTile& tt, const TreeRow& r, int b, int e) {
+  const KeyList& k = ks.fresh;
+  uint32_t see = low_bits(k.n - e);
+  if (!a.depth) {  // entries from k.pre on are nodes in order; every node sees those before
+    const int f = -k.shift - e;
     return see & low_bits(r.node + 1 + f) &
-           (low_bits(ks.a0 - e) | low_bits(sink + f) | ~low_bits(r.node - a.W + 1 + f));
+           (low_bits(k.pre - e) | low_bits(tt.sink + f) | ~low_bits(r.node - a.W + 1 + f));
   }
   const int64_t at = static_cast<int64_t>(b) * a.N;
   see &= e / 32 < a.words ? a.anc[(at + r.node) * a.words + e / 32] : 0u;
-  if (deep)
+  if (tt.deepest >= a.W)  // some node has ancestors out of its window
     for (uint32_t m = see; m; m &= m - 1) {
       const int i = __builtin_ctz(m), de = a.depth[at + e + i];
-      if (de >= sink && r.dep - de >= a.W) see &= ~(1u << i);
+      if (de >= tt.sink && r.dep - de >= a.W) see &= ~(1u << i);
     }
   return see;
 }
 
-// Whether some row of nodes n0 .. n1 (the deepest at depth `deepest`) must not
-// see some of the `keys` cached (new) entries from e on.
+// Whether some row of the tile must not see some of the `keys` entries from e on.
 __device__ __forceinline__ bool hides_cached(const TreeArgs& a, const TreeReq& rq,
-                                             const TreeKeys& ks, int e, int keys, int deepest) {
-  const int thr = ks.pre + rq.base + deepest - a.W - ks.j0;
-  return e + keys > ks.nold || (e + keys > ks.pre && max(e, ks.pre) <= thr);
+                                             const TreeKeys& ks, const TreeTile& tt, int e,
+                                             int keys) {
+  const KeyList& k = ks.cached;
+  const int thr = k.pre + rq.base + tt.deepest - a.W - ks.j0;
+  return e + keys > k.n || (e + keys > k.pre && max(e, k.pre) <= thr);
 }
-__device__ __forceinline__ bool hides_new(const TreeArgs& a, const TreeKeys& ks, int e, int keys,
-                                          int n0, int n1) {
-  return a.depth || !(e + keys <= ks.a0 ||
-                      (e >= ks.a0 && e + keys <= ks.nnew && ks.node(e + keys - 1) <= n0 &&
-                       ks.node(e) > n1 - a.W));
+__device__ __forceinline__ bool hides_fresh(const TreeArgs& a, const TreeKeys& ks,
+                                            const TreeTile& tt, int e, int keys) {
+  const KeyList& k = ks.fresh;
+  return a.depth || !(e + keys <= k.pre || (e >= k.pre && e + keys <= k.n &&
+                                            k.row(e + keys - 1) <= tt.n0 && k.row(e) > tt.n1 - a.W));
 }
 
 // Elements of a K or V row in LDS.  Padded so that neither the K operand's
@@ -193,122 +202,153 @@ struct TreeWave {
                        lv + r * kVRow<D> + 32 * c + 16 * ((lane >> 4) & 1) + 4 * (s16 & 3))));
   }
 
-  // A tile of 32 KB keys.  sl: score scale (positive), flip: of negated scores;
-  // vs: scale of V; see: the keys each row sees, used where `hides`.
-  template <int KB>
-  __device__ __forceinline__ void tile(int lane, const uint16_t* lk, const uint16_t* lv, float sl,
-                                       bool flip, float vs, bool hides,
-                                       const uint32_t (&see)[NB][KB]) {
+  // S^T of 32 keys: lane (lq, hh) gets row lq's scores of keys 8 (i / 4) + 4 hh +
+  // i % 4, negated where `flip`, -inf where `hides` and the row does not see them.
+  __device__ __forceinline__ void scores(int lane, const uint16_t* lk, bool flip, bool hides,
+                                         const uint32_t (&see)[NB], f32x16 (&sc)[NB]) {
     const int lq = lane & 31, hh = lane >> 5;
-    f32x16 sc[NB][KB];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[nb][i] = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lk + lq * kKRow<D> + 16 * s + 8 * hh);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[nb][kb][i] = 0.f;
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s) {
-        const bf16x8 kf =
-            *reinterpret_cast<const bf16x8*>(lk + (32 * kb + lq) * kKRow<D> + 16 * s + 8 * hh);
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-          sc[nb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[nb][s], sc[nb][kb], 0, 0, 0);
-      }
+        sc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[nb][s], sc[nb], 0, 0, 0);
     }
-    // Lane (lq, hh) holds row lq's scores of keys 32 kb + 8 (i / 4) + 4 hh + i % 4.
     if (flip) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) sc[nb][kb][i] = -sc[nb][kb][i];
+        for (int i = 0; i < 16; ++i) sc[nb][i] = -sc[nb][i];
     }
     if (hides) {
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+      for (int nb = 0; nb < NB; ++nb) {
+        const uint32_t w = see[nb] >> (4 * hh);
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-          const uint32_t w = see[nb][kb] >> (4 * hh);
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            sc[nb][kb][i] =
-                w & (1u << (8 * (i / 4) + i % 4)) ? sc[nb][kb][i] : -__builtin_inff();
-        }
+        for (int i = 0; i < 16; ++i)
+          sc[nb][i] = w & (1u << (8 * (i / 4) + i % 4)) ? sc[nb][i] : -__builtin_inff();
+      }
     }
+  }
+
+  // The running maximum takes the scores in.  Weights stay relative to the maximum
+  // of an earlier tile as long as none passes 2^kTreeSlack: every sum keeps its
+  // relative precision, and the rescale (a multiply per output, and per
+  // weight in `held`, not yet in the outputs) leaves most tiles.
+  template <bool HELD>
+  __device__ __forceinline__ void raise(float sl, const f32x16 (&sc)[NB], f32x16 (&held)[NB]) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      float mx = sc[nb][0][0];
+      float mx = sc[nb][0];
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[nb][kb][i]);
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[nb][i]);
       float x1, x2;
       xor_pair<32>(mx, x1, x2);
       const float mnew = fmaxf(m[nb], fmaxf(x1, x2) * sl);
-      if (__ballot(mnew > m[nb])) {
+      if (__ballot(mnew > m[nb] + kTreeSlack)) {
         const float alpha = fast_exp2(m[nb] - mnew);
         l[nb] *= alpha;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[nb][c][i] *= alpha;
+        if constexpr (HELD) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) held[nb][i] *= alpha;
+        }
         m[nb] = mnew;
       }
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          sc[nb][kb][i] = fast_exp2(fmaf(sc[nb][kb][i], sl, -m[nb]));
-          l[nb] += sc[nb][kb][i];
-          if (vs != 1.f) sc[nb][kb][i] *= vs;
-        }
     }
-    // P.V, 16 keys a step.  Half hh's eight operand slots are the keys 4 hh ..
-    // + 3 and 8 + 4 hh .. + 3 of the step, and V is read in that order.  For
-    // fp32 outputs the weights go in as three bf16 terms, which hold all their
-    // 24 bits; for bf16 outputs rounded to one, off by half a step as the
-    // outputs are.
+  }
+
+  // Scores to weights, in place.
+  __device__ __forceinline__ void weights(float sl, float vs, f32x16 (&sc)[NB]) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        constexpr int NE = F32 ? 3 : 1;
-        bf16x8 pf[NB][NE];
+      for (int i = 0; i < 16; ++i) {
+        sc[nb][i] = fast_exp2(fmaf(sc[nb][i], sl, -m[nb]));
+        l[nb] += sc[nb][i];
+        if (vs != 1.f) sc[nb][i] *= vs;
+      }
+  }
+
+  // O += P V of 32 keys, 16 a step.  Half hh's eight operand slots are the keys
+  // 4 hh .. + 3 and 8 + 4 hh .. + 3 of the step, and V is read in that order.
+  // For fp32 outputs the weights go in as three bf16 terms, which hold all their
+  // 24 bits; for bf16 outputs rounded to one, off by half a step as the outputs
+  // are.
+  __device__ __forceinline__ void values(int lane, const uint16_t* lv, const f32x16 (&p)[NB]) {
+    constexpr int NE = F32 ? 3 : 1;
+    const int hh = lane >> 5;
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          uint32_t w[NE][4];
+    for (int s = 0; s < 2; ++s) {
+      bf16x8 pf[NB][NE];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float u = sc[nb][kb][8 * s + 2 * j], v = sc[nb][kb][8 * s + 2 * j + 1];
-            if constexpr (F32) {
+      for (int nb = 0; nb < NB; ++nb) {
+        uint32_t w[NE][4];
 #pragma unroll
-              for (int e = 0; e < NE; ++e) {
-                w[e][j] = high_halves(u, v);
-                u -= __uint_as_float(__float_as_uint(u) & 0xffff0000u);
-                v -= __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-              }
-            } else {
-              w[0][j] = pack_bf16(u, v);
+        for (int j = 0; j < 4; ++j) {
+          float u = p[nb][8 * s + 2 * j], v = p[nb][8 * s + 2 * j + 1];
+          if constexpr (F32) {
+#pragma unroll
+            for (int e = 0; e < NE; ++e) {
+              w[e][j] = high_halves(u, v);
+              u -= __uint_as_float(__float_as_uint(u) & 0xffff0000u);
+              v -= __uint_as_float(__float_as_uint(v) & 0xffff0000u);
             }
+          } else {
+            w[0][j] = pack_bf16(u, v);
           }
+        }
+#pragma unroll
+        for (int e = 0; e < NE; ++e)
+          pf[nb][e] = __builtin_bit_cast(bf16x8, make_uint4(w[e][0], w[e][1], w[e][2], w[e][3]));
+      }
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        const uint2 va = vread(lv, lane, 16 * s + 4 * hh, c);
+        const uint2 vb = vread(lv, lane, 16 * s + 8 + 4 * hh, c);
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(va.x, va.y, vb.x, vb.y));
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int e = 0; e < NE; ++e)
-            pf[nb][e] = __builtin_bit_cast(bf16x8, make_uint4(w[e][0], w[e][1], w[e][2], w[e][3]));
-        }
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          const uint2 va = vread(lv, lane, 32 * kb + 16 * s + 4 * hh, c);
-          const uint2 vb = vread(lv, lane, 32 * kb + 16 * s + 8 + 4 * hh, c);
-          const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(va.x, va.y, vb.x, vb.y));
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int e = 0; e < NE; ++e)
-              o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[nb][e], o[nb][c], 0, 0, 0);
-        }
+            o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[nb][e], o[nb][c], 0, 0, 0);
       }
+    }
+  }
+
+  // A tile of 32 keys.  sl: score scale (positive), flip: of negated scores; vs:
+  // scale of V; see: the keys each row sees, used where `hides`.
+  __device__ __forceinline__ void tile(int lane, const uint16_t* lk, const uint16_t* lv, float sl,
+                                       bool flip, float vs, bool hides,
+                                       const uint32_t (&see)[NB]) {
+    f32x16 sc[NB];
+    scores(lane, lk, flip, hides, see, sc);
+    raise<false>(sl, sc, sc);
+    weights(sl, vs, sc);
+    values(lane, lv, sc);
+  }
+
+  // 64 keys: the second half's scores are under way while the first's weights
+  // are computed, and the first half's values while the second's are.
+  __device__ __forceinline__ void tile2(int lane, const uint16_t* lk, const uint16_t* lv, float sl,
+                                        bool flip, float vs, bool hides,
+                                        const uint32_t (&see)[2][NB]) {
+    f32x16 s0[NB], s1[NB];
+    scores(lane, lk, flip, hides, see[0], s0);
+    raise<false>(sl, s0, s0);
+    scores(lane, lk + 32 * kKRow<D>, flip, hides, see[1], s1);
+    weights(sl, vs, s0);
+    raise<true>(sl, s1, s0);
+    values(lane, lv, s0);
+    weights(sl, vs, s1);
+    values(lane, lv + 32 * kVRow<D>, s1);
   }
 
   // Adds the infinities and NaN of V row v to the rows that see its key: as
@@ -355,23 +395,26 @@ __device__ __forceinline__ CacheScale cache_scale(const TreeArgs& a, int pair) {
 
 // In a tile with hidden keys a V row's infinity or NaN would reach queries that
 // must not see it, as 0 times it.  Such elements become 0 in LDS, and
-// add_nonfinite adds them where they are seen.  Each lane takes the N chunks of 16
-// bytes it has just stored, chunk i at `v` + i * step, D / 8 lanes to a row;
-// returns the rows that had any: bit i * (512 / D) + g for row g of pass i.  (A
-// loop over LDS: the same on the registers before they are stored costs 20 more.)
-template <int D>
-__device__ __forceinline__ uint32_t clean_rows(uint16_t* v, int n, int step) {
+// add_nonfinite adds them where they are seen.  x: the N chunks of 16 bytes that
+// each lane has just stored, chunk i at `v` + i * step, D / 8 lanes to a row;
+// returns the rows that had any: bit i * (512 / D) + g for row g of pass i.  (The
+// rare second pass goes over LDS: on the registers it cost 20 of them.)
+template <int D, int N>
+__device__ __forceinline__ uint32_t clean_rows(const uint4 (&x)[N], uint16_t* v, int step) {
   constexpr int CPR = D / 8, RPW = 64 / CPR;
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) any |= nonfinite_bit(x[i]);
+  if (!__ballot((any & 0x8000u) != 0)) return 0;
   uint32_t rows = 0;
 #pragma unroll 1
-  for (int i = 0; i < n; ++i, v += step) {
-    const uint4 x = *reinterpret_cast<const uint4*>(v);
-    const bool mine = (nonfinite_bit(x) & 0x8000u) != 0;
+  for (int i = 0; i < N; ++i, v += step) {
+    const uint4 y = *reinterpret_cast<const uint4*>(v);
+    const bool mine = (nonfinite_bit(y) & 0x8000u) != 0;
     const uint64_t who = __ballot(mine);
-    if (!who) continue;
     if (mine)
       *reinterpret_cast<uint4*>(v) =
-          make_uint4(finite_pair(x.x), finite_pair(x.y), finite_pair(x.z), finite_pair(x.w));
+          make_uint4(finite_pair(y.x), finite_pair(y.y), finite_pair(y.z), finite_pair(y.w));
 #pragma unroll
     for (int g = 0; g < RPW; ++g)
       rows |= (who >> (g * CPR) & ((1ull << CPR) - 1)) ? 1u << (i * RPW + g) : 0u;
@@ -402,14 +445,14 @@ __device__ __forceinline__ int tree_cut(int tiles, int part, int parts) {
 
 // ---- many query rows -----------------------------------------------------------
 
-constexpr int kTileRows = 128;  // query rows of a workgroup: four waves of 32
 constexpr int kTileKeys = 64;   // keys of a tile
 
-// A workgroup of four waves takes 128 query rows (node, query head of the KV
+// A workgroup of four waves takes 128 NB query rows (node, query head of the KV
 // head's group) of one request and KV head, and a share of the keys.  Tiles of
 // 64 keys go through LDS for all four waves, two buffers in turn.
-template <bool FP8, int D, bool F32>
-__global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
+template <bool FP8, int D, bool F32, int NB>
+__global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(TreeArgs a) {
+  constexpr int kTileRows = 128 * NB;
   constexpr int CPR = D / 8;           // 16-byte chunks of a bf16 row
   constexpr int NP = CPR * kTileKeys / 256;
   constexpr int RPP = 256 / CPR;       // rows per pass of the workgroup
@@ -423,171 +466,182 @@ __global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
   if (item < 0) return;
   const int pair = item / per_pair, sub = item % per_pair;
   const int b = pair / a.Hkv, h = pair % a.Hkv;
-  const int qt = sub / a.splits, sp = sub % a.splits;
+  const int qt = a.row_tiles - 1 - sub / a.splits, sp = sub % a.splits;  // longest first
   const TreeReq rq = tree_request(a.base, a.count, b, a.N, a.Lp, a.Ldec);
   const int rows = rq.n * a.G, r0 = qt * kTileRows;
   if (r0 >= rows) return;
-  const int n0 = r0 / a.G, n1 = (min(r0 + kTileRows, rows) - 1) / a.G;
-  const TreeKeys ks = tree_keys(a, rq, n0, n1);
-  const int t_old = (ks.nold + kTileKeys - 1) / kTileKeys;
-  const int tiles = t_old + (ks.nnew + kTileKeys - 1) / kTileKeys;
+  TreeTile tt{r0 / a.G, (min(r0 + kTileRows, rows) - 1) / a.G, 0, a.S - rq.base};
+  tt.deepest = a.depth ? a.max_depth[b] : tt.n1;
+  const TreeKeys ks = tree_keys(a, rq, tt.n0, tt.n1);
+  const int t_old = (ks.cached.n + kTileKeys - 1) / kTileKeys;
+  const int tiles = t_old + (ks.fresh.n + kTileKeys - 1) / kTileKeys;
   const int nsp = tree_splits(a, tiles);
   if (sp >= nsp) return;
   const int t0 = tree_cut(tiles, sp, nsp), t1 = tree_cut(tiles, sp + 1, nsp);
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int row = r0 + 32 * wave + (lane & 31);
-  const bool wave_on = r0 + 32 * wave < rows;
-  const TreeRow my = tree_row(a, rq, ks, b, h, min(row, rows - 1));
-  const int deepest = a.depth ? a.max_depth[b] : n1;
-  const int sink = a.S - rq.base;
+  const int row0 = r0 + 32 * NB * wave + (lane & 31);
+  const bool wave_on = r0 + 32 * NB * wave < rows;
   const CacheScale cs = cache_scale<FP8>(a, pair);
-  TreeWave<D, F32, 1> w;
-  w.start(a, lane, 0,
-          a.q + b * a.qsb + my.node * a.qsn + (h * a.G + min(row, rows - 1) % a.G) * a.qsh);
+  TreeRow my[NB];
+  TreeWave<D, F32, NB> w;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int row = min(row0 + 32 * nb, rows - 1);
+    my[nb] = tree_row(a, rq, ks, b, row);
+    w.start(a, lane, nb,
+            a.q + b * a.qsb + my[nb].node * a.qsn + (h * a.G + row % a.G) * a.qsh);
+  }
 
-  const int64_t cbase = tree_cache_base(a, b, h, FP8 ? 1 : 2);
-  const uint16_t* kn = a.kn + b * a.nsb + h * a.nsh;
-  const uint16_t* vn = a.vn + b * a.nsb + h * a.nsh;
+  const uint8_t* kc = a.k + tree_cache_base(a, b, h, FP8 ? 1 : 2);
+  const uint8_t* vc = a.v + tree_cache_base(a, b, h, FP8 ? 1 : 2);
+  const uint8_t* kn = reinterpret_cast<const uint8_t*>(a.kn + b * a.nsb + h * a.nsh);
+  const uint8_t* vn = reinterpret_cast<const uint8_t*>(a.vn + b * a.nsb + h * a.nsh);
   uint4 rk[NP], rv[NP];
 
-  // A tile of bf16 rows (new ones, or the cache's) into LDS.
-  auto put = [&](int buf, bool hides) {
+  // Tile t, of bf16 rows: of the new tokens, or of a bf16 cache.
+  auto load = [&](int t) {
+    const bool old = !FP8 && t < t_old;
+    const KeyList& list = old ? ks.cached : ks.fresh;
+    const uint8_t* k = old ? kc : kn;
+    const uint8_t* v = old ? vc : vn;
+    const int64_t step = old ? a.sr : a.nsn * 2;
+    const int e0 = (t - (t < t_old ? 0 : t_old)) * kTileKeys + tid / CPR;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int64_t at = list.row(min(e0 + i * RPP, list.n - 1)) * step + (tid % CPR) * 16;
+      rk[i] = load16(k + at);
+      rv[i] = load16(v + at);
+    }
+  };
+  auto hides = [&](int t) {
+    return t < t_old ? hides_cached(a, rq, ks, tt, t * kTileKeys, kTileKeys)
+                     : hides_fresh(a, ks, tt, (t - t_old) * kTileKeys, kTileKeys);
+  };
+  auto put = [&](int t, int buf) {
     const int c = tid % CPR;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int r = i * RPP + tid / CPR;
-      *reinterpret_cast<uint4*>(lk[buf] + r * kKRow<D> + (c) * 8) = rk[i];
-      *reinterpret_cast<uint4*>(lv[buf] + r * kVRow<D> + (c) * 8) = rv[i];
+      *reinterpret_cast<uint4*>(lk[buf] + r * kKRow<D> + c * 8) = rk[i];
+      *reinterpret_cast<uint4*>(lv[buf] + r * kVRow<D> + c * 8) = rv[i];
     }
     uint32_t bad = 0;
-    if (hides) bad = clean_rows<D>(lv[buf] + (tid / CPR) * kVRow<D> + c * 8, NP, RPP * kVRow<D>);
+    if (hides(t))
+      bad = clean_rows<D>(rv, lv[buf] + (tid / CPR) * kVRow<D> + c * 8, RPP * kVRow<D>);
     if (lane == 0) lbad[buf][wave] = bad;
   };
-  auto add_hidden = [&](int buf, const uint32_t (&see)[1][2], auto&& row_of) {
+  // The same of an fp8 cache: sixteen elements a load.
+  auto load8 = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < NP8; ++i) {
+      const int e = min(t * kTileKeys + i * RP8 + tid / CP8, ks.cached.n - 1);
+      const int64_t at = ks.cached.row(e) * a.sr + (tid % CP8) * 16;
+      rk[i] = load16(kc + at);
+      rv[i] = load16(vc + at);
+    }
+  };
+  auto put8 = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < NP8; ++i) {
+      const int r = i * RP8 + tid / CP8, c = 2 * (tid % CP8);
+      uint4 lo, hi;
+      widen_fp8(rk[i], lo, hi);
+      *reinterpret_cast<uint4*>(lk[buf] + r * kKRow<D> + c * 8) = lo;
+      *reinterpret_cast<uint4*>(lk[buf] + r * kKRow<D> + c * 8 + 8) = hi;
+      widen_fp8(rv[i], lo, hi);
+      *reinterpret_cast<uint4*>(lv[buf] + r * kVRow<D> + c * 8) = lo;
+      *reinterpret_cast<uint4*>(lv[buf] + r * kVRow<D> + c * 8 + 8) = hi;
+    }
+  };
+  auto see_of = [&](int t, uint32_t (&see)[2][NB]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+        see[i][nb] = t < t_old
+                         ? see_cached(ks, my[nb], t * kTileKeys + 32 * i)
+                         : see_fresh(a, ks, tt, my[nb], b, (t - t_old) * kTileKeys + 32 * i);
+  };
+  auto add_hidden = [&](int t, int buf, const uint32_t (&see)[2][NB]) {
     constexpr int RPW = 64 / CPR;  // rows of a wave's pass
+    const bool old = t < t_old;
 #pragma unroll 1
     for (int i = 0; i < 4; ++i)
 #pragma unroll 1
       for (uint32_t bad = lbad[buf][i]; bad; bad &= bad - 1) {
         const int at = __builtin_ctz(bad), e = at / RPW * RPP + i * RPW + at % RPW;
-        const bool mine[1] = {static_cast<bool>((see[0][e >> 5] >> (e & 31)) & 1u)};
-        w.add_nonfinite(lane, row_of(e), mine);
+        bool mine[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) mine[nb] = (see[e >> 5][nb] >> (e & 31)) & 1u;
+        const uint8_t* v = old ? vc + ks.cached.row(t * kTileKeys + e) * a.sr
+                               : vn + ks.fresh.row((t - t_old) * kTileKeys + e) * a.nsn * 2;
+        w.add_nonfinite(lane, reinterpret_cast<const uint16_t*>(v), mine);
       }
   };
 
-  // The cache's tiles.
-  auto load_old = [&](int t) {
-    constexpr int N = FP8 ? NP8 : NP, R = FP8 ? RP8 : RPP, C = FP8 ? CP8 : CPR;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int r = min(t * kTileKeys + i * R + tid / C, ks.nold - 1);
-      const int64_t at = cbase + ks.row(r) * a.sr + (tid % C) * 16;
-      rk[i] = load_stream16(a.k + at);
-      rv[i] = load_stream16(a.v + at);
-    }
-  };
-  auto hides_old = [&](int t) {
-    return hides_cached(a, rq, ks, t * kTileKeys, kTileKeys, deepest);
-  };
-  auto put_old = [&](int t, int buf) {
-    if constexpr (FP8) {
-#pragma unroll
-      for (int i = 0; i < NP8; ++i) {
-        const int r = i * RP8 + tid / CP8, c = 2 * (tid % CP8);
-        uint4 lo, hi;
-        widen_fp8(rk[i], lo, hi);
-        *reinterpret_cast<uint4*>(lk[buf] + r * kKRow<D> + (c) * 8) = lo;
-        *reinterpret_cast<uint4*>(lk[buf] + r * kKRow<D> + (c + 1) * 8) = hi;
-        widen_fp8(rv[i], lo, hi);
-        *reinterpret_cast<uint4*>(lv[buf] + r * kVRow<D> + (c) * 8) = lo;
-        *reinterpret_cast<uint4*>(lv[buf] + r * kVRow<D> + (c + 1) * 8) = hi;
-      }
-    } else {
-      put(buf, hides_old(t));
-    }
-  };
   int t = t0, buf = 0;
-  const int e_old = min(t1, t_old);
-  if (t < e_old) {
-    load_old(t);
-    put_old(t, 0);
-    __syncthreads();
-    for (; t < e_old; ++t, buf ^= 1) {
-      if (t + 1 < e_old) load_old(t + 1);
+  if constexpr (FP8) {
+    const int end = min(t1, t_old);
+    if (t < end) {
+      load8(t);
+      put8(0);
+      __syncthreads();
+    }
+    for (; t < end; ++t, buf ^= 1) {
+      if (t + 1 < end) load8(t + 1);
       if (wave_on) {
-        const bool hides = hides_old(t);
-        uint32_t see[1][2] = {};
-        if (hides) {
-          see[0][0] = see_cached(ks, my, t * kTileKeys);
-          see[0][1] = see_cached(ks, my, t * kTileKeys + 32);
-        }
-        w.template tile<2>(lane, lk[buf], lv[buf], cs.sl, FP8 && cs.flip, FP8 ? cs.vs : 1.f, hides,
-                           see);
-        if (!FP8 && hides)
-          add_hidden(buf, see, [&](int e) {
-            return reinterpret_cast<const uint16_t*>(a.v + cbase + ks.row(t * kTileKeys + e) * a.sr);
-          });
+        uint32_t see[2][NB] = {};
+        const bool hide = hides(t);
+        if (hide) see_of(t, see);
+        w.tile2(lane, lk[buf], lv[buf], cs.sl, cs.flip, cs.vs, hide, see);
       }
-      if (t + 1 < e_old) put_old(t + 1, buf ^ 1);
+      if (t + 1 < end) put8(buf ^ 1);
       __syncthreads();
     }
   }
-
-  // The new tokens' tiles.
-  auto load_new = [&](int x0) {
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int x = min(x0 + i * RPP + tid / CPR, ks.nnew - 1);
-      const int64_t at = ks.node(x) * a.nsn + (tid % CPR) * 8;
-      rk[i] = *reinterpret_cast<const uint4*>(kn + at);
-      rv[i] = *reinterpret_cast<const uint4*>(vn + at);
-    }
-  };
-  auto hides_at = [&](int x) { return hides_new(a, ks, x, kTileKeys, n0, n1); };
   if (t < t1) {
-    const int end = (t1 - t_old) * kTileKeys;
-    int x = (t - t_old) * kTileKeys;
-    load_new(x);
-    put(buf, hides_at(x));
+    load(t);
+    put(t, buf);
     __syncthreads();
-    for (; x < end; x += kTileKeys, buf ^= 1) {
-      if (x + kTileKeys < end) load_new(x + kTileKeys);
-      if (wave_on) {
-        const bool hides = hides_at(x);
-        uint32_t see[1][2] = {};
-        if (hides) {
-          see[0][0] = see_new(a, ks, my, b, x, sink, deepest >= a.W);
-          see[0][1] = see_new(a, ks, my, b, x + 32, sink, deepest >= a.W);
-        }
-        w.template tile<2>(lane, lk[buf], lv[buf], a.scale_log2, false, 1.f, hides, see);
-        if (hides)
-          add_hidden(buf, see, [&](int e) { return vn + ks.node(x + e) * a.nsn; });
-      }
-      if (x + kTileKeys < end) put(buf ^ 1, hides_at(x + kTileKeys));
-      __syncthreads();
+  }
+  for (; t < t1; ++t, buf ^= 1) {
+    if (t + 1 < t1) load(t + 1);
+    if (wave_on) {
+      uint32_t see[2][NB] = {};
+      const bool hide = hides(t);
+      if (hide) see_of(t, see);
+      w.tile2(lane, lk[buf], lv[buf], a.scale_log2, false, 1.f, hide, see);
+      if (hide) add_hidden(t, buf, see);
     }
+    if (t + 1 < t1) put(t + 1, buf ^ 1);
+    __syncthreads();
   }
 
-  float l1, l2;
-  xor_pair<32>(w.l[0], l1, l2);
-  const float l = l1 + l2;
-  if (row >= rows) return;
-  if (nsp == 1) {
-    tree_write<D, F32>(a, lane, w.o[0], 1.f / l, my.out);
-    return;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int row = row0 + 32 * nb;
+    float l1, l2;
+    xor_pair<32>(w.l[nb], l1, l2);
+    const float l = l1 + l2;
+    if (row >= rows) continue;
+    if (nsp == 1) {
+      tree_write<D, F32>(a, lane, w.o[nb], 1.f / l,
+                         (static_cast<int64_t>(b) * a.N + my[nb].node) * a.Hq + h * a.G + row % a.G);
+      continue;
+    }
+    float* part = a.part + ((static_cast<int64_t>(pair) * a.row_tiles + qt) * a.splits + sp) *
+                               kTileRows * kPartRow<D> +
+                  (row - r0) * kPartRow<D>;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<float4*>(part + 32 * c + 2 * i + 4 * (lane >> 5)) = make_float4(
+            w.o[nb][c][i], w.o[nb][c][i + 1], w.o[nb][c][i + 2], w.o[nb][c][i + 3]);
+    if (lane < 32) *reinterpret_cast<float2*>(part + D) = make_float2(w.m[nb], l);
   }
-  float* part = a.part + ((static_cast<int64_t>(pair) * a.row_tiles + qt) * a.splits + sp) *
-                             kTileRows * kPartRow<D> +
-                (row - r0) * kPartRow<D>;
-#pragma unroll
-  for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4)
-      *reinterpret_cast<float4*>(part + 32 * c + 2 * i + 4 * (lane >> 5)) =
-          make_float4(w.o[0][c][i], w.o[0][c][i + 1], w.o[0][c][i + 2], w.o[0][c][i + 3]);
-  if (lane < 32) *reinterpret_cast<float2*>(part + D) = make_float2(w.m[0], l);
 }
 
 // ---- few query rows --------------------------------------------------------------
@@ -610,17 +664,20 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
   __shared__ __align__(16) uint16_t lds[NW * (kStreamLds<D> / 2)];
   __shared__ float lm[NW][32], ll[NW][32];
 
-  const int item = xcd_item(a.B * a.Hkv * a.splits);
+  // Row tiles of the same keys are next to each other.
+  const int per_pair = a.splits * a.row_tiles;
+  const int item = xcd_item(a.B * a.Hkv * per_pair);
   if (item < 0) return;
-  const int pair = item / a.splits, sp = item % a.splits;
+  const int pair = item / per_pair, sp = item % per_pair / a.row_tiles, qt = item % a.row_tiles;
   const int b = pair / a.Hkv, h = pair % a.Hkv;
   const TreeReq rq = tree_request(a.base, a.count, b, a.N, a.Lp, a.Ldec);
-  const int rows = rq.n * a.G;
-  if (rows == 0) return;
-  const int n1 = rq.n - 1;
-  const TreeKeys ks = tree_keys(a, rq, 0, n1);
-  const int t_old = (ks.nold + kStreamKeys - 1) / kStreamKeys;
-  const int tiles = t_old + (ks.nnew + kStreamKeys - 1) / kStreamKeys;
+  const int rows = rq.n * a.G, r0 = qt * 32 * NB;
+  if (r0 >= rows) return;
+  TreeTile tt{r0 / a.G, (min(r0 + 32 * NB, rows) - 1) / a.G, 0, a.S - rq.base};
+  tt.deepest = a.depth ? a.max_depth[b] : tt.n1;
+  const TreeKeys ks = tree_keys(a, rq, tt.n0, tt.n1);
+  const int t_old = (ks.cached.n + kStreamKeys - 1) / kStreamKeys;
+  const int tiles = t_old + (ks.fresh.n + kStreamKeys - 1) / kStreamKeys;
   const int nsp = tree_splits(a, tiles);
   if (sp >= nsp) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -629,120 +686,146 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
 
   uint16_t* lk = lds + wave * (kStreamLds<D> / 2);
   uint16_t* lv = lk + kStreamKeys * kKRow<D>;
-  const int64_t cbase = tree_cache_base(a, b, h, FP8 ? 1 : 2);
-  uint4 rk[PF][N], rv[PF][N];
-  auto load_old = [&](int t, uint4 (&k)[N], uint4 (&v)[N]) {
+  const uint8_t* kc = a.k + tree_cache_base(a, b, h, FP8 ? 1 : 2);
+  const uint8_t* vc = a.v + tree_cache_base(a, b, h, FP8 ? 1 : 2);
+  const uint8_t* kn = reinterpret_cast<const uint8_t*>(a.kn + b * a.nsb + h * a.nsh);
+  const uint8_t* vn = reinterpret_cast<const uint8_t*>(a.vn + b * a.nsb + h * a.nsh);
+  uint4 rk[PF * N], rv[PF * N];
+  static_assert(PF * N >= NP, "the registers of the cache's tiles hold a tile of new rows");
+
+  // Tile t, of bf16 rows: of the new tokens, or of a bf16 cache.
+  auto load = [&](int t, int set) {
+    const bool old = !FP8 && t < t_old;
+    const KeyList& list = old ? ks.cached : ks.fresh;
+    const uint8_t* k = old ? kc : kn;
+    const uint8_t* v = old ? vc : vn;
+    const int64_t step = old ? a.sr : a.nsn * 2;
+    const int e0 = (t - (t < t_old ? 0 : t_old)) * kStreamKeys + lane / CPR;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int r = min(t * kStreamKeys + i * R + lane / C, ks.nold - 1);
-      const int64_t at = cbase + ks.row(r) * a.sr + (lane % C) * 16;
-      k[i] = load_stream16(a.k + at);
-      v[i] = load_stream16(a.v + at);
+    for (int i = 0; i < NP; ++i) {
+      const int64_t at = list.row(min(e0 + i * RPP, list.n - 1)) * step + (lane % CPR) * 16;
+      rk[set + i] = load_stream16(k + at);
+      rv[set + i] = load_stream16(v + at);
     }
   };
-  const int e_old = min(t1, t_old);
+  // The same of an fp8 cache: sixteen elements a load.
+  auto load8 = [&](int t, int set) {
 #pragma unroll
-  for (int j = 0; j < PF; ++j)
-    if (t0 + j < e_old) load_old(t0 + j, rk[j], rv[j]);
+    for (int i = 0; i < N; ++i) {
+      const int e = min(t * kStreamKeys + i * R + lane / C, ks.cached.n - 1);
+      const int64_t at = ks.cached.row(e) * a.sr + (lane % C) * 16;
+      rk[set + i] = load_stream16(kc + at);
+      rv[set + i] = load_stream16(vc + at);
+    }
+  };
+  const int end8 = FP8 ? min(t1, t_old) : t0;  // tiles before it are of an fp8 cache
+#pragma unroll
+  for (int j = 0; j < PF; ++j) {
+    if constexpr (FP8) {
+      if (t0 + j < end8) load8(t0 + j, j * N);
+    } else {
+      if (t0 + j < t1) load(t0 + j, j * NP);
+    }
+  }
 
   TreeRow my[NB];
   TreeWave<D, F32, NB> w;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    const int row = min(32 * nb + (lane & 31), rows - 1);
-    my[nb] = tree_row(a, rq, ks, b, h, row);
+    const int row = min(r0 + 32 * nb + (lane & 31), rows - 1);
+    my[nb] = tree_row(a, rq, ks, b, row);
     w.start(a, lane, nb,
             a.q + b * a.qsb + my[nb].node * a.qsn + (h * a.G + row % a.G) * a.qsh);
   }
-  const int deepest = a.depth ? a.max_depth[b] : n1;
   const CacheScale cs = cache_scale<FP8>(a, pair);
 
-  auto add_hidden = [&](uint32_t bad, const uint32_t (&see)[NB][1], auto&& row_of) {
+  // A tile of bf16 rows in registers [set, set + NP); `next` fills them again.
+  auto tile = [&](int t, int set, auto&& next) {
+    const bool old = !FP8 && t < t_old;
+    const int e0 = (t - (t < t_old ? 0 : t_old)) * kStreamKeys;
+    const bool hide = old ? hides_cached(a, rq, ks, tt, e0, kStreamKeys)
+                          : hides_fresh(a, ks, tt, e0, kStreamKeys);
+    uint32_t see[NB] = {};
+    if (hide)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+        see[nb] = old ? see_cached(ks, my[nb], e0) : see_fresh(a, ks, tt, my[nb], b, e0);
+    uint4 v[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int r = i * RPP + lane / CPR;
+      v[i] = rv[set + i];
+      *reinterpret_cast<uint4*>(lk + r * kKRow<D> + (lane % CPR) * 8) = rk[set + i];
+      *reinterpret_cast<uint4*>(lv + r * kVRow<D> + (lane % CPR) * 8) = v[i];
+    }
+    uint32_t bad = 0;
+    if (hide) bad = clean_rows<D>(v, lv + (lane / CPR) * kVRow<D> + (lane % CPR) * 8, RPP * kVRow<D>);
+    next();
+    fence_wave();
+    w.tile(lane, lk, lv, a.scale_log2, false, 1.f, hide, see);
 #pragma unroll 1
     for (; bad; bad &= bad - 1) {
       const int e = __builtin_ctz(bad);
       bool mine[NB];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) mine[nb] = (see[nb][0] >> e) & 1u;
-      w.add_nonfinite(lane, row_of(e), mine);
+      for (int nb = 0; nb < NB; ++nb) mine[nb] = (see[nb] >> e) & 1u;
+      const uint8_t* x =
+          old ? vc + ks.cached.row(e0 + e) * a.sr : vn + ks.fresh.row(e0 + e) * a.nsn * 2;
+      w.add_nonfinite(lane, reinterpret_cast<const uint16_t*>(x), mine);
     }
+    fence_wave();
   };
 
-  for (int t = t0; t < e_old; t += PF) {
+  if constexpr (FP8) {
+    for (int t = t0; t < end8; t += PF) {
 #pragma unroll
-    for (int j = 0; j < PF; ++j) {
-      if (t + j >= e_old) break;
-      const int e0 = (t + j) * kStreamKeys;
-      const bool hides = hides_cached(a, rq, ks, e0, kStreamKeys, deepest);
+      for (int j = 0; j < PF; ++j) {
+        if (t + j >= end8) break;
+        const int e0 = (t + j) * kStreamKeys;
+        const bool hide = hides_cached(a, rq, ks, tt, e0, kStreamKeys);
+        uint32_t see[NB] = {};
+        if (hide)
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int r = i * R + lane / C;
-        if constexpr (FP8) {
-          const int c = 2 * (lane % C);
+          for (int nb = 0; nb < NB; ++nb) see[nb] = see_cached(ks, my[nb], e0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int r = i * R + lane / C, c = 2 * (lane % C);
           uint4 lo, hi;
-          widen_fp8(rk[j][i], lo, hi);
-          *reinterpret_cast<uint4*>(lk + r * kKRow<D> + (c) * 8) = lo;
-          *reinterpret_cast<uint4*>(lk + r * kKRow<D> + (c + 1) * 8) = hi;
-          widen_fp8(rv[j][i], lo, hi);
-          *reinterpret_cast<uint4*>(lv + r * kVRow<D> + (c) * 8) = lo;
-          *reinterpret_cast<uint4*>(lv + r * kVRow<D> + (c + 1) * 8) = hi;
-        } else {
-          *reinterpret_cast<uint4*>(lk + r * kKRow<D> + (lane % C) * 8) = rk[j][i];
-          *reinterpret_cast<uint4*>(lv + r * kVRow<D> + (lane % C) * 8) = rv[j][i];
+          widen_fp8(rk[j * N + i], lo, hi);
+          *reinterpret_cast<uint4*>(lk + r * kKRow<D> + c * 8) = lo;
+          *reinterpret_cast<uint4*>(lk + r * kKRow<D> + c * 8 + 8) = hi;
+          widen_fp8(rv[j * N + i], lo, hi);
+          *reinterpret_cast<uint4*>(lv + r * kVRow<D> + c * 8) = lo;
+          *reinterpret_cast<uint4*>(lv + r * kVRow<D> + c * 8 + 8) = hi;
         }
+        if (t + j + PF < end8) load8(t + j + PF, j * N);
+        fence_wave();
+        w.tile(lane, lk, lv, cs.sl, cs.flip, cs.vs, hide, see);
+        fence_wave();
       }
-      if (t + j + PF < e_old) load_old(t + j + PF, rk[j], rv[j]);
-      uint32_t bad = 0;
-      if (!FP8 && hides) bad = clean_rows<D>(lv + (lane / C) * kVRow<D> + (lane % C) * 8, N, R * kVRow<D>);
-      fence_wave();
-      uint32_t see[NB][1] = {};
-      if (hides)
+    }
+    for (int t = max(t0, t_old); t < t1; ++t) {
+      load(t, 0);
+      tile(t, 0, [] {});
+    }
+  } else {
+    for (int t = t0; t < t1; t += PF) {
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) see[nb][0] = see_cached(ks, my[nb], e0);
-      w.template tile<1>(lane, lk, lv, cs.sl, FP8 && cs.flip, FP8 ? cs.vs : 1.f, hides, see);
-      if (!FP8 && bad)
-        add_hidden(bad, see, [&](int e) {
-          return reinterpret_cast<const uint16_t*>(a.v + cbase + ks.row(e0 + e) * a.sr);
+      for (int j = 0; j < PF; ++j) {
+        if (t + j >= t1) break;
+        tile(t + j, j * NP, [&] {
+          if (t + j + PF < t1) load(t + j + PF, j * NP);
         });
-      fence_wave();
+      }
     }
-  }
-
-  const uint16_t* kn = a.kn + b * a.nsb + h * a.nsh;
-  const uint16_t* vn = a.vn + b * a.nsb + h * a.nsh;
-  for (int t = max(t0, t_old); t < t1; ++t) {
-    const int x0 = (t - t_old) * kStreamKeys;
-    uint4 k[NP], v[NP];
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int x = min(x0 + i * RPP + lane / CPR, ks.nnew - 1);
-      const int64_t at = ks.node(x) * a.nsn + (lane % CPR) * 8;
-      k[i] = *reinterpret_cast<const uint4*>(kn + at);
-      v[i] = *reinterpret_cast<const uint4*>(vn + at);
-    }
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int r = i * RPP + lane / CPR;
-      *reinterpret_cast<uint4*>(lk + r * kKRow<D> + (lane % CPR) * 8) = k[i];
-      *reinterpret_cast<uint4*>(lv + r * kVRow<D> + (lane % CPR) * 8) = v[i];
-    }
-    const uint32_t bad =
-        clean_rows<D>(lv + (lane / CPR) * kVRow<D> + (lane % CPR) * 8, NP, RPP * kVRow<D>);
-    fence_wave();
-    uint32_t see[NB][1];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-      see[nb][0] = see_new(a, ks, my[nb], b, x0, a.S - rq.base, deepest >= a.W);
-    w.template tile<1>(lane, lk, lv, a.scale_log2, false, 1.f, true, see);
-    add_hidden(bad, see, [&](int e) { return vn + ks.node(x0 + e) * a.nsn; });
-    fence_wave();
   }
 
   // Join the waves' results, a block of rows at a time: every wave scales its own
   // to the common maximum and leaves them in its LDS region, 32 columns of a row
   // per step, then the workgroup's threads add them up.
   const bool split = nsp > 1;
-  float* part = a.part + (static_cast<int64_t>(pair) * a.splits + sp) * (32 * NB) * kPartRow<D>;
+  float* part = a.part + ((static_cast<int64_t>(pair) * a.row_tiles + qt) * a.splits + sp) *
+                             (32 * NB) * kPartRow<D>;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     float l1, l2;
@@ -768,7 +851,7 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
       }
     __syncthreads();
     for (int at = threadIdx.x; at < 32 * (D / 4); at += 64 * NW) {
-      const int r = at / (D / 4), g = at % (D / 4), row = 32 * nb + r;
+      const int r = at / (D / 4), g = at % (D / 4), row = r0 + 32 * nb + r;
       if (row >= rows) break;
       float mr = kTreeMin, lr = 0.f;
 #pragma unroll
@@ -787,7 +870,7 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
         s.w += x.w;
       }
       if (split) {
-        float* p = part + row * kPartRow<D>;
+        float* p = part + (row - r0) * kPartRow<D>;
         *reinterpret_cast<float4*>(p + 4 * g) = s;
         if (g == 0) *reinterpret_cast<float2*>(p + D) = make_float2(mr, lr);
       } else {
@@ -801,31 +884,53 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
 }
 
 // Joins a row's splits: out = sum_s 2^(m_s - M) acc_s / sum_s 2^(m_s - M) l_s.
-// One wave per query row.
+// One wave per query row.  Bound by its chain of memory latencies, so the first
+// kAhead splits are read before it is known how many there are.
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a, int tile_rows,
                                                            int tile_keys) {
-  constexpr int E = D / 64;
+  constexpr int E = D / 64, kAhead = 8;
   const int lane = threadIdx.x & 63;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + wave;
   const int per_pair = a.row_tiles * tile_rows;
   const int pair = static_cast<int>(at / per_pair), row = static_cast<int>(at % per_pair);
   if (pair >= a.B * a.Hkv) return;
-  const int b = pair / a.Hkv, h = pair % a.Hkv, qt = row / tile_rows;
-  const TreeReq rq = tree_request(a.base, a.count, b, a.N, a.Lp, a.Ldec);
-  const int rows = rq.n * a.G, r0 = qt * tile_rows;
-  if (row >= rows) return;
-  const TreeKeys ks = tree_keys(a, rq, r0 / a.G, (min(r0 + tile_rows, rows) - 1) / a.G);
-  const int tiles = (ks.nold + tile_keys - 1) / tile_keys + (ks.nnew + tile_keys - 1) / tile_keys;
-  const int nsp = tree_splits(a, tiles);
-  if (nsp <= 1) return;
+  const int b = pair / a.Hkv, h = pair % a.Hkv, qt = row / tile_rows, r0 = qt * tile_rows;
   const int64_t step = static_cast<int64_t>(tile_rows) * kPartRow<D>;
   const float* part = a.part + (static_cast<int64_t>(pair) * a.row_tiles + qt) * a.splits * step +
                       (row - r0) * kPartRow<D>;
-  float M = kTreeMin;
-  for (int s = 0; s < nsp; ++s) M = fmaxf(M, part[s * step + D]);
-  float L = 0.f, acc[E] = {};
-  for (int s = 0; s < nsp; ++s) {
+  float pm[kAhead], pl[kAhead], px[kAhead][E];
+#pragma unroll
+  for (int s = 0; s < kAhead; ++s) {
+    const float* x = part + min(s, a.splits - 1) * step;
+    pm[s] = x[D];
+    pl[s] = x[D + 1];
+#pragma unroll
+    for (int e = 0; e < E; ++e) px[s][e] = x[lane * E + e];
+  }
+  const TreeReq rq = tree_request(a.base, a.count, b, a.N, a.Lp, a.Ldec);
+  const int rows = rq.n * a.G;
+  if (row >= rows) return;
+  const TreeKeys ks = tree_keys(a, rq, r0 / a.G, (min(r0 + tile_rows, rows) - 1) / a.G);
+  const int tiles = (ks.cached.n + tile_keys - 1) / tile_keys + (ks.fresh.n + tile_keys - 1) / tile_keys;
+  const int nsp = tree_splits(a, tiles);
+  if (nsp <= 1) return;
+  float M = kTreeMin, L = 0.f, acc[E] = {};
+#pragma unroll
+  for (int s = 0; s < kAhead; ++s)
+    if (s < nsp) M = fmaxf(M, pm[s]);
+  for (int s = kAhead; s < nsp; ++s) M = fmaxf(M, part[s * step + D]);
+#pragma unroll
+  for (int s = 0; s < kAhead; ++s)
+    if (s < nsp) {
+      const float w = fast_exp2(pm[s] - M);
+      L = fmaf(pl[s], w, L);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(px[s][e], w, acc[e]);
+    }
+#pragma unroll 4
+  for (int s = kAhead; s < nsp; ++s) {
     const float* x = part + s * step;
     const float w = fast_exp2(x[D] - M);
     L = fmaf(x[D + 1], w, L);
@@ -833,8 +938,8 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a, int tile_
     for (int e = 0; e < E; ++e) acc[e] = fmaf(x[lane * E + e], w, acc[e]);
   }
   const float inv = 1.f / L;
-  const int64_t to = ((static_cast<int64_t>(b) * a.N + row / a.G) * a.Hq + h * a.G + row % a.G) * D +
-                     lane * E;
+  const int64_t to =
+      ((static_cast<int64_t>(b) * a.N + row / a.G) * a.Hq + h * a.G + row % a.G) * D + lane * E;
   if constexpr (F32) {
 #pragma unroll
     for (int e = 0; e < E; ++e) static_cast<float*>(a.out)[to + e] = acc[e] * inv;
@@ -856,12 +961,10 @@ hipError_t launch_stream(const TreeLaunch& l, const TreeArgs& a, hipStream_t st)
 template <bool FP8, int D, bool F32>
 hipError_t launch_one(const TreeLaunch& l, const TreeArgs& a, hipStream_t st) {
   hipError_t e;
-  if (l.rows > 64) {
-    tree_tile_kernel<FP8, D, F32><<<dim3(static_cast<uint32_t>((l.workgroups + 7) / 8 * 8)),
-                                    dim3(256), 0, st>>>(a);
+  const dim3 grid(static_cast<uint32_t>((l.workgroups + 7) / 8 * 8));
+  if (l.rows == 128) {
+    tree_tile_kernel<FP8, D, F32, 1><<<grid, dim3(256), 0, st>>>(a);
     e = hipGetLastError();
-  } else if (l.rows > 32) {
-    e = launch_stream<FP8, D, F32, 2, 4>(l, a, st);
   } else {
     e = l.waves == 8 ? launch_stream<FP8, D, F32, 1, 8>(l, a, st)
                      : launch_stream<FP8, D, F32, 1, 4>(l, a, st);
