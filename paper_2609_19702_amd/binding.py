@@ -456,17 +456,21 @@ class Tree:
             raise ValueError(f"a tree has at most {MAX_TREE_NODES} nodes, got {nodes}")
         self.nodes, self.base, self.count, self.plan = int(nodes), base, count, plan
         self.c = TreeRequest(self.nodes, _ptr(base), _ptr(count), _ptr(plan))
-        self._batch = None  # the batch these tensors were last checked for
+        self.ref = C.byref(self.c)
+        self._seen = None  # the batch and device these tensors were last checked for
 
-    def check(self, batch, where, base=True):
+    def check(self, batch, device, where, base=True):
         if base and self.base is None:
             raise ValueError(f"{where} needs the tree's base positions")
-        if batch != self._batch:
+        if (batch, device) != self._seen:
             _need(self.base, "base", torch.int32, batch * 4)
             _need(self.count, "count", torch.int32, batch * 4)
             if self.plan is not None:
                 _need(self.plan, "plan", None, tree_plan_bytes(batch, self.nodes))
-            self._batch = batch
+            for x in (self.base, self.count, self.plan):
+                if isinstance(x, torch.Tensor) and x.get_device() != device:
+                    raise _elsewhere(x, "the tree", device)
+            self._seen = (batch, device)
 
 
 def make_tree(nodes, base=None, count=None, plan=None) -> Tree:
@@ -494,71 +498,89 @@ def tree_workspace_bytes(p: Params, s: Shape, nodes: int) -> int:
     return lib().dsa_tree_workspace_bytes(C.byref(p), C.byref(s), nodes)
 
 
-def _on_device(*tensors):
-    """Every tensor is on the current device, whose stream the call takes."""
-    at = torch.cuda.current_device()
-    for x in tensors:
-        if x is not None and x.device.index != at:
-            raise ValueError(f"a tensor is on {x.device}, the current device is cuda:{at}")
+# The checks below follow one pattern: a few comparisons that a right call
+# passes, and the words for what is wrong only after one of them failed.
+
+def _elsewhere(x, name, device):
+    return ValueError(f"{name} is on {x.device}, the current device is cuda:{device}")
 
 
-def _need_shape(x, name, dtype, shape):
+def _need_dense(x, name, dtype, shape, device):
+    """A dense tensor on the current device, whose stream the call takes."""
+    if (x.dtype is dtype and x.shape == shape and x.get_device() == device
+            and x.is_contiguous()):
+        return
     _need(x, name, dtype)
-    if tuple(x.shape) != shape:
-        raise ValueError(f"{name} must have shape {shape}, got {tuple(x.shape)}")
+    if x.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(x.shape)}")
+    raise _elsewhere(x, name, device)
 
 
-def _node_rows(x, name, shape):
+def _need_bytes(x, name, device):
+    if x is None or (x.get_device() == device and x.is_contiguous()):
+        return
+    _need(x, name)
+    raise _elsewhere(x, name, device)
+
+
+def _node_rows(x, name, shape, device):
     """Strides of a bf16 tensor of rows ``[(layers,) B, nodes, heads, d]``, the
     rows themselves dense."""
-    if x.dtype is not torch.bfloat16 or not x.is_cuda:
-        _need(x, name, torch.bfloat16, contiguous=False)
-    if tuple(x.shape) != shape:
-        raise ValueError(f"{name} must have shape {shape}, got {tuple(x.shape)}")
     st = x.stride()
-    if st[-1] != 1:
+    if not (x.dtype is torch.bfloat16 and x.shape == shape and x.get_device() == device
+            and st[-1] == 1):
+        _need(x, name, torch.bfloat16, contiguous=False)
+        if x.shape != shape:
+            raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(x.shape)}")
+        if x.get_device() != device:
+            raise _elsewhere(x, name, device)
         raise ValueError(f"{name}: head_dim must be contiguous")
+    return st
+
+
+def _new_rows(k_new, v_new, shape, device):
+    st = _node_rows(k_new, "k_new", shape, device)
+    if _node_rows(v_new, "v_new", shape, device) != st:
+        raise ValueError("k_new and v_new must share strides")
     return NodeRows(st[-4], st[-3], st[-2], st[0] if len(st) == 5 else 0)
 
 
-def _new_rows(k_new, v_new, shape):
-    rows = _node_rows(k_new, "k_new", shape)
-    _node_rows(v_new, "v_new", shape)
-    if k_new.stride() != v_new.stride():
-        raise ValueError("k_new and v_new must share strides")
-    return rows
-
-
-def _check_caches(p, s, k, v, layout, rows_needed, layers=None):
+def _check_caches(p, s, k, v, layout, rows_needed, layers, device):
     _need(k, "k", _KV_DTYPES, contiguous=False)
     _need(v, "v", _KV_DTYPES, contiguous=False)
-    if k.dtype != v.dtype or k.shape != v.shape or k.stride() != v.stride():
+    shape, st = k.shape, k.stride()
+    if k.dtype is not v.dtype or shape != v.shape or st != v.stride():
         raise ValueError("k and v must share element type, shape and strides")
+    for x, name in ((k, "k"), (v, "v")):
+        if x.get_device() != device:
+            raise _elsewhere(x, name, device)
     if (layout.dtype == KV_BF16) != (k.dtype is torch.bfloat16):
         raise ValueError(f"the layout is not of a {k.dtype} cache")
-    if layers is not None and (k.dim() != 5 or k.shape[0] != layers):
-        raise ValueError(f"the caches must be of {layers} layers, got shape {tuple(k.shape)}")
-    if k.dim() >= 4 and layout.d_row_base is None:
-        nb, nh, rows, nd = k.shape[-4:]
+    if layers is not None and (len(shape) != 5 or shape[0] != layers):
+        raise ValueError(f"the caches must be of {layers} layers, got shape {tuple(shape)}")
+    if len(shape) >= 4 and layout.d_row_base is None:
+        nb, nh, rows, nd = shape[-4:]
         if (nb < s.batch or nh < s.num_kv_heads or nd != s.head_dim or rows < rows_needed
-                or (layout.stride_batch, layout.stride_head, layout.stride_row)
-                != tuple(k.stride()[-4:-1])):
-            raise ValueError(f"cache of shape {tuple(k.shape)} does not hold {s.batch} requests x "
+                or layout.stride_batch != st[-4] or layout.stride_head != st[-3]
+                or layout.stride_row != st[-2]):
+            raise ValueError(f"cache of shape {tuple(shape)} does not hold {s.batch} requests x "
                              f"{s.num_kv_heads} KV heads x {rows_needed}+ rows of {s.head_dim} "
                              "elements as the layout says")
 
 
 def tree_plan(parent, count, plan_buf, stream=None):
     """Depths and ancestors of trees: ``parent`` int32 [B, nodes], -1 for none."""
-    _need(parent, "parent", torch.int32)
-    if parent.dim() != 2:
-        raise ValueError(f"parent must be [B, nodes], got {tuple(parent.shape)}")
-    batch, nodes = parent.shape
-    _need(count, "count", torch.int32, batch * 4)
-    _need(plan_buf, "plan")
-    _on_device(parent, count, plan_buf)
-    _check(lib().dsa_tree_plan(batch, nodes, _ptr(parent), _ptr(count), _ptr(plan_buf),
-                               _nbytes(plan_buf), _stream(stream)), "dsa_tree_plan")
+    device = torch.cuda.current_device() if parent.is_cuda else None
+    shape = parent.shape
+    if len(shape) != 2:
+        raise ValueError(f"parent must be [B, nodes], got {tuple(shape)}")
+    _need_dense(parent, "parent", torch.int32, shape, device)
+    if count is not None:
+        _need_dense(count, "count", torch.int32, shape[:1], device)
+    _need_bytes(plan_buf, "plan", device)
+    _check(lib().dsa_tree_plan(shape[0], shape[1], parent.data_ptr(), _ptr(count),
+                               plan_buf.data_ptr(), plan_buf.nbytes, _stream(stream)),
+           "dsa_tree_plan")
 
 
 def tree_attention(p, s, tree: Tree, q, k_new, v_new, k, v, layout: KVLayout, sm_scale, out,
@@ -567,24 +589,23 @@ def tree_attention(p, s, tree: Tree, q, k_new, v_new, k, v, layout: KVLayout, sm
     bf16 [B, nodes, Hq, d], ``k_new`` and ``v_new`` bf16 [B, nodes, Hkv, d]
     (any strides with dense rows, as slices of a fused projection), ``out``
     [B, nodes, Hq, d] in fp32 or bf16."""
-    B_, Hq, Hkv, d = s.batch, s.num_q_heads, s.num_kv_heads, s.head_dim
-    n = tree.nodes
-    tree.check(B_, "tree_attention")
-    q_rows = _node_rows(q, "q", (B_, n, Hq, d))
-    new_rows = _new_rows(k_new, v_new, (B_, n, Hkv, d))
+    device = torch.cuda.current_device() if q.is_cuda else None
+    B_, Hq, Hkv, d, n = s.batch, s.num_q_heads, s.num_kv_heads, s.head_dim, tree.nodes
+    shape = (B_, n, Hq, d)
+    st = _node_rows(q, "q", shape, device)
+    tree.check(B_, device, "tree_attention")
+    new_rows = _new_rows(k_new, v_new, (B_, n, Hkv, d), device)
     out_type = _OUT_TYPES.get(out.dtype)
     if out_type is None:
         raise ValueError(f"out must be fp32 or bf16, got {out.dtype}")
-    _need_shape(out, "out", out.dtype, (B_, n, Hq, d))
-    _check_caches(p, s, k, v, layout,
-                  p.prompt_len + layout.ring_rows)
-    _need(workspace, "workspace")
-    _on_device(tree.base, q, k_new, v_new, k, v, out, workspace)
+    _need_dense(out, "out", out.dtype, shape, device)
+    _check_caches(p, s, k, v, layout, p.prompt_len + layout.ring_rows, None, device)
+    _need_bytes(workspace, "workspace", device)
     _check(lib().dsa_tree_attention(
-        C.byref(p), C.byref(s), C.byref(tree.c), _ptr(q), C.byref(q_rows), _ptr(k_new),
-        _ptr(v_new), C.byref(new_rows), _ptr(k), _ptr(v), C.byref(layout), float(sm_scale),
-        _ptr(out), out_type, _ptr(workspace), 0 if workspace is None else _nbytes(workspace),
-        _stream(stream)), "dsa_tree_attention")
+        C.byref(p), C.byref(s), tree.ref, q.data_ptr(), C.byref(NodeRows(st[0], st[1], st[2], 0)),
+        k_new.data_ptr(), v_new.data_ptr(), C.byref(new_rows), k.data_ptr(), v.data_ptr(),
+        C.byref(layout), sm_scale, out.data_ptr(), out_type, _ptr(workspace),
+        0 if workspace is None else workspace.nbytes, _stream(stream)), "dsa_tree_attention")
 
 
 def tree_verify(tree: Tree, tokens, target, draft, uniform, path, accepted, next_token,
@@ -593,24 +614,26 @@ def tree_verify(tree: Tree, tokens, target, draft, uniform, path, accepted, next
     [B, nodes], ``target`` fp32 [B, nodes, V], ``draft`` the same or None
     (certain drafts), ``uniform`` fp32 [B, nodes + 1]; out: ``path`` int32
     [B, nodes], ``accepted`` and ``next_token`` int32 [B]."""
-    _need(target, "target", torch.float32)
-    if target.dim() != 3:
-        raise ValueError(f"target must be [B, nodes, V], got {tuple(target.shape)}")
-    batch, n, vocab = target.shape
+    device = torch.cuda.current_device() if target.is_cuda else None
+    shape = target.shape
+    if len(shape) != 3:
+        raise ValueError(f"target must be [B, nodes, V], got {tuple(shape)}")
+    batch, n, vocab = shape
     if n != tree.nodes:
         raise ValueError(f"target has {n} nodes, the tree {tree.nodes}")
-    tree.check(batch, "tree_verify", base=False)
-    _need_shape(tokens, "tokens", torch.int32, (batch, n))
+    _need_dense(target, "target", torch.float32, shape, device)
+    tree.check(batch, device, "tree_verify", base=False)
     if draft is not None:
-        _need_shape(draft, "draft", torch.float32, (batch, n, vocab))
-    _need_shape(uniform, "uniform", torch.float32, (batch, n + 1))
-    _need_shape(path, "path", torch.int32, (batch, n))
-    _need_shape(accepted, "accepted", torch.int32, (batch,))
-    _need_shape(next_token, "next_token", torch.int32, (batch,))
-    _on_device(tokens, target, draft, uniform, path, accepted, next_token, tree.count, tree.plan)
-    _check(lib().dsa_tree_verify(batch, vocab, C.byref(tree.c), _ptr(tokens), _ptr(target),
-                                 _ptr(draft), _ptr(uniform), _ptr(path), _ptr(accepted),
-                                 _ptr(next_token), _stream(stream)), "dsa_tree_verify")
+        _need_dense(draft, "draft", torch.float32, shape, device)
+    _need_dense(tokens, "tokens", torch.int32, (batch, n), device)
+    _need_dense(uniform, "uniform", torch.float32, (batch, n + 1), device)
+    _need_dense(path, "path", torch.int32, (batch, n), device)
+    _need_dense(accepted, "accepted", torch.int32, (batch,), device)
+    _need_dense(next_token, "next_token", torch.int32, (batch,), device)
+    _check(lib().dsa_tree_verify(batch, vocab, tree.ref, tokens.data_ptr(), target.data_ptr(),
+                                 _ptr(draft), uniform.data_ptr(), path.data_ptr(),
+                                 accepted.data_ptr(), next_token.data_ptr(), _stream(stream)),
+           "dsa_tree_verify")
 
 
 def kv_append(p, s, tree: Tree, k_new, v_new, k, v, layout: KVLayout, path=None, accepted=None,
@@ -620,20 +643,21 @@ def kv_append(p, s, tree: Tree, k_new, v_new, k, v, layout: KVLayout, path=None,
     layer (``k_new`` [B, nodes, Hkv, d], ``k`` [B, Hkv, rows, d]) or all of
     them (both with layers in front, ``layout`` of one layer's cache but with
     the scales of all, [layers, B * Hkv])."""
+    device = torch.cuda.current_device() if k_new.is_cuda else None
     B_, Hkv, d, n = s.batch, s.num_kv_heads, s.head_dim, tree.nodes
-    tree.check(B_, "kv_append")
     layers = k_new.shape[0] if k_new.dim() == 5 else None
-    lead = () if layers is None else (layers,)
-    rows = _new_rows(k_new, v_new, lead + (B_, n, Hkv, d))
+    shape = (B_, n, Hkv, d) if layers is None else (layers, B_, n, Hkv, d)
+    rows = _new_rows(k_new, v_new, shape, device)
+    tree.check(B_, device, "kv_append")
     _check_caches(p, s, k, v, layout,
-                  p.prompt_len + (layout.ring_rows or p.grid_h * p.grid_w), layers)
+                  p.prompt_len + (layout.ring_rows or p.grid_h * p.grid_w), layers, device)
     if path is not None:
-        _need_shape(path, "path", torch.int32, (B_, n))
-    _need(accepted, "accepted", torch.int32, B_ * 4)
-    _on_device(tree.base, k_new, v_new, k, v, path, accepted)
+        _need_dense(path, "path", torch.int32, (B_, n), device)
+    if accepted is not None:
+        _need_dense(accepted, "accepted", torch.int32, (B_,), device)
     _check(lib().dsa_kv_append(
-        C.byref(p), C.byref(s), C.byref(tree.c), _ptr(k_new), _ptr(v_new), C.byref(rows),
-        _ptr(path), _ptr(accepted), layers or 1, _ptr(k), _ptr(v), C.byref(layout),
+        C.byref(p), C.byref(s), tree.ref, k_new.data_ptr(), v_new.data_ptr(), C.byref(rows),
+        _ptr(path), _ptr(accepted), layers or 1, k.data_ptr(), v.data_ptr(), C.byref(layout),
         k.stride(0) if layers else 0, _stream(stream)), "dsa_kv_append")
 
 

@@ -64,8 +64,7 @@ __global__ __launch_bounds__(kMaxNodes) void tree_plan_kernel(TreePlanArgs a) {
 
 constexpr int kVerifyWaves = 16;
 constexpr int kVerifyBlock = 64 * kVerifyWaves;
-constexpr int kMaxBlocks = 1024;  // of a vocabulary, each a multiple of kScan tokens
-constexpr int kScan = 1024;       // tokens a wave takes at a time
+constexpr int kScan = 1024;  // tokens a wave takes at a time, 16 to a lane
 
 __device__ __forceinline__ double wave_add(double x) {
 #pragma unroll
@@ -83,30 +82,112 @@ __device__ __forceinline__ double wave_upto(double x, int lane) {
   return x;
 }
 
+// What the rejected children of a node leave of its distribution, up to a
+// factor.  With draft rows, P_0 = p and P_k+1 = max(P_k - q, 0) / its sum is
+// max(p - a_k q, 0) / s_k with a_0 = 0, s_0 = 1, a_k+1 = a_k + s_k and s_k the sum
+// of max(p - a_k q, 0): one multiply-add per token, however many were rejected.
+// Without, the tokens taken out are gone.
+struct Rest {
+  const float* p;  // target row
+  const float* q;  // draft row, or nullptr
+  double a;
+  const int* taken;
+  int ntaken;
+
+  // fmax gives 0 for NaN.
+  __device__ __forceinline__ static double of(float p, float q, double a) {
+    return fmax(fma(-a, static_cast<double>(fmaxf(q, 0.f)), static_cast<double>(p)), 0.);
+  }
+  // Some taken token in [lo, hi): then every value there is checked.
+  __device__ __forceinline__ bool any(int lo, int hi) const {
+    bool yes = false;
+    for (int i = 0; i < ntaken; ++i) yes |= taken[i] >= lo && taken[i] < hi;
+    return yes;
+  }
+  __device__ __forceinline__ bool gone(int v) const {
+    bool yes = false;
+    for (int i = 0; i < ntaken; ++i) yes |= taken[i] == v;
+    return yes;
+  }
+  __device__ __forceinline__ double at(int v) const {
+    return gone(v) ? 0. : of(p[v], q ? q[v] : 0.f, a);
+  }
+  // A lane's sum over the tokens [lo, hi) that it takes.  1024 at a time with 8
+  // loads of 16 bytes on their way (4 where nothing was rejected yet, a = 0): one CU
+  // reads a row, and only bytes in flight make it fast.  Rows need not be
+  // 16-byte aligned.
+  __device__ __forceinline__ double sum(int lane, int lo, int hi) const {
+    struct __attribute__((packed, aligned(4))) Four {
+      float f[4];
+    };
+    constexpr int kWide = 4;
+    double s = 0.;
+    if (any(lo, hi)) {
+      for (int v = lo + lane; v < hi; v += 64) s += at(v);
+      return s;
+    }
+    for (; hi - lo >= 256 * kWide; lo += 256 * kWide) {
+      Four x[kWide], y[kWide];
+      const Four* px = reinterpret_cast<const Four*>(p + lo) + lane;
+      const Four* qx = reinterpret_cast<const Four*>(q + lo) + lane;
+#pragma unroll
+      for (int e = 0; e < kWide; ++e) x[e] = px[64 * e];
+      if (a != 0.) {
+#pragma unroll
+        for (int e = 0; e < kWide; ++e) y[e] = qx[64 * e];
+#pragma unroll
+        for (int e = 0; e < kWide; ++e)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) s += of(x[e].f[k], y[e].f[k], a);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kWide; ++e)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) s += fmax(static_cast<double>(x[e].f[k]), 0.);
+      }
+    }
+    for (; lo < hi; lo += kScan) {
+      float x[16], y[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int v = min(lo + 64 * e + lane, hi - 1);
+        x[e] = p[v];
+        y[e] = a != 0. ? q[v] : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s += of(lo + 64 * e + lane < hi ? x[e] : 0.f, y[e], a);
+    }
+    return s;
+  }
+};
+
 // One workgroup per request.  What the decisions read of the distributions, two
 // numbers per drafted token, is gathered for all nodes at once; the walk down
 // the tree then runs on LDS.  The vocabulary is only streamed where a child was
 // rejected and the residual's sum is needed (draft rows), and for the next
-// token; the blocks' sums of that last pass lead to the block it lies in.
-// Sums and comparisons are in fp64: every difference of two fp32 values that
-// is compared with a random number is then exact or nearly so.
+// token, where the sums of that last pass, a sixteenth of the vocabulary per
+// wave, lead to the sixteenth it lies in, and so on down.  Sums and comparisons
+// are in fp64: every difference of two fp32 values that is compared with a
+// random number is then exact or nearly so.  Bound by what one CU reads of a row
+// (64 bytes a cycle: 1.7 us for 65536 fp32 numbers) and by latency.
 __global__ __launch_bounds__(kVerifyBlock) void tree_verify_kernel(VerifyArgs a) {
   __shared__ int parent[kMaxNodes], token[kMaxNodes], path[kMaxNodes], taken[kMaxNodes];
   __shared__ float uni[kMaxNodes], px[kMaxNodes], qx[kMaxNodes];
-  __shared__ double z[kMaxNodes + 1], zinv[kMaxNodes + 1];  // residual sums of the node at hand
-  __shared__ double block_sum[kMaxBlocks];
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ double part[2][kVerifyWaves];  // sums of the waves' shares, two passes in turn
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = a.count ? min(max(a.count[b], 0), a.N) : a.N;
   const int V = a.V;
   const bool draft = a.draft != nullptr;
+  const float last = a.uniform[static_cast<int64_t>(b) * (a.N + 1) + a.N];
   if (tid < kMaxNodes) {
     int par = -1, tok = -1;
     float u = 1.f, p = 0.f, q = 0.f;
     if (tid < n) {
       par = a.parent ? a.parent[b * a.N + tid] : tid - 1;
-      if (par < 0 || par >= tid) par = -1;
       tok = a.tokens[b * a.N + tid];
       u = a.uniform[static_cast<int64_t>(b) * (a.N + 1) + tid];
+      if (par < 0 || par >= tid) par = -1;
       if (par >= 0 && tok >= 0 && tok < V) {
         const int64_t at = (static_cast<int64_t>(b) * a.N + par) * V + tok;
         p = a.target[at];
@@ -122,184 +203,136 @@ __global__ __launch_bounds__(kVerifyBlock) void tree_verify_kernel(VerifyArgs a)
   }
   __syncthreads();
 
-  const int span = kScan * ((V + kScan * kMaxBlocks - 1) / (kScan * kMaxBlocks));  // tokens per block
-  const int blocks = (V + span - 1) / span;
-  const float* tr = nullptr;
-  const float* dr = nullptr;
-  int ntaken = 0;
-  // What is left of token v's probability after k rejected children.
-  auto residual = [&](float pf, float qf, int k) {
-    double r = pf > 0.f ? pf : 0.f;
-    const double q = qf > 0.f ? qf : 0.f;
-    for (int i = 0; i < k; ++i) {
-      r = r * zinv[i] - q;
-      r = r > 0. ? r : 0.;
-    }
-    return r;
-  };
-  auto left = [&](int v, float pf, float qf, int k) {
-    if (draft) return residual(pf, qf, k);
-    double r = pf > 0.f ? pf : 0.f;
-    for (int i = 0; i < ntaken; ++i)
-      if (taken[i] == v) r = 0.;
-    return r;
-  };
-  // Block sums of the residual after k rejected children of the node at hand.
-  auto pass = [&](int k) {
-    for (int j = wave; j < blocks; j += kVerifyWaves) {
-      double s = 0.;
-      for (int v0 = j * span; v0 < min((j + 1) * span, V); v0 += kScan) {
-        float p[16], q[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int v = v0 + 64 * e + lane;
-          p[e] = v < V ? tr[v] : 0.f;
-          q[e] = draft && v < V ? dr[v] : 0.f;
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s += left(v0 + 64 * e + lane, p[e], q[e], k);
-      }
-      s = wave_add(s);
-      if (lane == 0) block_sum[j] = s;
-    }
+  Rest rest{nullptr, nullptr, 0., taken, 0};
+  const int share = V / kVerifyWaves;  // tokens per wave; the last one takes the rest, too
+  int turn = 0;
+  // The residual's sum; the waves' shares of it stay in part[turn].
+  auto pass = [&]() {
+    turn ^= 1;
+    const double s = wave_add(rest.sum(lane, wave * share, wave == kVerifyWaves - 1 ? V : (wave + 1) * share));
+    if (lane == 0) part[turn][wave] = s;
     __syncthreads();
-  };
-  // Their total: every wave computes it alike.
-  auto total = [&]() {
-    double s = 0.;
-    for (int j = lane; j < blocks; j += 64) s += block_sum[j];
-    return wave_add(s);
+    double all = 0.;
+#pragma unroll
+    for (int i = 0; i < kVerifyWaves; ++i) all += part[turn][i];
+    return all;
   };
 
-  int cur = 0, len = 0, k = 0;
-  bool summed = false;  // block_sum holds the sums for (cur, k)
+  int cur = 0, len = 0;
   double sum = 0.;
   if (n > 0) {
+    bool summed = false;  // part[turn] belongs to `rest`
     for (;;) {
-      if (tid == 0) {
-        path[len] = cur;
-        z[0] = zinv[0] = 1.;
-      }
+      if (tid == 0) path[len] = cur;
       ++len;
-      tr = a.target + (static_cast<int64_t>(b) * a.N + cur) * V;
-      dr = draft ? a.draft + (static_cast<int64_t>(b) * a.N + cur) * V : nullptr;
-      k = ntaken = 0;
+      const int64_t row = (static_cast<int64_t>(b) * a.N + cur) * V;
+      rest.p = a.target + row;
+      rest.q = draft ? a.draft + row : nullptr;
+      rest.a = 0.;
+      rest.ntaken = 0;
+      double s = 1.;       // the residual's sum (draft rows), or what is not taken out
+      bool spent = false;  // nothing is left of the residual
       summed = false;
-      double rest = 1.;
-      bool spent = false;
       int next = -1;
-      __syncthreads();
-      for (int w = 0; w < kMaxNodes && next < 0; w += 64) {
+      for (int w = 0; w < a.N && next < 0; w += 64) {
         uint64_t kids = __ballot(w + lane > cur && parent[w + lane] == cur);
         while (kids && next < 0) {
           const int i = w + __builtin_ctzll(kids);
           kids &= kids - 1;
-          const double u = uni[i];
+          const double u = uni[i], p = px[i];
           if (draft) {
             if (spent) continue;
-            const double r = residual(px[i], qx[i], k);
-            if (u * static_cast<double>(qx[i]) * z[k] < r) {
+            if (u * static_cast<double>(qx[i]) * s < Rest::of(px[i], qx[i], rest.a)) {
               next = i;
               break;
             }
-            pass(k + 1);
-            const double s = total();
-            __syncthreads();
-            if (s > 0.) {
-              ++k;
-              if (tid == 0) {
-                z[k] = s;
-                zinv[k] = 1. / s;
-              }
-              sum = s;
-              summed = true;
-              __syncthreads();
-            } else {
-              spent = true;
+            const double before = rest.a;
+            rest.a += s;
+            const double left = pass();
+            summed = spent = left <= 0.;
+            if (spent) {
+              rest.a = before;
               summed = false;
+            } else {
+              s = sum = left;
+              summed = true;
             }
           } else {
-            const double p = px[i];
             bool again = false;
-            for (int e = 0; e < ntaken; ++e) again |= taken[e] == token[i];
-            if (!again && p > 0. && u * rest < p) {
+            for (int e = 0; e < rest.ntaken; ++e) again |= taken[e] == token[i];
+            if (again) continue;
+            if (p > 0. && u * s < p) {
               next = i;
               break;
             }
-            if (!again) {
-              rest -= p;
-              __syncthreads();
-              if (tid == 0) taken[ntaken] = token[i];
-              ++ntaken;
-              __syncthreads();
-            }
+            s -= p;
+            if (tid == 0) taken[rest.ntaken] = token[i];
+            ++rest.ntaken;
+            __syncthreads();
           }
         }
       }
       if (next < 0) break;
       cur = next;
-      __syncthreads();
+      __syncthreads();  // `taken` starts anew
     }
-    if (!summed) {
-      pass(k);
-      sum = total();
-    }
+    if (!summed) sum = pass();
   }
-  if (tid < a.N) a.path[b * a.N + tid] = path[tid];
+  if (tid < a.N) a.path[static_cast<int64_t>(b) * a.N + tid] = path[tid];
   if (tid == 0) a.accepted[b] = len;
-  if (wave) return;
 
-  // The next token, by the first wave: the first block whose running sum passes
-  // the target, then the first token in it.
-  int found = -1;
-  if (n > 0 && sum > 0.) {
-    const double aim = static_cast<double>(a.uniform[static_cast<int64_t>(b) * (a.N + 1) + a.N]) * sum;
-    double before = 0.;
-    int at = -1, some = -1;  // the block, and the last one with any mass
-    for (int j0 = 0; j0 < blocks && at < 0; j0 += 64) {
-      const double x = j0 + lane < blocks ? block_sum[j0 + lane] : 0.;
-      const double upto = before + wave_upto(x, lane);
-      const uint64_t over = __ballot(upto > aim && x > 0.);
-      const uint64_t mass = __ballot(x > 0.);
-      if (mass) some = j0 + 63 - __builtin_clzll(mass);
-      if (over) {
-        const int w = __builtin_ctzll(over);
-        at = j0 + w;
-        before = __shfl(upto - x, w, 64);
-      } else {
-        before = __shfl(upto, 63, 64);
-      }
-    }
-    const bool past = at < 0;  // rounding only: take the last token with mass
-    if (past) at = some;
-    int last = -1;
-    for (int v0 = at * span; v0 < min((at + 1) * span, V) && found < 0; v0 += kScan) {
-      double r[16], s = 0.;
-      const int v1 = v0 + lane * 16;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const bool in = v1 + e < V;
-        r[e] = left(v1 + e, in ? tr[v1 + e] : 0.f, in && draft ? dr[v1 + e] : 0.f, k);
-        s += r[e];
-      }
-      double upto = before + wave_upto(s, lane) - s;
-      int mine = -1, tail = -1;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        upto += r[e];
-        if (r[e] > 0.) {
-          tail = v1 + e;
-          if (mine < 0 && !past && upto > aim) mine = v1 + e;
-        }
-      }
-      const uint64_t hit = __ballot(mine >= 0), any = __ballot(tail >= 0);
-      if (any) last = __shfl(tail, 63 - __builtin_clzll(any), 64);
-      if (hit) found = __shfl(mine, __builtin_ctzll(hit), 64);
-      before = __shfl(upto, 63, 64);
-    }
-    if (found < 0) found = last;
+  // The next token: the first share whose running sum passes the target, then the
+  // first of its sixteenths, down to what one wave holds.  Rounding can leave the
+  // target unpassed at the very end: then the last share with any mass, and the
+  // last token of it.
+  if (!(n > 0 && sum > 0.)) {
+    if (tid == 0) a.next[b] = -1;
+    return;
   }
-  if (lane == 0) a.next[b] = found;
+  const double aim = static_cast<double>(last) * sum;
+  double before = 0.;  // sum ahead of `lo`
+  bool past = false;   // the target was not passed
+  int lo = 0, hi = V;
+  // The share that the target lies in, of those in part[turn].
+  auto pick = [&]() {
+    int at = -1, some = 0;
+    for (int i = 0; i < kVerifyWaves && at < 0; ++i) {
+      const double x = part[turn][i];
+      if (x > 0.) some = i;
+      if (x > 0. && !past && before + x > aim)
+        at = i;
+      else
+        before += x;
+    }
+    past |= at < 0;
+    return at < 0 ? some : at;
+  };
+  int size = share, at = pick();
+  for (;;) {
+    lo += at * size;
+    hi = at == kVerifyWaves - 1 ? hi : lo + size;
+    turn ^= 1;
+    if (hi - lo <= 64 * kVerifyWaves) break;
+    size = (hi - lo) / kVerifyWaves;
+    const int from = lo + wave * size;
+    const double s =
+        wave_add(rest.sum(lane, from, wave == kVerifyWaves - 1 ? hi : from + size));
+    if (lane == 0) part[turn][wave] = s;
+    __syncthreads();
+    at = pick();
+  }
+  // A token per thread.
+  const int v = lo + tid;
+  const double r = v < hi ? rest.at(v) : 0.;
+  const double s = wave_add(r);
+  if (lane == 0) part[turn][wave] = s;
+  __syncthreads();
+  at = pick();
+  if (wave != at) return;
+  const double upto = before + wave_upto(r, lane);
+  const uint64_t hit = __ballot(!past && r > 0. && upto > aim), mass = __ballot(r > 0.);
+  const int found = hit ? __builtin_ctzll(hit) : 63 - __builtin_clzll(mass | 1);
+  if (lane == 0) a.next[b] = lo + 64 * wave + found;
 }
 
 // Eight elements of a row and of its V row per thread: 16 bytes in, 16 (bf16)
