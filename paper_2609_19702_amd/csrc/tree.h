@@ -132,6 +132,12 @@ struct KeyList {
   }
 };
 
+// One of two lists, field by field (a reference to either would put both into memory).
+__device__ __forceinline__ KeyList pick_list(bool first, const KeyList& a, const KeyList& b) {
+  return {first ? a.n : b.n, first ? a.pre : b.pre, first ? a.shift : b.shift,
+          first ? a.wrap : b.wrap, first ? a.ring : b.ring};
+}
+
 // The keys that nodes n0 .. n1 of a request can attend.
 //   cached: rows 0 .. pre - 1 of the cache (prompt and sinks), which every node
 //           attends, then the positions from j0 on

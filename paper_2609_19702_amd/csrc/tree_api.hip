@@ -54,7 +54,9 @@ dsa_status tree_derive(const dsa_params* p, const dsa_shape* s, int nodes, Deriv
   if (nodes < 1 || nodes > kMostNodes) return DSA_ERR_INVALID_ARG;
   if (d->mode == DSA_MODE_DIAGONAL) return DSA_ERR_UNSUPPORTED;
   *l = tree_launch(*d, nodes);
-  if (l->workgroups + 8 > kMostGrid || static_cast<int64_t>(d->B) * nodes > (int64_t(1) << 30))
+  // pairs rounded up to eight (tree_grid)
+  if (l->workgroups / d->B / d->Hkv * (static_cast<int64_t>(d->B) * d->Hkv + 8) > kMostGrid ||
+      static_cast<int64_t>(d->B) * nodes > (int64_t(1) << 30))
     return DSA_ERR_INVALID_ARG;
   return DSA_OK;
 }

@@ -69,13 +69,31 @@ __device__ __forceinline__ uint32_t low_bits(int x) {
   return x <= 0 ? 0u : x >= 32 ? ~0u : (1u << x) - 1u;
 }
 
-// Work item of a workgroup: consecutive items share K and V, and the eight
-// XCDs (workgroup id mod 8) take an eighth of the items each, in order, so what
-// one workgroup brings into an XCD's L2 the next finds there.
-__device__ __forceinline__ int xcd_item(int items) {
-  const int per = (items + 7) / 8, at = blockIdx.x >> 3;
-  const int item = (blockIdx.x & 7) * per + at;
-  return at < per && item < items ? item : -1;
+// The (request, KV head) pair of a workgroup and its place among the pair's
+// per_pair workgroups, which share K and V.  Workgroup ids go round the eight XCDs,
+// each with an L2 of its own, so a pair stays on one XCD, and neighbouring pairs (a
+// request's heads, with its length) go to different ones.  Where the pairs do not
+// go evenly round, the workgroups are cut into eight equal runs instead.  (All
+// heads of a request on one XCD: 62.3 us where this takes 59.9 for 32 ragged
+// requests of 32 heads, 41.9 and 38.8 for 16 ragged prompts.)
+struct TreeItem {
+  int pair, sub;  // pair < 0: nothing to do
+};
+__device__ __forceinline__ TreeItem tree_item(int pairs, int per_pair) {
+  const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3;
+  if (pairs % 8 == 0 || pairs >= 64) {
+    const int pair = at / per_pair * 8 + xcd;
+    return {pair < pairs ? pair : -1, at % per_pair};
+  }
+  const int items = pairs * per_pair, per = (items + 7) / 8, item = xcd * per + at;
+  if (at >= per || item >= items) return {-1, 0};
+  return {item / per_pair, item % per_pair};
+}
+// Workgroups to launch for it.
+inline uint32_t tree_grid(int64_t pairs, int64_t per_pair) {
+  return static_cast<uint32_t>(pairs % 8 == 0 || pairs >= 64
+                                   ? (pairs + 7) / 8 * 8 * per_pair
+                                   : (pairs * per_pair + 7) / 8 * 8);
 }
 
 template <int D>
@@ -160,6 +178,19 @@ constexpr int kKRow = D + 8;
 template <int D>
 constexpr int kVRow = D + 16;
 
+// Order of a row's 16-byte chunks (8 elements) in LDS.  A lane widens 16 fp8
+// elements to two chunks; stored side by side, the first chunks of all lanes
+// would take every second place and meet in the banks, so fp8 builds put the even
+// chunks ahead of the odd ones: chunk at place j.
+template <int D, bool EVEN>
+__host__ __device__ constexpr int chunk_at(int j) {
+  return !EVEN ? j : j < D / 16 ? 2 * j : 2 * (j - D / 16) + 1;
+}
+template <int D, bool EVEN>
+__host__ __device__ constexpr int place_of(int c) {
+  return !EVEN ? c : c / 2 + D / 16 * (c % 2);
+}
+
 // A wave's NB blocks of 32 query rows against tiles of keys in LDS.
 //
 // Both products run on the matrix cores with the keys as rows, S^T = K Q^T and
@@ -168,17 +199,18 @@ constexpr int kVRow = D + 16;
 // maximum and the rescale need one exchange, with the lane's other half, and the
 // weights are the second product's operand where they are.  V comes back from
 // LDS transposed (ds_read_b64_tr_b16) in the order of keys the weights have.
-template <int D, bool F32, int NB>
+template <int D, bool F32, int NB, bool FP8>
 struct TreeWave {
   bf16x8 qf[NB][D / 16];
   f32x16 o[NB][D / 32];
   float m[NB], l[NB];
 
-  // Queries: the second operand of S^T, elements 16 s + 8 hh .. of the row.
+  // Queries: the second operand of S^T, in the order of K's elements in LDS.
   __device__ __forceinline__ void start(const TreeArgs& a, int lane, int nb, const uint16_t* q) {
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
-      uint4 x = *reinterpret_cast<const uint4*>(q + 16 * s + 8 * (lane >> 5));
+      uint4 x = *reinterpret_cast<const uint4*>(q + (lane >> 5 ? 8 * chunk_at<D, FP8>(2 * s + 1)
+                                                              : 8 * chunk_at<D, FP8>(2 * s)));
       x.x ^= a.q_sign;
       x.y ^= a.q_sign;
       x.z ^= a.q_sign;
@@ -206,14 +238,14 @@ struct TreeWave {
   // i % 4, negated where `flip`, -inf where `hides` and the row does not see them.
   __device__ __forceinline__ void scores(int lane, const uint16_t* lk, bool flip, bool hides,
                                          const uint32_t (&see)[NB], f32x16 (&sc)[NB]) {
-    const int lq = lane & 31, hh = lane >> 5;
+    const int hh = lane >> 5;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[nb][i] = 0.f;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
-      const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lk + lq * kKRow<D> + 16 * s + 8 * hh);
+      const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lk + (lane & 31) * kKRow<D> + 16 * s + 8 * hh);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
         sc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[nb][s], sc[nb], 0, 0, 0);
@@ -335,8 +367,8 @@ struct TreeWave {
     values(lane, lv, sc);
   }
 
-  // 64 keys: the second half's scores are under way while the first's weights
-  // are computed, and the first half's values while the second's are.
+  // 64 keys: the second half's scores are under way while the first's
+  // weights are computed, and the first half's values while the second's are.
   __device__ __forceinline__ void tile2(int lane, const uint16_t* lk, const uint16_t* lv, float sl,
                                         bool flip, float vs, bool hides,
                                         const uint32_t (&see)[2][NB]) {
@@ -358,7 +390,9 @@ struct TreeWave {
                                                 const bool (&mine)[NB]) {
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
-      const uint32_t x = v[32 * c + (lane & 31)], size = x & 0x7fffu;
+      const int place = 4 * c + ((lane & 31) >> 3);  // (chunk_at of a lane's place)
+      const int at = FP8 ? (place < D / 16 ? 2 * place : 2 * (place - D / 16) + 1) : place;
+      const uint32_t x = v[8 * at + (lane & 7)], size = x & 0x7fffu;
       const uint32_t up = x == 0x7f80u || size > 0x7f80u ? 0x7f7f7f7fu : 0u;
       const uint32_t down = x == 0xff80u || size > 0x7f80u ? 0xff7fff7fu : 0u;
 #pragma unroll
@@ -422,17 +456,10 @@ __device__ __forceinline__ uint32_t clean_rows(const uint4 (&x)[N], uint16_t* v,
   return rows;
 }
 
-// Outputs of a finished block of 32 rows, or its partial result.
-template <int D, bool F32>
-__device__ __forceinline__ void tree_write(const TreeArgs& a, int lane, const f32x16 (&o)[D / 32],
-                                           float inv, int64_t out) {
-  const int64_t at = out * D + 4 * (lane >> 5);
-#pragma unroll
-  for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4)
-      store4<F32>(a.out, at + 32 * c + 2 * i, o[c][i] * inv, o[c][i + 1] * inv, o[c][i + 2] * inv,
-                  o[c][i + 3] * inv);
+// Columns of output registers 4 k .. of block c (k = 0 .. 3), half hh's four.
+template <int D, bool FP8>
+__device__ __forceinline__ int out_col(int c, int k, int hh) {
+  return 8 * chunk_at<D, FP8>(4 * c + k) + 4 * hh;
 }
 
 // Splits of a row tile that have keys, and the tiles of 'part' of 'parts'.
@@ -461,11 +488,9 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
   __shared__ __align__(16) uint16_t lv[2][kTileKeys * kVRow<D>];
   __shared__ uint32_t lbad[2][4];  // V rows of a tile that are not finite, by wave (clean_rows)
 
-  const int per_pair = a.row_tiles * a.splits;
-  const int item = xcd_item(a.B * a.Hkv * per_pair);
-  if (item < 0) return;
-  const int pair = item / per_pair, sub = item % per_pair;
-  const int b = pair / a.Hkv, h = pair % a.Hkv;
+  const TreeItem item = tree_item(a.B * a.Hkv, a.row_tiles * a.splits);
+  if (item.pair < 0) return;
+  const int pair = item.pair, sub = item.sub, b = pair / a.Hkv, h = pair % a.Hkv;
   const int qt = a.row_tiles - 1 - sub / a.splits, sp = sub % a.splits;  // longest first
   const TreeReq rq = tree_request(a.base, a.count, b, a.N, a.Lp, a.Ldec);
   const int rows = rq.n * a.G, r0 = qt * kTileRows;
@@ -485,7 +510,7 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
   const bool wave_on = r0 + 32 * NB * wave < rows;
   const CacheScale cs = cache_scale<FP8>(a, pair);
   TreeRow my[NB];
-  TreeWave<D, F32, NB> w;
+  TreeWave<D, F32, NB, FP8> w;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int row = min(row0 + 32 * nb, rows - 1);
@@ -503,7 +528,7 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
   // Tile t, of bf16 rows: of the new tokens, or of a bf16 cache.
   auto load = [&](int t) {
     const bool old = !FP8 && t < t_old;
-    const KeyList& list = old ? ks.cached : ks.fresh;
+    const KeyList list = pick_list(old, ks.cached, ks.fresh);
     const uint8_t* k = old ? kc : kn;
     const uint8_t* v = old ? vc : vn;
     const int64_t step = old ? a.sr : a.nsn * 2;
@@ -520,7 +545,7 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
                      : hides_fresh(a, ks, tt, (t - t_old) * kTileKeys, kTileKeys);
   };
   auto put = [&](int t, int buf) {
-    const int c = tid % CPR;
+    const int c = place_of<D, FP8>(tid % CPR);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int r = i * RPP + tid / CPR;
@@ -545,14 +570,14 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
   auto put8 = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < NP8; ++i) {
-      const int r = i * RP8 + tid / CP8, c = 2 * (tid % CP8);
+      const int r = i * RP8 + tid / CP8, c = tid % CP8;
       uint4 lo, hi;
       widen_fp8(rk[i], lo, hi);
       *reinterpret_cast<uint4*>(lk[buf] + r * kKRow<D> + c * 8) = lo;
-      *reinterpret_cast<uint4*>(lk[buf] + r * kKRow<D> + c * 8 + 8) = hi;
+      *reinterpret_cast<uint4*>(lk[buf] + r * kKRow<D> + c * 8 + D / 2) = hi;
       widen_fp8(rv[i], lo, hi);
       *reinterpret_cast<uint4*>(lv[buf] + r * kVRow<D> + c * 8) = lo;
-      *reinterpret_cast<uint4*>(lv[buf] + r * kVRow<D> + c * 8 + 8) = hi;
+      *reinterpret_cast<uint4*>(lv[buf] + r * kVRow<D> + c * 8 + D / 2) = hi;
     }
   };
   auto see_of = [&](int t, uint32_t (&see)[2][NB]) {
@@ -581,33 +606,40 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
       }
   };
 
+  // A tile's rows go into LDS at the start of the tile before, when they have had a
+  // whole tile's time to arrive, and the tile after them is asked for.
   int t = t0, buf = 0;
   if constexpr (FP8) {
     const int end = min(t1, t_old);
     if (t < end) {
       load8(t);
       put8(0);
+      if (t + 1 < end) load8(t + 1);
       __syncthreads();
     }
     for (; t < end; ++t, buf ^= 1) {
-      if (t + 1 < end) load8(t + 1);
+      if (t + 1 < end) put8(buf ^ 1);
+      if (t + 2 < end) load8(t + 2);
+      asm volatile("" ::: "memory");
       if (wave_on) {
         uint32_t see[2][NB] = {};
         const bool hide = hides(t);
         if (hide) see_of(t, see);
         w.tile2(lane, lk[buf], lv[buf], cs.sl, cs.flip, cs.vs, hide, see);
       }
-      if (t + 1 < end) put8(buf ^ 1);
       __syncthreads();
     }
   }
   if (t < t1) {
     load(t);
     put(t, buf);
+    if (t + 1 < t1) load(t + 1);
     __syncthreads();
   }
   for (; t < t1; ++t, buf ^= 1) {
-    if (t + 1 < t1) load(t + 1);
+    if (t + 1 < t1) put(t + 1, buf ^ 1);
+    if (t + 2 < t1) load(t + 2);
+    asm volatile("" ::: "memory");  // the loads stay ahead of the tile
     if (wave_on) {
       uint32_t see[2][NB] = {};
       const bool hide = hides(t);
@@ -615,7 +647,6 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
       w.tile2(lane, lk[buf], lv[buf], a.scale_log2, false, 1.f, hide, see);
       if (hide) add_hidden(t, buf, see);
     }
-    if (t + 1 < t1) put(t + 1, buf ^ 1);
     __syncthreads();
   }
 
@@ -626,9 +657,17 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
     xor_pair<32>(w.l[nb], l1, l2);
     const float l = l1 + l2;
     if (row >= rows) continue;
+    const int hh = lane >> 5;
     if (nsp == 1) {
-      tree_write<D, F32>(a, lane, w.o[nb], 1.f / l,
-                         (static_cast<int64_t>(b) * a.N + my[nb].node) * a.Hq + h * a.G + row % a.G);
+      const float inv = 1.f / l;
+      const int64_t out =
+          ((static_cast<int64_t>(b) * a.N + my[nb].node) * a.Hq + h * a.G + row % a.G) * D;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          store4<F32>(a.out, out + out_col<D, FP8>(c, i / 4, hh), w.o[nb][c][i] * inv,
+                      w.o[nb][c][i + 1] * inv, w.o[nb][c][i + 2] * inv, w.o[nb][c][i + 3] * inv);
       continue;
     }
     float* part = a.part + ((static_cast<int64_t>(pair) * a.row_tiles + qt) * a.splits + sp) *
@@ -638,7 +677,7 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
       for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<float4*>(part + 32 * c + 2 * i + 4 * (lane >> 5)) = make_float4(
+        *reinterpret_cast<float4*>(part + out_col<D, FP8>(c, i / 4, hh)) = make_float4(
             w.o[nb][c][i], w.o[nb][c][i + 1], w.o[nb][c][i + 2], w.o[nb][c][i + 3]);
     if (lane < 32) *reinterpret_cast<float2*>(part + D) = make_float2(w.m[nb], l);
   }
@@ -649,27 +688,27 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
 constexpr int kStreamKeys = 32;  // keys of a wave's tile
 
 template <int D>
-constexpr uint32_t kStreamLds = kStreamKeys * (kKRow<D> + kVRow<D>) * 2;  // a wave's K and V tile, bytes
+constexpr uint32_t kStreamLds = kStreamKeys * (kKRow<D> + kVRow<D>) * 2;  // a wave's K and V tile
 
-// At most 32 NB query rows per (request, KV head): bound by the cache's bytes.
-// Every wave streams tiles of 32 keys of its own for all rows, through registers
-// (the next tiles are on their way while one is computed) and an LDS region of
-// its own, so the waves of a workgroup wait for each other only to join
-// their results at the end.
+// At most 32 NB query rows per workgroup: bound by the cache's bytes.  Every wave
+// streams tiles of 32 keys of its own for all rows, through registers (the next
+// tiles are on their way while one is computed) and an LDS region of its own, so
+// the waves of a workgroup wait for each other only to join their results at
+// the end.  (K straight into the matrix operand, a row per lane, halves the LDS
+// traffic but reads 32 bytes of a row at a time: 67 us against 62 for 1024 pairs of
+// 290 to 800 keys, d = 128.)
 template <bool FP8, int D, bool F32, int NB, int NW>
 __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeArgs a) {
-  constexpr int CPR = D / 8, RPP = 64 / CPR, NP = kStreamKeys / RPP;  // bf16 rows
+  constexpr int CPR = D / 8, RPP = 64 / CPR, NP = kStreamKeys / RPP;  // bf16 rows of V
   constexpr int C = FP8 ? D / 16 : CPR, R = 64 / C, N = kStreamKeys / R;  // the cache's
   constexpr int PF = N > 4 ? 1 : 2;  // tiles in flight ahead of the one at hand
   __shared__ __align__(16) uint16_t lds[NW * (kStreamLds<D> / 2)];
   __shared__ float lm[NW][32], ll[NW][32];
 
-  // Row tiles of the same keys are next to each other.
-  const int per_pair = a.splits * a.row_tiles;
-  const int item = xcd_item(a.B * a.Hkv * per_pair);
-  if (item < 0) return;
-  const int pair = item / per_pair, sp = item % per_pair / a.row_tiles, qt = item % a.row_tiles;
-  const int b = pair / a.Hkv, h = pair % a.Hkv;
+  const TreeItem item = tree_item(a.B * a.Hkv, a.row_tiles * a.splits);
+  if (item.pair < 0) return;
+  const int pair = item.pair, b = pair / a.Hkv, h = pair % a.Hkv;
+  const int sp = item.sub / a.row_tiles, qt = item.sub % a.row_tiles;
   const TreeReq rq = tree_request(a.base, a.count, b, a.N, a.Lp, a.Ldec);
   const int rows = rq.n * a.G, r0 = qt * 32 * NB;
   if (r0 >= rows) return;
@@ -696,14 +735,15 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
   // Tile t, of bf16 rows: of the new tokens, or of a bf16 cache.
   auto load = [&](int t, int set) {
     const bool old = !FP8 && t < t_old;
-    const KeyList& list = old ? ks.cached : ks.fresh;
+    const KeyList list = pick_list(old, ks.cached, ks.fresh);
+    const int64_t step = old ? a.sr : a.nsn * 2;
+    const int e0 = (t - (t < t_old ? 0 : t_old)) * kStreamKeys;
     const uint8_t* k = old ? kc : kn;
     const uint8_t* v = old ? vc : vn;
-    const int64_t step = old ? a.sr : a.nsn * 2;
-    const int e0 = (t - (t < t_old ? 0 : t_old)) * kStreamKeys + lane / CPR;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int64_t at = list.row(min(e0 + i * RPP, list.n - 1)) * step + (lane % CPR) * 16;
+      const int e = min(e0 + i * RPP + lane / CPR, list.n - 1);
+      const int64_t at = list.row(e) * step + (lane % CPR) * 16;
       rk[set + i] = load_stream16(k + at);
       rv[set + i] = load_stream16(v + at);
     }
@@ -729,7 +769,7 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
   }
 
   TreeRow my[NB];
-  TreeWave<D, F32, NB> w;
+  TreeWave<D, F32, NB, FP8> w;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int row = min(r0 + 32 * nb + (lane & 31), rows - 1);
@@ -750,16 +790,17 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
         see[nb] = old ? see_cached(ks, my[nb], e0) : see_fresh(a, ks, tt, my[nb], b, e0);
+    const int c = place_of<D, FP8>(lane % CPR);
     uint4 v[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int r = i * RPP + lane / CPR;
       v[i] = rv[set + i];
-      *reinterpret_cast<uint4*>(lk + r * kKRow<D> + (lane % CPR) * 8) = rk[set + i];
-      *reinterpret_cast<uint4*>(lv + r * kVRow<D> + (lane % CPR) * 8) = v[i];
+      *reinterpret_cast<uint4*>(lk + r * kKRow<D> + c * 8) = rk[set + i];
+      *reinterpret_cast<uint4*>(lv + r * kVRow<D> + c * 8) = v[i];
     }
     uint32_t bad = 0;
-    if (hide) bad = clean_rows<D>(v, lv + (lane / CPR) * kVRow<D> + (lane % CPR) * 8, RPP * kVRow<D>);
+    if (hide) bad = clean_rows<D>(v, lv + (lane / CPR) * kVRow<D> + c * 8, RPP * kVRow<D>);
     next();
     fence_wave();
     w.tile(lane, lk, lv, a.scale_log2, false, 1.f, hide, see);
@@ -789,14 +830,14 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
           for (int nb = 0; nb < NB; ++nb) see[nb] = see_cached(ks, my[nb], e0);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const int r = i * R + lane / C, c = 2 * (lane % C);
+          const int r = i * R + lane / C, c = lane % C;
           uint4 lo, hi;
           widen_fp8(rk[j * N + i], lo, hi);
           *reinterpret_cast<uint4*>(lk + r * kKRow<D> + c * 8) = lo;
-          *reinterpret_cast<uint4*>(lk + r * kKRow<D> + c * 8 + 8) = hi;
+          *reinterpret_cast<uint4*>(lk + r * kKRow<D> + c * 8 + D / 2) = hi;
           widen_fp8(rv[j * N + i], lo, hi);
           *reinterpret_cast<uint4*>(lv + r * kVRow<D> + c * 8) = lo;
-          *reinterpret_cast<uint4*>(lv + r * kVRow<D> + c * 8 + 8) = hi;
+          *reinterpret_cast<uint4*>(lv + r * kVRow<D> + c * 8 + D / 2) = hi;
         }
         if (t + j + PF < end8) load8(t + j + PF, j * N);
         fence_wave();
@@ -844,7 +885,7 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
-        const int g = 8 * c + i / 2 + (lane >> 5), r = lane & 31;
+        const int g = out_col<D, FP8>(c, i / 4, lane >> 5) / 4, r = lane & 31;
         *reinterpret_cast<float4*>(red + r * D + ((g ^ (r & 15)) * 4)) =
             make_float4(w.o[nb][c][i] * mine, w.o[nb][c][i + 1] * mine, w.o[nb][c][i + 2] * mine,
                         w.o[nb][c][i + 3] * mine);
@@ -903,7 +944,8 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a, int tile_
   float pm[kAhead], pl[kAhead], px[kAhead][E];
 #pragma unroll
   for (int s = 0; s < kAhead; ++s) {
-    const float* x = part + min(s, a.splits - 1) * step;
+    if (s >= a.splits) break;
+    const float* x = part + s * step;
     pm[s] = x[D];
     pl[s] = x[D + 1];
 #pragma unroll
@@ -953,15 +995,16 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a, int tile_
 
 template <bool FP8, int D, bool F32, int NB, int NW>
 hipError_t launch_stream(const TreeLaunch& l, const TreeArgs& a, hipStream_t st) {
-  tree_stream_kernel<FP8, D, F32, NB, NW><<<dim3(static_cast<uint32_t>((l.workgroups + 7) / 8 * 8)),
-                                            dim3(64 * NW), 0, st>>>(a);
+  tree_stream_kernel<FP8, D, F32, NB, NW>
+      <<<dim3(tree_grid(static_cast<int64_t>(a.B) * a.Hkv, a.row_tiles * a.splits)), dim3(64 * NW),
+         0, st>>>(a);
   return hipGetLastError();
 }
 
 template <bool FP8, int D, bool F32>
 hipError_t launch_one(const TreeLaunch& l, const TreeArgs& a, hipStream_t st) {
   hipError_t e;
-  const dim3 grid(static_cast<uint32_t>((l.workgroups + 7) / 8 * 8));
+  const dim3 grid(tree_grid(static_cast<int64_t>(a.B) * a.Hkv, a.row_tiles * a.splits));
   if (l.rows == 128) {
     tree_tile_kernel<FP8, D, F32, 1><<<grid, dim3(256), 0, st>>>(a);
     e = hipGetLastError();
