@@ -559,9 +559,10 @@ DSA_API size_t dsa_tree_workspace_bytes(const dsa_params* p, const dsa_shape* s,
  *             request, or -1 for none (depth 0); any other value is taken as
  *             -1 and flagged
  *   d_count   int32 [B] or NULL, as in dsa_tree
- *   d_plan    output, plan_bytes >= dsa_tree_plan_bytes(batch, nodes)
+ *   d_plan    output, 16-byte aligned, plan_bytes >=
+ *             dsa_tree_plan_bytes(batch, nodes)
  * Errors: INVALID_ARG (batch < 1, nodes outside [1, DSA_MAX_TREE_NODES], NULL
- * pointers), WORKSPACE (plan_bytes too small), HIP.
+ * or unaligned pointers), WORKSPACE (plan_bytes too small), HIP.
  */
 DSA_API dsa_status dsa_tree_plan(int32_t batch, int32_t nodes, const int32_t* d_parent,
                                  const int32_t* d_count, void* d_plan, size_t plan_bytes,
@@ -586,7 +587,8 @@ DSA_API dsa_status dsa_tree_plan(int32_t batch, int32_t nodes, const int32_t* d_
  *                    before base_b that a node can attend
  *   d_out            [B][N][Hq][d] in out_type, 16-byte aligned; rows of nodes
  *                    past a request's count are left as they are
- *   d_ws, ws_bytes   dsa_tree_workspace_bytes() bytes
+ *   d_ws, ws_bytes   dsa_tree_workspace_bytes() bytes, 16-byte aligned; need not be
+ *                    cleared
  * Algorithm 1 chooses what a token keeps from the step before it, one token
  * at a time: DSA_MODE_DIAGONAL is refused (a prompt goes in dense mode).
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.

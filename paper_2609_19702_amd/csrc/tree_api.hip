@@ -33,7 +33,8 @@ dsa_status tree_plan_layout(int batch, int nodes, dsa_tree_plan_layout* l) {
 
 dsa_status check_tree(const dsa_tree* t, int batch, int most) {
   if (!t || t->nodes < 1 || t->nodes > most) return DSA_ERR_INVALID_ARG;
-  if (t->d_plan && t->nodes > DSA_MAX_TREE_NODES) return DSA_ERR_INVALID_ARG;
+  if (t->d_plan && (t->nodes > DSA_MAX_TREE_NODES || !aligned16(t->d_plan)))
+    return DSA_ERR_INVALID_ARG;
   if (static_cast<int64_t>(batch) * t->nodes > (int64_t(1) << 30)) return DSA_ERR_INVALID_ARG;
   return DSA_OK;
 }
@@ -141,7 +142,7 @@ DSA_API dsa_status dsa_tree_plan(int32_t batch, int32_t nodes, const int32_t* d_
   dsa_tree_plan_layout l;
   const dsa_status st = dsa::tree_plan_layout(batch, nodes, &l);
   if (st != DSA_OK) return st;
-  if (!d_parent || !d_plan) return DSA_ERR_INVALID_ARG;
+  if (!d_parent || !d_plan || !dsa::aligned16(d_plan)) return DSA_ERR_INVALID_ARG;
   if (plan_bytes < l.bytes) return DSA_ERR_WORKSPACE;
   char* pb = static_cast<char*>(d_plan);
   dsa::TreePlanArgs a{};

@@ -48,7 +48,7 @@ def attention(p=None, s=None, t=None, q=PTR, qr=ROWS, kn=PTR, vn=PTR, nr=ROWS, k
 
 INVALID = [
     dict(t=False), dict(t=tree(0)), dict(t=tree(-1)), dict(t=tree((1 << 20) + 1)),
-    dict(t=tree(257, plan=PTR)), dict(t=tree(base=None)),
+    dict(t=tree(257, plan=PTR)), dict(t=tree(5, plan=PTR + 4)), dict(t=tree(base=None)),
     dict(q=None), dict(kn=None), dict(vn=None), dict(k=None), dict(v=None), dict(out=None),
     dict(qr=False), dict(nr=False), dict(q=PTR + 8), dict(kn=PTR + 2), dict(vn=PTR + 4),
     dict(k=PTR + 8), dict(v=PTR + 8), dict(out=PTR + 4),
@@ -128,6 +128,7 @@ def test_plan_refuses():
     assert f(2, 9, None, None, PTR, need, None) == B.ERR_INVALID_ARG
     assert f(2, 9, PTR, None, None, need, None) == B.ERR_INVALID_ARG
     assert f(2, 257, PTR, None, PTR, 1 << 30, None) == B.ERR_INVALID_ARG
+    assert f(2, 9, PTR, None, PTR + 8, need, None) == B.ERR_INVALID_ARG
     assert f(0, 9, PTR, None, PTR, need, None) == B.ERR_INVALID_ARG
     assert f(2, 9, PTR, None, PTR, need - 1, None) == B.ERR_WORKSPACE
 
