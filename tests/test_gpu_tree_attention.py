@@ -136,6 +136,59 @@ def test_equals_a_decode_step(d):
     assert (bufs.out - out[:, 0]).abs().max() <= (2 ** -15) * pr.v.abs().max()
 
 
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+@pytest.mark.parametrize("order", ["padded", "tokens"])
+def test_cache_strides(kv, order):
+    """Rows that are not next to each other: padded ones (not 16-byte aligned in
+    fp8), and a token-major cache."""
+    pr = Problem(nodes=21, heads=(8, 2), kv=kv, d=128, seed=6)
+    want = pr.run().clone()
+    b, h, rows, d = pr.k.shape
+    pr.out.fill_(7.0)
+    for name in ("k", "v"):
+        x = getattr(pr, name)
+        if order == "padded":
+            y = torch.zeros((b, h, rows, d + 8), dtype=x.dtype, device=DEV)[..., :d]
+        else:
+            y = torch.zeros((b, rows, h, d), dtype=x.dtype, device=DEV).transpose(1, 2)
+        y.view(torch.uint8 if kv == "fp8" else torch.bfloat16).copy_(
+            x.view(torch.uint8 if kv == "fp8" else torch.bfloat16))
+        setattr(pr, name, y)
+    pr.layout = B.kv_layout(pr.k, k_scale=pr.k_scale, v_scale=pr.v_scale)
+    assert torch.equal(pr.run(), want)
+
+
+def test_binding_refuses_wrong_tensors():
+    pr = Problem(nodes=6, heads=(8, 4))
+    ok = dict(q=pr.q, k_new=pr.kn, v_new=pr.vn, k=pr.k, v=pr.v, out=pr.out, workspace=pr.ws)
+
+    def call(**kw):
+        a = {**ok, **kw}
+        B.tree_attention(pr.p, pr.s, kw.pop("tree", pr.tree), a["q"], a["k_new"], a["v_new"],
+                         a["k"], a["v"], pr.layout, pr.scale, a["out"], a["workspace"])
+
+    bad = [dict(q=pr.q.float()), dict(q=pr.q[:, :5]), dict(k_new=pr.kn[..., :32]),
+           dict(q=pr.q.contiguous().transpose(2, 3)), dict(v_new=pr.vn.contiguous()),
+           dict(k=pr.k[:, :, :10], v=pr.v[:, :, :10]), dict(k=pr.k.float()), dict(v=pr.v[:1]),
+           dict(out=pr.out.half()), dict(out=pr.out[:, :5]), dict(out=pr.out.transpose(0, 1)),
+           dict(q=pr.q.cpu()), dict(out=pr.out.cpu()), dict(k=pr.k.cpu(), v=pr.v.cpu()),
+           dict(tree=B.make_tree(6, pr.base[:1], None, pr.tree_plan)),
+           dict(tree=B.make_tree(6, None, None, pr.tree_plan)),
+           dict(tree=B.make_tree(6, pr.base, None, pr.tree_plan[:64]))]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            call(**kw)
+    with pytest.raises(ValueError):
+        B.make_tree(6, pr.base.long())
+    with pytest.raises(ValueError):
+        B.tree_plan(pr.parent.long(), None, pr.tree_plan)
+    with pytest.raises(B.DSAError):
+        B.tree_plan(pr.parent, None, pr.tree_plan[:64])
+    with pytest.raises(ValueError):  # linear caches that cannot hold the whole image
+        B.kv_append(pr.p, pr.s, pr.tree, pr.kn, pr.vn, pr.k[:, :, :50], pr.v[:, :, :50], pr.layout)
+    call()
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
 def test_scales(scale):
     pr = Problem(nodes=20, heads=(8, 4), seed=9)

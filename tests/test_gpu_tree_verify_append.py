@@ -357,3 +357,63 @@ def test_append_replays():
         a.v.copy_(v0)
         a.check()
         assert torch.equal(a.k, k1) and torch.equal(a.v, v1)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+def test_append_into_padded_and_token_major_caches(kv):
+    """Any row strides, and nothing written between the rows."""
+    for order in ("padded", "tokens"):
+        a = Append(kv=kv, layers=2)
+        la, b, h, rows, d = a.k.shape
+        want = Append(kv=kv, layers=2)
+        want.run()
+        full = []
+        for name in ("k", "v"):
+            x = getattr(a, name)
+            if order == "padded":
+                f = torch.full((la, b, h, rows, d + 8), 3, dtype=x.dtype, device=DEV)
+                y = f[..., :d]
+                full.append(f[..., d:])
+            else:
+                y = torch.zeros((la, b, rows, h, d), dtype=x.dtype, device=DEV).transpose(2, 3)
+            y.copy_(x)
+            setattr(a, name, y)
+        a.run()
+        assert torch.equal(a.k, want.k) and torch.equal(a.v, want.v)
+        for f in full:
+            assert (f == 3).all()
+
+
+def test_verify_writes_its_outputs_only():
+    v = Verify(5, 9, 100, seed=6)
+    batch, nodes, vocab = v.target.shape
+    plan = torch.empty(B.tree_plan_bytes(batch, nodes), dtype=torch.uint8, device=DEV)
+    B.tree_plan(ints(v.parents), None, plan)
+    full = torch.full((batch * (nodes + 2) + 192,), -77, dtype=torch.int32, device=DEV)
+    path = full[64:64 + batch * nodes].view(batch, nodes)
+    got = full[64 + batch * nodes:64 + batch * (nodes + 1)]
+    tok = full[64 + batch * (nodes + 1):64 + batch * (nodes + 2)]
+    B.tree_verify(B.make_tree(nodes, plan=plan), v.tokens.to(DEV), v.target.to(DEV),
+                  v.draft.to(DEV), v.uniform.to(DEV), path, got, tok)
+    want = v.run()
+    assert torch.equal(path, want[0]) and torch.equal(got, want[1]) and torch.equal(tok, want[2])
+    assert (full[:64] == -77).all() and (full[-128:] == -77).all()
+
+
+def test_verify_binding_refuses_wrong_tensors():
+    v = Verify(2, 4, 30, seed=1)
+    t, d, u = v.target.to(DEV), v.draft.to(DEV), v.uniform.to(DEV)
+    x = v.tokens.to(DEV)
+    path = torch.empty((2, 4), dtype=torch.int32, device=DEV)
+    got, tok = (torch.empty(2, dtype=torch.int32, device=DEV) for _ in range(2))
+    tree = B.make_tree(4)
+    ok = [tree, x, t, d, u, path, got, tok]
+    bad = [(0, B.make_tree(5)), (1, x.long()), (1, x[:, :3]), (2, t.half()), (2, t[0]),
+           (2, t.transpose(0, 1)), (3, d[..., :29]), (3, d.double()), (4, u[:, :4]),
+           (5, path[:, :3]), (6, got[:1]), (7, tok.float()), (2, t.cpu()), (5, path.cpu())]
+    for i, wrong in bad:
+        with pytest.raises(ValueError):
+            B.tree_verify(*[wrong if j == i else y for j, y in enumerate(ok)])
+    with pytest.raises(ValueError):
+        B.tree_verify(B.make_tree(4, count=got[:1]), *ok[1:])
+    B.tree_verify(*ok)
