@@ -285,7 +285,9 @@ DSA_API dsa_status dsa_kv_append(const dsa_params* p, const dsa_shape* s, const 
                         static_cast<const void*>(d_v)})
     if (!dsa::aligned16(x)) return DSA_ERR_INVALID_ARG;
   const int64_t per = (static_cast<int64_t>(tree->nodes) * d.Hkv * (d.D / 8) + 255) / 256;
-  if (per > dsa::kMostGrid / layers / d.B) return DSA_ERR_INVALID_ARG;
+  // (a thread's place among a request's rows is counted in 31 bits)
+  if (per > std::min(dsa::kMostGrid / 256, dsa::kMostGrid / layers / d.B))
+    return DSA_ERR_INVALID_ARG;
   const int64_t esz = kv->dtype == DSA_KV_BF16 ? 2 : 1;
   dsa::AppendArgs a{};
   a.kn = static_cast<const uint16_t*>(d_k_new);

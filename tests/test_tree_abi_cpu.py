@@ -161,7 +161,8 @@ def test_append_refuses():
                 dict(layers=-1), dict(sl=-8), dict(sl=12), dict(kn=PTR + 8), dict(k=PTR + 4),
                 dict(nr=B.NodeRows(8, 8, 8, -8)), dict(nr=B.NodeRows(8, 8, 4, 8)),
                 dict(kv=layout(ring_rows=50)), dict(kv=layout(dtype=7)), dict(s=shape(batch=0)),
-                dict(t=tree(1 << 20), layers=1 << 30)):
+                dict(t=tree(1 << 20), layers=1 << 30),
+                dict(s=shape(1, 256, 256), t=tree(1 << 20))):
         assert call(**bad) == B.ERR_INVALID_ARG, bad
     assert call(s=shape(d=32)) == B.ERR_UNSUPPORTED
 
@@ -189,3 +190,17 @@ def test_binding_refuses_what_is_not_on_the_gpu():
                     B.kv_layout(k))
     with pytest.raises(ValueError):
         B.make_tree(300, PTR, plan=z(1))
+
+
+def test_a_tree_keeps_its_tensors():
+    """Its tensors cannot be exchanged under the pointers that it holds."""
+    t = B.make_tree(4, PTR)
+    for name in ("nodes", "base", "count", "plan"):
+        with pytest.raises(AttributeError):
+            setattr(t, name, None)
+    assert (t.nodes, t.base, t.count, t.plan) == (4, PTR, None, None)
+
+
+def test_plan_needs_a_buffer():
+    with pytest.raises(ValueError):
+        B.tree_plan(torch.zeros((2, 4), dtype=torch.int32), None, None)
