@@ -446,7 +446,8 @@ class Tree:
     """New tokens of every request (``dsa_tree``): ``nodes`` per request at
     most, ``base`` the decode position of each request's first (int32 [B]),
     ``count`` how many of them each has (int32 [B]; all), ``plan`` a buffer
-    filled by ``tree_plan`` (a chain).  Keeps the tensors it points to."""
+    filled by ``tree_plan`` (a chain).  Keeps the tensors it points to; they
+    can be written, not exchanged."""
 
     def __init__(self, nodes, base=None, count=None, plan=None):
         _need(base, "base", torch.int32)
@@ -454,10 +455,15 @@ class Tree:
         _need(plan, "plan")
         if plan is not None and nodes > MAX_TREE_NODES:
             raise ValueError(f"a tree has at most {MAX_TREE_NODES} nodes, got {nodes}")
-        self.nodes, self.base, self.count, self.plan = int(nodes), base, count, plan
-        self.c = TreeRequest(self.nodes, _ptr(base), _ptr(count), _ptr(plan))
+        self._held = (int(nodes), base, count, plan)
+        self.c = TreeRequest(int(nodes), _ptr(base), _ptr(count), _ptr(plan))
         self.ref = C.byref(self.c)
         self._seen = None  # the batch and device these tensors were last checked for
+
+    nodes = property(lambda self: self._held[0])
+    base = property(lambda self: self._held[1])
+    count = property(lambda self: self._held[2])
+    plan = property(lambda self: self._held[3])
 
     def check(self, batch, device, where, base=True):
         if base and self.base is None:
@@ -574,6 +580,8 @@ def tree_plan(parent, count, plan_buf, stream=None):
     shape = parent.shape
     if len(shape) != 2:
         raise ValueError(f"parent must be [B, nodes], got {tuple(shape)}")
+    if plan_buf is None:
+        raise ValueError("tree_plan needs a buffer for the plan")
     _need_dense(parent, "parent", torch.int32, shape, device)
     if count is not None:
         _need_dense(count, "count", torch.int32, shape[:1], device)
