@@ -130,6 +130,8 @@ struct KeyList {
     const int x = e + shift;
     return e < pre ? e : x >= wrap ? x - ring : x;
   }
+  // Row of entry e, of the last one for those after it: a tile's end.
+  __device__ __forceinline__ int64_t near(int e) const { return row(min(e, n - 1)); }
 };
 
 // One of two lists, field by field (a reference to either would put both into memory).

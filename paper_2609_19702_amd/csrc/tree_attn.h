@@ -2,6 +2,8 @@
 // (dsa_tree_attention), as templates over the cache's element type.
 #pragma once
 
+#include <type_traits>
+
 #include "device.h"
 #include "tree.h"
 
@@ -55,6 +57,11 @@ __device__ __forceinline__ void widen_fp8(const uint4& r, uint4& lo, uint4& hi) 
   }
   lo = make_uint4(o[0], o[1], o[2], o[3]);
   hi = make_uint4(o[4], o[5], o[6], o[7]);
+}
+
+// The sign bit of every byte of x that is an E4M3 NaN (seven ones).
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t x) {
+  return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
 }
 
 // x with every infinity and NaN replaced by 0.
@@ -191,22 +198,22 @@ __host__ __device__ constexpr int place_of(int c) {
   return !EVEN ? c : c / 2 + D / 16 * (c % 2);
 }
 
-// A wave's NB blocks of 32 query rows against tiles of keys in LDS.
+// A wave's 32 query rows against tiles of keys in LDS.
 //
 // Both products run on the matrix cores with the keys as rows, S^T = K Q^T and
 // O^T = V^T P^T (v_mfma_f32_32x32x16_bf16).  A lane then holds scores, weights
-// and outputs of one query row of each block (lane % 32) only: the running
+// and outputs of one query row (lane % 32) only: the running
 // maximum and the rescale need one exchange, with the lane's other half, and the
 // weights are the second product's operand where they are.  V comes back from
 // LDS transposed (ds_read_b64_tr_b16) in the order of keys the weights have.
-template <int D, bool F32, int NB, bool FP8>
+template <int D, bool F32, bool FP8>
 struct TreeWave {
-  bf16x8 qf[NB][D / 16];
-  f32x16 o[NB][D / 32];
-  float m[NB], l[NB];
+  bf16x8 qf[D / 16];
+  f32x16 o[D / 32];
+  float m, l;
 
   // Queries: the second operand of S^T, in the order of K's elements in LDS.
-  __device__ __forceinline__ void start(const TreeArgs& a, int lane, int nb, const uint16_t* q) {
+  __device__ __forceinline__ void start(const TreeArgs& a, int lane, const uint16_t* q) {
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
       uint4 x = *reinterpret_cast<const uint4*>(q + (lane >> 5 ? 8 * chunk_at<D, FP8>(2 * s + 1)
@@ -215,14 +222,14 @@ struct TreeWave {
       x.y ^= a.q_sign;
       x.z ^= a.q_sign;
       x.w ^= a.q_sign;
-      qf[nb][s] = __builtin_bit_cast(bf16x8, x);
+      qf[s] = __builtin_bit_cast(bf16x8, x);
     }
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[nb][c][i] = 0.f;
-    m[nb] = kTreeMin;
-    l[nb] = 0.f;
+      for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
+    m = kTreeMin;
+    l = 0.f;
   }
 
   // Four keys from `key` on, 16 columns of block c: see kernels above.
@@ -237,33 +244,24 @@ struct TreeWave {
   // S^T of 32 keys: lane (lq, hh) gets row lq's scores of keys 8 (i / 4) + 4 hh +
   // i % 4, negated where `flip`, -inf where `hides` and the row does not see them.
   __device__ __forceinline__ void scores(int lane, const uint16_t* lk, bool flip, bool hides,
-                                         const uint32_t (&see)[NB], f32x16 (&sc)[NB]) {
+                                         uint32_t see, f32x16& sc) {
     const int hh = lane >> 5;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sc[nb][i] = 0.f;
+    for (int i = 0; i < 16; ++i) sc[i] = 0.f;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
       const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lk + (lane & 31) * kKRow<D> + 16 * s + 8 * hh);
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-        sc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[nb][s], sc[nb], 0, 0, 0);
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], sc, 0, 0, 0);
     }
     if (flip) {
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[nb][i] = -sc[nb][i];
+      for (int i = 0; i < 16; ++i) sc[i] = -sc[i];
     }
     if (hides) {
+      const uint32_t w = see >> (4 * hh);
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const uint32_t w = see[nb] >> (4 * hh);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          sc[nb][i] = w & (1u << (8 * (i / 4) + i % 4)) ? sc[nb][i] : -__builtin_inff();
-      }
+      for (int i = 0; i < 16; ++i)
+        sc[i] = w & (1u << (8 * (i / 4) + i % 4)) ? sc[i] : -__builtin_inff();
     }
   }
 
@@ -272,41 +270,36 @@ struct TreeWave {
   // relative precision, and the rescale (a multiply per output, and per
   // weight in `held`, not yet in the outputs) leaves most tiles.
   template <bool HELD>
-  __device__ __forceinline__ void raise(float sl, const f32x16 (&sc)[NB], f32x16 (&held)[NB]) {
+  __device__ __forceinline__ void raise(float sl, const f32x16& sc, f32x16& held) {
+    float mx = sc[0];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      float mx = sc[nb][0];
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+    float x1, x2;
+    xor_pair<32>(mx, x1, x2);
+    const float mnew = fmaxf(m, fmaxf(x1, x2) * sl);
+    if (__ballot(mnew > m + kTreeSlack)) {
+      const float alpha = fast_exp2(m - mnew);
+      l *= alpha;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[nb][i]);
-      float x1, x2;
-      xor_pair<32>(mx, x1, x2);
-      const float mnew = fmaxf(m[nb], fmaxf(x1, x2) * sl);
-      if (__ballot(mnew > m[nb] + kTreeSlack)) {
-        const float alpha = fast_exp2(m[nb] - mnew);
-        l[nb] *= alpha;
+      for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c)
+        for (int i = 0; i < 16; ++i) o[c][i] *= alpha;
+      if constexpr (HELD) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[nb][c][i] *= alpha;
-        if constexpr (HELD) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) held[nb][i] *= alpha;
-        }
-        m[nb] = mnew;
+        for (int i = 0; i < 16; ++i) held[i] *= alpha;
       }
+      m = mnew;
     }
   }
 
   // Scores to weights, in place.
-  __device__ __forceinline__ void weights(float sl, float vs, f32x16 (&sc)[NB]) {
+  __device__ __forceinline__ void weights(float sl, float vs, f32x16& sc) {
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[nb][i] = fast_exp2(fmaf(sc[nb][i], sl, -m[nb]));
-        l[nb] += sc[nb][i];
-        if (vs != 1.f) sc[nb][i] *= vs;
-      }
+    for (int i = 0; i < 16; ++i) {
+      sc[i] = fast_exp2(fmaf(sc[i], sl, -m));
+      l += sc[i];
+      if (vs != 1.f) sc[i] *= vs;
+    }
   }
 
   // O += P V of 32 keys, 16 a step.  Half hh's eight operand slots are the keys
@@ -314,43 +307,38 @@ struct TreeWave {
   // For fp32 outputs the weights go in as three bf16 terms, which hold all their
   // 24 bits; for bf16 outputs rounded to one, off by half a step as the outputs
   // are.
-  __device__ __forceinline__ void values(int lane, const uint16_t* lv, const f32x16 (&p)[NB]) {
+  __device__ __forceinline__ void values(int lane, const uint16_t* lv, const f32x16& p) {
     constexpr int NE = F32 ? 3 : 1;
     const int hh = lane >> 5;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      bf16x8 pf[NB][NE];
+      bf16x8 pf[NE];
+      uint32_t w[NE][4];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        uint32_t w[NE][4];
+      for (int j = 0; j < 4; ++j) {
+        float u = p[8 * s + 2 * j], v = p[8 * s + 2 * j + 1];
+        if constexpr (F32) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float u = p[nb][8 * s + 2 * j], v = p[nb][8 * s + 2 * j + 1];
-          if constexpr (F32) {
-#pragma unroll
-            for (int e = 0; e < NE; ++e) {
-              w[e][j] = high_halves(u, v);
-              u -= __uint_as_float(__float_as_uint(u) & 0xffff0000u);
-              v -= __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-            }
-          } else {
-            w[0][j] = pack_bf16(u, v);
+          for (int e = 0; e < NE; ++e) {
+            w[e][j] = high_halves(u, v);
+            u -= __uint_as_float(__float_as_uint(u) & 0xffff0000u);
+            v -= __uint_as_float(__float_as_uint(v) & 0xffff0000u);
           }
+        } else {
+          w[0][j] = pack_bf16(u, v);
         }
-#pragma unroll
-        for (int e = 0; e < NE; ++e)
-          pf[nb][e] = __builtin_bit_cast(bf16x8, make_uint4(w[e][0], w[e][1], w[e][2], w[e][3]));
       }
+#pragma unroll
+      for (int e = 0; e < NE; ++e)
+        pf[e] = __builtin_bit_cast(bf16x8, make_uint4(w[e][0], w[e][1], w[e][2], w[e][3]));
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
         const uint2 va = vread(lv, lane, 16 * s + 4 * hh, c);
         const uint2 vb = vread(lv, lane, 16 * s + 8 + 4 * hh, c);
         const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(va.x, va.y, vb.x, vb.y));
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int e = 0; e < NE; ++e)
-            o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[nb][e], o[nb][c], 0, 0, 0);
+        for (int e = 0; e < NE; ++e)
+          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[e], o[c], 0, 0, 0);
       }
     }
   }
@@ -358,9 +346,8 @@ struct TreeWave {
   // A tile of 32 keys.  sl: score scale (positive), flip: of negated scores; vs:
   // scale of V; see: the keys each row sees, used where `hides`.
   __device__ __forceinline__ void tile(int lane, const uint16_t* lk, const uint16_t* lv, float sl,
-                                       bool flip, float vs, bool hides,
-                                       const uint32_t (&see)[NB]) {
-    f32x16 sc[NB];
+                                       bool flip, float vs, bool hides, uint32_t see) {
+    f32x16 sc;
     scores(lane, lk, flip, hides, see, sc);
     raise<false>(sl, sc, sc);
     weights(sl, vs, sc);
@@ -371,8 +358,8 @@ struct TreeWave {
   // weights are computed, and the first half's values while the second's are.
   __device__ __forceinline__ void tile2(int lane, const uint16_t* lk, const uint16_t* lv, float sl,
                                         bool flip, float vs, bool hides,
-                                        const uint32_t (&see)[2][NB]) {
-    f32x16 s0[NB], s1[NB];
+                                        const uint32_t (&see)[2]) {
+    f32x16 s0, s1;
     scores(lane, lk, flip, hides, see[0], s0);
     raise<false>(sl, s0, s0);
     scores(lane, lk + 32 * kKRow<D>, flip, hides, see[1], s1);
@@ -383,26 +370,35 @@ struct TreeWave {
     values(lane, lv + 32 * kVRow<D>, s1);
   }
 
-  // Adds the infinities and NaN of V row v to the rows that see its key: as
-  // products of 1 and the largest bf16 values, whose sum overflows where it is
-  // added, and of 0 where the key is hidden.  A NaN is both infinities.
-  __device__ __forceinline__ void add_nonfinite(int lane, const uint16_t* v,
-                                                const bool (&mine)[NB]) {
+  // Adds the infinities and NaN of V row v (fp8 where CODES) to the rows that see
+  // its key: as products of 1 and the largest bf16 values, whose sum overflows, and of
+  // 0 where the key is hidden.  A NaN is both infinities, one after the other.  (Summed
+  // up by themselves: an infinity stays one where the matrix core adds these to it.)
+  template <bool CODES>
+  __device__ __forceinline__ void add_nonfinite(int lane, const uint8_t* v, bool mine) {
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
       const int place = 4 * c + ((lane & 31) >> 3);  // (chunk_at of a lane's place)
       const int at = FP8 ? (place < D / 16 ? 2 * place : 2 * (place - D / 16) + 1) : place;
-      const uint32_t x = v[8 * at + (lane & 7)], size = x & 0x7fffu;
+      const int col = 8 * at + (lane & 7);
+      const uint32_t x = CODES ? ((v[col] & 0x7fu) == 0x7fu ? 0x7fc0u : 0u)
+                               : reinterpret_cast<const uint16_t*>(v)[col];
+      const uint32_t size = x & 0x7fffu;
       const uint32_t up = x == 0x7f80u || size > 0x7f80u ? 0x7f7f7f7fu : 0u;
       const uint32_t down = x == 0xff80u || size > 0x7f80u ? 0xff7fff7fu : 0u;
+      const uint32_t one = mine ? 0x3f803f80u : 0u;
+      const bf16x8 p = __builtin_bit_cast(bf16x8, make_uint4(one, one, one, one));
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const uint32_t one = mine[nb] ? 0x3f803f80u : 0u;
-        const bf16x8 p = __builtin_bit_cast(bf16x8, make_uint4(one, one, one, one));
-        o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_bit_cast(bf16x8, make_uint4(up, up, up, up)), p, o[nb][c], 0, 0, 0);
-        o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_bit_cast(bf16x8, make_uint4(down, down, down, down)), p, o[nb][c], 0, 0, 0);
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t big = e ? down : up;
+        f32x16 t;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t[i] = 0.f;
+        t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, make_uint4(big, big, big, big)), p, t, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[c][i] += t[i];
+        __builtin_amdgcn_sched_barrier(0);  // one t at a time
       }
     }
   }
@@ -434,7 +430,7 @@ __device__ __forceinline__ CacheScale cache_scale(const TreeArgs& a, int pair) {
 // returns the rows that had any: bit i * (512 / D) + g for row g of pass i.  (The
 // rare second pass goes over LDS: on the registers it cost 20 of them.)
 template <int D, int N>
-__device__ __forceinline__ uint32_t clean_rows(const uint4 (&x)[N], uint16_t* v, int step) {
+__device__ __forceinline__ uint32_t clean_rows(const uint4* x, uint16_t* v, int step) {
   constexpr int CPR = D / 8, RPW = 64 / CPR;
   uint32_t any = 0;
 #pragma unroll
@@ -452,6 +448,35 @@ __device__ __forceinline__ uint32_t clean_rows(const uint4 (&x)[N], uint16_t* v,
 #pragma unroll
     for (int g = 0; g < RPW; ++g)
       rows |= (who >> (g * CPR) & ((1ull << CPR) - 1)) ? 1u << (i * RPW + g) : 0u;
+  }
+  return rows;
+}
+
+// The same of fp8 rows, in registers: x: N chunks of 16 elements, D / 16 lanes to a
+// row; bit i * (1024 / D) + g of the result for row g of pass i.
+template <int D, int N>
+__device__ __forceinline__ uint32_t clean_codes(uint4* x) {
+  constexpr int CPR = D / 16, RPW = 64 / CPR;
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    any |= nan_bytes(x[i].x) | nan_bytes(x[i].y) | nan_bytes(x[i].z) | nan_bytes(x[i].w);
+  if (!__ballot(any != 0)) return 0;
+  uint32_t rows = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w}, bad = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t b = nan_bytes(w[e]);
+      bad |= b;
+      w[e] &= ~((b >> 7) * 0xffu);
+    }
+    x[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    const uint64_t who = __ballot(bad != 0);
+#pragma unroll
+    for (int g = 0; g < RPW; ++g)
+      rows |= (who >> (g * CPR)) & ((1ull << CPR) - 1) ? 1u << (i * RPW + g) : 0u;
   }
   return rows;
 }
@@ -474,12 +499,12 @@ __device__ __forceinline__ int tree_cut(int tiles, int part, int parts) {
 
 constexpr int kTileKeys = 64;   // keys of a tile
 
-// A workgroup of four waves takes 128 NB query rows (node, query head of the KV
+// A workgroup of four waves takes 128 query rows (node, query head of the KV
 // head's group) of one request and KV head, and a share of the keys.  Tiles of
 // 64 keys go through LDS for all four waves, two buffers in turn.
-template <bool FP8, int D, bool F32, int NB>
-__global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(TreeArgs a) {
-  constexpr int kTileRows = 128 * NB;
+template <bool FP8, int D, bool F32>
+__global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
+  constexpr int kTileRows = 128;
   constexpr int CPR = D / 8;           // 16-byte chunks of a bf16 row
   constexpr int NP = CPR * kTileKeys / 256;
   constexpr int RPP = 256 / CPR;       // rows per pass of the workgroup
@@ -506,18 +531,13 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int row0 = r0 + 32 * NB * wave + (lane & 31);
-  const bool wave_on = r0 + 32 * NB * wave < rows;
+  const int row = r0 + 32 * wave + (lane & 31);
+  const bool wave_on = r0 + 32 * wave < rows;
   const CacheScale cs = cache_scale<FP8>(a, pair);
-  TreeRow my[NB];
-  TreeWave<D, F32, NB, FP8> w;
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    const int row = min(row0 + 32 * nb, rows - 1);
-    my[nb] = tree_row(a, rq, ks, b, row);
-    w.start(a, lane, nb,
-            a.q + b * a.qsb + my[nb].node * a.qsn + (h * a.G + row % a.G) * a.qsh);
-  }
+  const TreeRow my = tree_row(a, rq, ks, b, min(row, rows - 1));
+  TreeWave<D, F32, FP8> w;
+  w.start(a, lane,
+          a.q + b * a.qsb + my.node * a.qsn + (h * a.G + min(row, rows - 1) % a.G) * a.qsh);
 
   const uint8_t* kc = a.k + tree_cache_base(a, b, h, FP8 ? 1 : 2);
   const uint8_t* vc = a.v + tree_cache_base(a, b, h, FP8 ? 1 : 2);
@@ -535,7 +555,7 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
     const int e0 = (t - (t < t_old ? 0 : t_old)) * kTileKeys + tid / CPR;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int64_t at = list.row(min(e0 + i * RPP, list.n - 1)) * step + (tid % CPR) * 16;
+      const int64_t at = list.near(e0 + i * RPP) * step + (tid % CPR) * 16;
       rk[i] = load16(k + at);
       rv[i] = load16(v + at);
     }
@@ -554,20 +574,22 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
     }
     uint32_t bad = 0;
     if (hides(t))
-      bad = clean_rows<D>(rv, lv[buf] + (tid / CPR) * kVRow<D> + c * 8, RPP * kVRow<D>);
+      bad = clean_rows<D, NP>(rv, lv[buf] + (tid / CPR) * kVRow<D> + c * 8, RPP * kVRow<D>);
     if (lane == 0) lbad[buf][wave] = bad;
   };
   // The same of an fp8 cache: sixteen elements a load.
   auto load8 = [&](int t) {
 #pragma unroll
     for (int i = 0; i < NP8; ++i) {
-      const int e = min(t * kTileKeys + i * RP8 + tid / CP8, ks.cached.n - 1);
-      const int64_t at = ks.cached.row(e) * a.sr + (tid % CP8) * 16;
+      const int64_t at = ks.cached.near(t * kTileKeys + i * RP8 + tid / CP8) * a.sr + (tid % CP8) * 16;
       rk[i] = load16(kc + at);
       rv[i] = load16(vc + at);
     }
   };
-  auto put8 = [&](int buf) {
+  auto put8 = [&](int t, int buf) {
+    uint32_t bad = 0;
+    if (hides(t)) bad = clean_codes<D, NP8>(rv);
+    if (lane == 0) lbad[buf][wave] = bad;
 #pragma unroll
     for (int i = 0; i < NP8; ++i) {
       const int r = i * RP8 + tid / CP8, c = tid % CP8;
@@ -580,29 +602,25 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
       *reinterpret_cast<uint4*>(lv[buf] + r * kVRow<D> + c * 8 + D / 2) = hi;
     }
   };
-  auto see_of = [&](int t, uint32_t (&see)[2][NB]) {
+  auto see_of = [&](int t, uint32_t (&see)[2]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-        see[i][nb] = t < t_old
-                         ? see_cached(ks, my[nb], t * kTileKeys + 32 * i)
-                         : see_fresh(a, ks, tt, my[nb], b, (t - t_old) * kTileKeys + 32 * i);
+      see[i] = t < t_old ? see_cached(ks, my, t * kTileKeys + 32 * i)
+                         : see_fresh(a, ks, tt, my, b, (t - t_old) * kTileKeys + 32 * i);
   };
-  auto add_hidden = [&](int t, int buf, const uint32_t (&see)[2][NB]) {
-    constexpr int RPW = 64 / CPR;  // rows of a wave's pass
+  auto add_hidden = [&](int t, int buf, const uint32_t (&see)[2], auto codes) {
+    constexpr int per = codes.value ? RP8 : RPP;  // rows of a pass of all waves, of one wave
+    constexpr int own = per / 4;
     const bool old = t < t_old;
 #pragma unroll 1
     for (int i = 0; i < 4; ++i)
 #pragma unroll 1
       for (uint32_t bad = lbad[buf][i]; bad; bad &= bad - 1) {
-        const int at = __builtin_ctz(bad), e = at / RPW * RPP + i * RPW + at % RPW;
-        bool mine[NB];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) mine[nb] = (see[e >> 5][nb] >> (e & 31)) & 1u;
-        const uint8_t* v = old ? vc + ks.cached.row(t * kTileKeys + e) * a.sr
-                               : vn + ks.fresh.row((t - t_old) * kTileKeys + e) * a.nsn * 2;
-        w.add_nonfinite(lane, reinterpret_cast<const uint16_t*>(v), mine);
+        const int at = __builtin_ctz(bad), e = at / own * per + i * own + at % own;
+        const bool mine = (see[e >> 5] >> (e & 31)) & 1u;
+        const uint8_t* v = old ? vc + ks.cached.near(t * kTileKeys + e) * a.sr
+                               : vn + ks.fresh.near((t - t_old) * kTileKeys + e) * a.nsn * 2;
+        w.template add_nonfinite<codes.value>(lane, v, mine);
       }
   };
 
@@ -613,19 +631,20 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
     const int end = min(t1, t_old);
     if (t < end) {
       load8(t);
-      put8(0);
+      put8(t, 0);
       if (t + 1 < end) load8(t + 1);
       __syncthreads();
     }
     for (; t < end; ++t, buf ^= 1) {
-      if (t + 1 < end) put8(buf ^ 1);
+      if (t + 1 < end) put8(t + 1, buf ^ 1);
       if (t + 2 < end) load8(t + 2);
       asm volatile("" ::: "memory");
       if (wave_on) {
-        uint32_t see[2][NB] = {};
+        uint32_t see[2] = {};
         const bool hide = hides(t);
         if (hide) see_of(t, see);
         w.tile2(lane, lk[buf], lv[buf], cs.sl, cs.flip, cs.vs, hide, see);
+        if (hide) add_hidden(t, buf, see, std::true_type());
       }
       __syncthreads();
     }
@@ -641,46 +660,42 @@ __global__ __launch_bounds__(256, NB * D > 128 ? 1 : 2) void tree_tile_kernel(Tr
     if (t + 2 < t1) load(t + 2);
     asm volatile("" ::: "memory");  // the loads stay ahead of the tile
     if (wave_on) {
-      uint32_t see[2][NB] = {};
+      uint32_t see[2] = {};
       const bool hide = hides(t);
       if (hide) see_of(t, see);
       w.tile2(lane, lk[buf], lv[buf], a.scale_log2, false, 1.f, hide, see);
-      if (hide) add_hidden(t, buf, see);
+      if (hide) add_hidden(t, buf, see, std::false_type());
     }
     __syncthreads();
   }
 
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    const int row = row0 + 32 * nb;
-    float l1, l2;
-    xor_pair<32>(w.l[nb], l1, l2);
-    const float l = l1 + l2;
-    if (row >= rows) continue;
-    const int hh = lane >> 5;
-    if (nsp == 1) {
-      const float inv = 1.f / l;
-      const int64_t out =
-          ((static_cast<int64_t>(b) * a.N + my[nb].node) * a.Hq + h * a.G + row % a.G) * D;
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4)
-          store4<F32>(a.out, out + out_col<D, FP8>(c, i / 4, hh), w.o[nb][c][i] * inv,
-                      w.o[nb][c][i + 1] * inv, w.o[nb][c][i + 2] * inv, w.o[nb][c][i + 3] * inv);
-      continue;
-    }
-    float* part = a.part + ((static_cast<int64_t>(pair) * a.row_tiles + qt) * a.splits + sp) *
-                               kTileRows * kPartRow<D> +
-                  (row - r0) * kPartRow<D>;
+  float l1, l2;
+  xor_pair<32>(w.l, l1, l2);
+  const float l = l1 + l2;
+  if (row >= rows) return;
+  const int hh = lane >> 5;
+  if (nsp == 1) {
+    const float inv = 1.f / l;
+    const int64_t out =
+        ((static_cast<int64_t>(b) * a.N + my.node) * a.Hq + h * a.G + row % a.G) * D;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
       for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<float4*>(part + out_col<D, FP8>(c, i / 4, hh)) = make_float4(
-            w.o[nb][c][i], w.o[nb][c][i + 1], w.o[nb][c][i + 2], w.o[nb][c][i + 3]);
-    if (lane < 32) *reinterpret_cast<float2*>(part + D) = make_float2(w.m[nb], l);
+        store4<F32>(a.out, out + out_col<D, FP8>(c, i / 4, hh), w.o[c][i] * inv,
+                    w.o[c][i + 1] * inv, w.o[c][i + 2] * inv, w.o[c][i + 3] * inv);
+    return;
   }
+  float* part = a.part + ((static_cast<int64_t>(pair) * a.row_tiles + qt) * a.splits + sp) *
+                             kTileRows * kPartRow<D> +
+                (row - r0) * kPartRow<D>;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      *reinterpret_cast<float4*>(part + out_col<D, FP8>(c, i / 4, hh)) = make_float4(
+          w.o[c][i], w.o[c][i + 1], w.o[c][i + 2], w.o[c][i + 3]);
+  if (lane < 32) *reinterpret_cast<float2*>(part + D) = make_float2(w.m, l);
 }
 
 // ---- few query rows --------------------------------------------------------------
@@ -690,15 +705,15 @@ constexpr int kStreamKeys = 32;  // keys of a wave's tile
 template <int D>
 constexpr uint32_t kStreamLds = kStreamKeys * (kKRow<D> + kVRow<D>) * 2;  // a wave's K and V tile
 
-// At most 32 NB query rows per workgroup: bound by the cache's bytes.  Every wave
+// At most 32 query rows per workgroup: bound by the cache's bytes.  Every wave
 // streams tiles of 32 keys of its own for all rows, through registers (the next
 // tiles are on their way while one is computed) and an LDS region of its own, so
 // the waves of a workgroup wait for each other only to join their results at
 // the end.  (K straight into the matrix operand, a row per lane, halves the LDS
 // traffic but reads 32 bytes of a row at a time: 67 us against 62 for 1024 pairs of
 // 290 to 800 keys, d = 128.)
-template <bool FP8, int D, bool F32, int NB, int NW>
-__global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(TreeArgs a) {
+template <bool FP8, int D, bool F32, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void tree_stream_kernel(TreeArgs a) {
   constexpr int CPR = D / 8, RPP = 64 / CPR, NP = kStreamKeys / RPP;  // bf16 rows of V
   constexpr int C = FP8 ? D / 16 : CPR, R = 64 / C, N = kStreamKeys / R;  // the cache's
   constexpr int PF = N > 4 ? 1 : 2;  // tiles in flight ahead of the one at hand
@@ -710,9 +725,9 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
   const int pair = item.pair, b = pair / a.Hkv, h = pair % a.Hkv;
   const int sp = item.sub / a.row_tiles, qt = item.sub % a.row_tiles;
   const TreeReq rq = tree_request(a.base, a.count, b, a.N, a.Lp, a.Ldec);
-  const int rows = rq.n * a.G, r0 = qt * 32 * NB;
+  const int rows = rq.n * a.G, r0 = qt * 32;
   if (r0 >= rows) return;
-  TreeTile tt{r0 / a.G, (min(r0 + 32 * NB, rows) - 1) / a.G, 0, a.S - rq.base};
+  TreeTile tt{r0 / a.G, (min(r0 + 32, rows) - 1) / a.G, 0, a.S - rq.base};
   tt.deepest = a.depth ? a.max_depth[b] : tt.n1;
   const TreeKeys ks = tree_keys(a, rq, tt.n0, tt.n1);
   const int t_old = (ks.cached.n + kStreamKeys - 1) / kStreamKeys;
@@ -742,8 +757,7 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
     const uint8_t* v = old ? vc : vn;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int e = min(e0 + i * RPP + lane / CPR, list.n - 1);
-      const int64_t at = list.row(e) * step + (lane % CPR) * 16;
+      const int64_t at = list.near(e0 + i * RPP + lane / CPR) * step + (lane % CPR) * 16;
       rk[set + i] = load_stream16(k + at);
       rv[set + i] = load_stream16(v + at);
     }
@@ -752,8 +766,7 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
   auto load8 = [&](int t, int set) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int e = min(t * kStreamKeys + i * R + lane / C, ks.cached.n - 1);
-      const int64_t at = ks.cached.row(e) * a.sr + (lane % C) * 16;
+      const int64_t at = ks.cached.near(t * kStreamKeys + i * R + lane / C) * a.sr + (lane % C) * 16;
       rk[set + i] = load_stream16(kc + at);
       rv[set + i] = load_stream16(vc + at);
     }
@@ -768,16 +781,20 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
     }
   }
 
-  TreeRow my[NB];
-  TreeWave<D, F32, NB, FP8> w;
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    const int row = min(r0 + 32 * nb + (lane & 31), rows - 1);
-    my[nb] = tree_row(a, rq, ks, b, row);
-    w.start(a, lane, nb,
-            a.q + b * a.qsb + my[nb].node * a.qsn + (h * a.G + row % a.G) * a.qsh);
-  }
+  const int lane_row = min(r0 + (lane & 31), rows - 1);
+  const TreeRow my = tree_row(a, rq, ks, b, lane_row);
+  TreeWave<D, F32, FP8> w;
+  w.start(a, lane, a.q + b * a.qsb + my.node * a.qsn + (h * a.G + lane_row % a.G) * a.qsh);
   const CacheScale cs = cache_scale<FP8>(a, pair);
+
+  // V rows of `bad`, from their place in memory, to the rows that see them.
+  auto add_hidden = [&](uint32_t bad, uint32_t see, auto codes, auto&& row_at) {
+#pragma unroll 1
+    for (; bad; bad &= bad - 1) {
+      const int e = __builtin_ctz(bad);
+      w.template add_nonfinite<codes.value>(lane, row_at(e), (see >> e) & 1u);
+    }
+  };
 
   // A tile of bf16 rows in registers [set, set + NP); `next` fills them again.
   auto tile = [&](int t, int set, auto&& next) {
@@ -785,35 +802,24 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
     const int e0 = (t - (t < t_old ? 0 : t_old)) * kStreamKeys;
     const bool hide = old ? hides_cached(a, rq, ks, tt, e0, kStreamKeys)
                           : hides_fresh(a, ks, tt, e0, kStreamKeys);
-    uint32_t see[NB] = {};
-    if (hide)
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-        see[nb] = old ? see_cached(ks, my[nb], e0) : see_fresh(a, ks, tt, my[nb], b, e0);
+    uint32_t see = 0;
+    if (hide) see = old ? see_cached(ks, my, e0) : see_fresh(a, ks, tt, my, b, e0);
     const int c = place_of<D, FP8>(lane % CPR);
-    uint4 v[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int r = i * RPP + lane / CPR;
-      v[i] = rv[set + i];
       *reinterpret_cast<uint4*>(lk + r * kKRow<D> + c * 8) = rk[set + i];
-      *reinterpret_cast<uint4*>(lv + r * kVRow<D> + c * 8) = v[i];
+      *reinterpret_cast<uint4*>(lv + r * kVRow<D> + c * 8) = rv[set + i];
     }
     uint32_t bad = 0;
-    if (hide) bad = clean_rows<D>(v, lv + (lane / CPR) * kVRow<D> + c * 8, RPP * kVRow<D>);
+    if (hide)
+      bad = clean_rows<D, NP>(rv + set, lv + (lane / CPR) * kVRow<D> + c * 8, RPP * kVRow<D>);
     next();
     fence_wave();
     w.tile(lane, lk, lv, a.scale_log2, false, 1.f, hide, see);
-#pragma unroll 1
-    for (; bad; bad &= bad - 1) {
-      const int e = __builtin_ctz(bad);
-      bool mine[NB];
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) mine[nb] = (see[nb] >> e) & 1u;
-      const uint8_t* x =
-          old ? vc + ks.cached.row(e0 + e) * a.sr : vn + ks.fresh.row(e0 + e) * a.nsn * 2;
-      w.add_nonfinite(lane, reinterpret_cast<const uint16_t*>(x), mine);
-    }
+    add_hidden(bad, see, std::false_type(), [&](int e) {
+      return old ? vc + ks.cached.near(e0 + e) * a.sr : vn + ks.fresh.near(e0 + e) * a.nsn * 2;
+    });
     fence_wave();
   };
 
@@ -824,10 +830,8 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
         if (t + j >= end8) break;
         const int e0 = (t + j) * kStreamKeys;
         const bool hide = hides_cached(a, rq, ks, tt, e0, kStreamKeys);
-        uint32_t see[NB] = {};
-        if (hide)
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) see[nb] = see_cached(ks, my[nb], e0);
+        const uint32_t see = hide ? see_cached(ks, my, e0) : 0u;
+        const uint32_t bad = hide ? clean_codes<D, N>(rv + j * N) : 0u;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const int r = i * R + lane / C, c = lane % C;
@@ -842,6 +846,8 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
         if (t + j + PF < end8) load8(t + j + PF, j * N);
         fence_wave();
         w.tile(lane, lk, lv, cs.sl, cs.flip, cs.vs, hide, see);
+        add_hidden(bad, see, std::true_type(),
+                   [&](int e) { return vc + ks.cached.near(e0 + e) * a.sr; });
         fence_wave();
       }
     }
@@ -861,66 +867,61 @@ __global__ __launch_bounds__(64 * NW, NB == 1 ? 2 : 1) void tree_stream_kernel(T
     }
   }
 
-  // Join the waves' results, a block of rows at a time: every wave scales its own
-  // to the common maximum and leaves them in its LDS region, 32 columns of a row
-  // per step, then the workgroup's threads add them up.
+  // Join the waves' results: every wave scales its own to the common maximum and
+  // leaves them in its LDS region, then the workgroup's threads add them up.
   const bool split = nsp > 1;
   float* part = a.part + ((static_cast<int64_t>(pair) * a.row_tiles + qt) * a.splits + sp) *
-                             (32 * NB) * kPartRow<D>;
+                             32 * kPartRow<D>;
+  float l1, l2;
+  xor_pair<32>(w.l, l1, l2);
+  if (lane < 32) {
+    lm[wave][lane] = w.m;
+    ll[wave][lane] = l1 + l2;
+  }
+  __syncthreads();
+  float M = kTreeMin;
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    float l1, l2;
-    xor_pair<32>(w.l[nb], l1, l2);
-    if (lane < 32) {
-      lm[wave][lane] = w.m[nb];
-      ll[wave][lane] = l1 + l2;
+  for (int i = 0; i < NW; ++i) M = fmaxf(M, lm[i][lane & 31]);
+  const float mine = fast_exp2(w.m - M);
+  float* red = reinterpret_cast<float*>(lk);  // [32 rows][D], groups of 4 columns swizzled
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int g = out_col<D, FP8>(c, i / 4, lane >> 5) / 4, r = lane & 31;
+      *reinterpret_cast<float4*>(red + r * D + ((g ^ (r & 15)) * 4)) =
+          make_float4(w.o[c][i] * mine, w.o[c][i + 1] * mine, w.o[c][i + 2] * mine,
+                      w.o[c][i + 3] * mine);
     }
-    __syncthreads();
-    float M = kTreeMin;
+  __syncthreads();
+  for (int at = threadIdx.x; at < 32 * (D / 4); at += 64 * NW) {
+    const int r = at / (D / 4), g = at % (D / 4), row = r0 + r;
+    if (row >= rows) break;
+    float mr = kTreeMin, lr = 0.f;
 #pragma unroll
-    for (int i = 0; i < NW; ++i) M = fmaxf(M, lm[i][lane & 31]);
-    const float mine = fast_exp2(w.m[nb] - M);
-    float* red = reinterpret_cast<float*>(lk);  // [32 rows][D], groups of 4 columns swizzled
+    for (int i = 0; i < NW; ++i) mr = fmaxf(mr, lm[i][r]);
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c)
+    for (int i = 0; i < NW; ++i) lr = fmaf(ll[i][r], fast_exp2(lm[i][r] - mr), lr);
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        const int g = out_col<D, FP8>(c, i / 4, lane >> 5) / 4, r = lane & 31;
-        *reinterpret_cast<float4*>(red + r * D + ((g ^ (r & 15)) * 4)) =
-            make_float4(w.o[nb][c][i] * mine, w.o[nb][c][i + 1] * mine, w.o[nb][c][i + 2] * mine,
-                        w.o[nb][c][i + 3] * mine);
-      }
-    __syncthreads();
-    for (int at = threadIdx.x; at < 32 * (D / 4); at += 64 * NW) {
-      const int r = at / (D / 4), g = at % (D / 4), row = r0 + 32 * nb + r;
-      if (row >= rows) break;
-      float mr = kTreeMin, lr = 0.f;
-#pragma unroll
-      for (int i = 0; i < NW; ++i) mr = fmaxf(mr, lm[i][r]);
-#pragma unroll
-      for (int i = 0; i < NW; ++i) lr = fmaf(ll[i][r], fast_exp2(lm[i][r] - mr), lr);
-      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int i = 0; i < NW; ++i) {
-        const float4 x = *reinterpret_cast<const float4*>(
-            reinterpret_cast<const float*>(lds + i * (kStreamLds<D> / 2)) + r * D +
-            ((g ^ (r & 15)) * 4));
-        s.x += x.x;
-        s.y += x.y;
-        s.z += x.z;
-        s.w += x.w;
-      }
-      if (split) {
-        float* p = part + (row - r0) * kPartRow<D>;
-        *reinterpret_cast<float4*>(p + 4 * g) = s;
-        if (g == 0) *reinterpret_cast<float2*>(p + D) = make_float2(mr, lr);
-      } else {
-        const float inv = 1.f / lr;
-        const int64_t out = (static_cast<int64_t>(b) * a.N + row / a.G) * a.Hq + h * a.G + row % a.G;
-        store4<F32>(a.out, out * D + 4 * g, s.x * inv, s.y * inv, s.z * inv, s.w * inv);
-      }
+    for (int i = 0; i < NW; ++i) {
+      const float4 x = *reinterpret_cast<const float4*>(
+          reinterpret_cast<const float*>(lds + i * (kStreamLds<D> / 2)) + r * D +
+          ((g ^ (r & 15)) * 4));
+      s.x += x.x;
+      s.y += x.y;
+      s.z += x.z;
+      s.w += x.w;
     }
-    if (nb + 1 < NB) __syncthreads();
+    if (split) {
+      float* p = part + (row - r0) * kPartRow<D>;
+      *reinterpret_cast<float4*>(p + 4 * g) = s;
+      if (g == 0) *reinterpret_cast<float2*>(p + D) = make_float2(mr, lr);
+    } else {
+      const float inv = 1.f / lr;
+      const int64_t out = (static_cast<int64_t>(b) * a.N + row / a.G) * a.Hq + h * a.G + row % a.G;
+      store4<F32>(a.out, out * D + 4 * g, s.x * inv, s.y * inv, s.z * inv, s.w * inv);
+    }
   }
 }
 
@@ -993,9 +994,9 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a, int tile_
   }
 }
 
-template <bool FP8, int D, bool F32, int NB, int NW>
+template <bool FP8, int D, bool F32, int NW>
 hipError_t launch_stream(const TreeLaunch& l, const TreeArgs& a, hipStream_t st) {
-  tree_stream_kernel<FP8, D, F32, NB, NW>
+  tree_stream_kernel<FP8, D, F32, NW>
       <<<dim3(tree_grid(static_cast<int64_t>(a.B) * a.Hkv, a.row_tiles * a.splits)), dim3(64 * NW),
          0, st>>>(a);
   return hipGetLastError();
@@ -1006,11 +1007,11 @@ hipError_t launch_one(const TreeLaunch& l, const TreeArgs& a, hipStream_t st) {
   hipError_t e;
   const dim3 grid(tree_grid(static_cast<int64_t>(a.B) * a.Hkv, a.row_tiles * a.splits));
   if (l.rows == 128) {
-    tree_tile_kernel<FP8, D, F32, 1><<<grid, dim3(256), 0, st>>>(a);
+    tree_tile_kernel<FP8, D, F32><<<grid, dim3(256), 0, st>>>(a);
     e = hipGetLastError();
   } else {
-    e = l.waves == 8 ? launch_stream<FP8, D, F32, 1, 8>(l, a, st)
-                     : launch_stream<FP8, D, F32, 1, 4>(l, a, st);
+    e = l.waves == 8 ? launch_stream<FP8, D, F32, 8>(l, a, st)
+                     : launch_stream<FP8, D, F32, 4>(l, a, st);
   }
   if (e != hipSuccess || l.splits == 1) return e;
   const int64_t waves = static_cast<int64_t>(a.B) * a.Hkv * a.row_tiles * l.rows;

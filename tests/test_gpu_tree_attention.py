@@ -254,6 +254,79 @@ def test_hidden_values_stay_hidden(kind, tree, heads, out):
                     assert not a[b, i][:, 5:9].isfinite().any()
 
 
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+@pytest.mark.parametrize("nodes,heads", [(7, (4, 4)), (40, (8, 2))])
+def test_nonfinite_value_in_the_last_row(kv, nodes, heads):
+    """The last row that a cache has, in a tile with no keys after it: seen by all
+    nodes, as the last of the new rows is by one."""
+    for counts in (None, [nodes - 2, nodes]):
+        case = dict(batch=2, nodes=nodes, heads=heads, tree=False, kv=kv, bases=[99, 99],
+                    counts=counts, seed=4)
+        want = Problem(**case)
+        want.run()
+        got = Problem(**case)
+        if kv == "bf16":
+            got.v[:, :, -1, 9] = math.inf
+        else:
+            got.v.view(torch.uint8)[:, :, -1, 9] = 0x7F
+        for b in range(2):
+            got.vn[b, (counts or [nodes] * 2)[b] - 1, :, 4] = -math.inf
+        got.run()
+        torch.cuda.synchronize()
+        a, w = got.out.cpu(), want.out.cpu()
+        for b in range(2):
+            n = (counts or [nodes] * 2)[b]
+            clean = [c for c in range(64) if c not in (4, 9)]
+            assert torch.equal(a[b, :n][..., clean], w[b, :n][..., clean])
+            if kv == "bf16":
+                assert (a[b, :n, :, 9] == math.inf).all()
+            else:
+                assert a[b, :n, :, 9].isnan().all()
+            assert torch.equal(a[b, :n - 1, :, 4], w[b, :n - 1, :, 4])
+            assert (a[b, n - 1, :, 4] == -math.inf).all()
+            assert torch.equal(a[b, n:], w[b, n:])
+
+
+@pytest.mark.parametrize("nodes,heads,d", [(6, (4, 4), 64), (13, (8, 1), 128), (30, (8, 4), 128),
+                                           (50, (8, 2), 64)])
+@pytest.mark.parametrize("ring", [0, 20])
+def test_hidden_fp8_codes_stay_hidden(nodes, heads, d, ring):
+    """NaN codes of cached positions that some nodes' windows have left: those get
+    the output that a zero in its place gives them, the others NaN."""
+    case = dict(batch=2, nodes=nodes, heads=heads, d=d, tree=False, kv="fp8", mode="window",
+                n_att=20, sinks=4, ring=ring, bases=[40, 61], grid=(11, 11), seed=8)
+    want, got = Problem(**case), Problem(**case)
+    for b in range(2):
+        for back in (1, 4, 9, 16):  # position base - back: node i sees it where i + back < 16
+            row = got.row_of(got.bases[b] - back)
+            got.v.view(torch.uint8)[b, :, row, back + 30] = 0xFF if back & 1 else 0x7F
+            want.v.view(torch.uint8)[b, :, row, back + 30] = 0
+    want.run()
+    got.run()
+    torch.cuda.synchronize()
+    a, w = got.out.cpu(), want.out.cpu()
+    for i in range(nodes):
+        for c in range(d):
+            if c - 30 in (1, 4, 9, 16) and i + c - 30 < 16:
+                assert a[:, i, :, c].isnan().all(), (i, c)
+            else:
+                assert torch.equal(a[:, i, :, c], w[:, i, :, c]), (i, c)
+
+
+@pytest.mark.parametrize("nodes,heads", [(5, (4, 4)), (40, (8, 2))])
+def test_visible_nan_is_a_nan(nodes, heads):
+    """Also beside hidden keys, and next to infinities of one sign."""
+    pr = Problem(nodes=nodes, heads=heads, tree=False, seed=2)
+    pr.vn[:, 2, :, 7] = math.nan
+    pr.vn[:, 3, :, 7] = math.inf
+    pr.vn[:, 1, :, 8] = -math.inf
+    pr.vn[:, 2, :, 8] = math.inf
+    out = pr.run().cpu()
+    assert out[:, 2:, :, 7].isnan().all() and out[:, 2:, :, 8].isnan().all()
+    assert out[:, :2, :, 7].isfinite().all() and (out[:, 1, :, 8] == -math.inf).all()
+    assert out[:, :, :, [c for c in range(64) if c not in (7, 8)]].isfinite().all()
+
+
 def test_visible_infinity_is_an_infinity():
     """An infinite V element of a key that is seen gives that infinity, also in
     a tile with hidden keys."""
