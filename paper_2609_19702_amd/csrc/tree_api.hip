@@ -68,8 +68,13 @@ dsa_status tree_derive(const dsa_params* p, const dsa_shape* s, int nodes, Deriv
 // time (tree_stream_kernel); more go through LDS for 128 at a time
 // (tree_tile_kernel; 64 rows of d = 128 over fp8, 32 requests: 70 us a layer
 // streamed, 98 through it).  The keys of a row tile are split where the row tiles
-// alone would leave CUs without a workgroup, but not finer than four tiles of
-// keys per wave: a split costs a second kernel and a row of partial results.
+// alone would leave CUs without a workgroup (4096 keys of 8 KV heads, d = 128, 8
+// nodes of one request: 16 us with splits, 45 without; 256 nodes of 32 heads: 55
+// and 150), but not finer than two tiles of keys per streaming wave (four: 19 us, one:
+// 17) or four per workgroup otherwise (8100 keys of one head, 16 nodes: 26 us,
+// two: 31), and not at all up to four per wave (32 heads, d = 128, 848 keys, a layer:
+// 14.9 us in two splits, 13.9 in one): a split costs a row of partial results and the
+// wait for them.
 TreeLaunch tree_launch(const Derived& d, int nodes) {
   TreeLaunch l{};
   const int64_t rows = static_cast<int64_t>(nodes) * d.G;
@@ -82,10 +87,12 @@ TreeLaunch tree_launch(const Derived& d, int nodes) {
                        int64_t{nodes};
   const int64_t tiles = (keys + l.keys - 1) / l.keys + 2;
   const int64_t wgs = pairs * l.row_tiles;
-  // Twice the waves on the keys where at most one workgroup per CU has work.
+  // Twice the waves on the keys where at most one workgroup per CU has work (32
+  // heads, d = 128, 848 keys, 16 nodes: 13.9 us a layer with eight waves, 14.5 with four);
+  // with more, what a CU holds at a time decides (32 such requests: 71 and 60).
   l.waves = stream && wgs <= 256 ? 8 : 4;
   const int64_t want = std::max<int64_t>(1, 256 / wgs);
-  const int64_t least = 4 * (stream ? l.waves : 1);
+  const int64_t least = !stream ? 4 : tiles <= 4 * l.waves ? tiles : 2 * l.waves;
   l.split_tiles = static_cast<int>(std::max<int64_t>(least, (tiles + want - 1) / want));
   l.splits = static_cast<int>((tiles + l.split_tiles - 1) / l.split_tiles);
   l.workgroups = wgs * l.splits;
