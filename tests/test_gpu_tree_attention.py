@@ -254,6 +254,20 @@ def test_hidden_values_stay_hidden(kind, tree, heads, out):
                     assert not a[b, i][:, 5:9].isfinite().any()
 
 
+@pytest.mark.parametrize("batch", [2, 31, 64, 65])
+@pytest.mark.parametrize("nodes", [5, 17])
+def test_ragged_batches(batch, nodes):
+    """Every request gets its own output, whatever the order they are worked in:
+    equal ones, unused ones, prompts and full images side by side."""
+    rng = random.Random(batch)
+    bases = [rng.choice([0, 17, 17, 99, -21, -5, -30]) for _ in range(batch)]
+    counts = [rng.choice([0, 1, nodes, nodes]) for _ in range(batch)]
+    pr = Problem(batch=batch, nodes=nodes, heads=(8, 1), tree=False, bases=bases, counts=counts,
+                 seed=batch)
+    pr.run()
+    pr.check(nodes=[0, nodes - 1])
+
+
 @pytest.mark.parametrize("kv", ["bf16", "fp8"])
 @pytest.mark.parametrize("nodes,heads", [(7, (4, 4)), (40, (8, 2))])
 def test_nonfinite_value_in_the_last_row(kv, nodes, heads):
