@@ -72,7 +72,7 @@ dsa_status tree_derive(const dsa_params* p, const dsa_shape* s, int nodes, Deriv
 // nodes of one request: 16 us with splits, 45 without; 256 nodes of 32 heads: 55
 // and 150), but not finer than two tiles of keys per streaming wave (four: 19 us, one:
 // 17) or four per workgroup otherwise (8100 keys of one head, 16 nodes: 26 us,
-// two: 31), and not at all up to four per wave (32 heads, d = 128, 848 keys, a layer:
+// two: 31), and not at all up to four per wave (32 heads, d = 128, 552 keys, a layer:
 // 14.9 us in two splits, 13.9 in one): a split costs a row of partial results and the
 // wait for them.
 TreeLaunch tree_launch(const Derived& d, int nodes) {
@@ -88,7 +88,7 @@ TreeLaunch tree_launch(const Derived& d, int nodes) {
   const int64_t tiles = (keys + l.keys - 1) / l.keys + 2;
   const int64_t wgs = pairs * l.row_tiles;
   // Twice the waves on the keys where at most one workgroup per CU has work (32
-  // heads, d = 128, 848 keys, 16 nodes: 13.9 us a layer with eight waves, 14.5 with four);
+  // heads, d = 128, 552 keys, 16 nodes: 13.9 us a layer with eight waves, 14.5 with four);
   // with more, what a CU holds at a time decides (32 such requests: 71 and 60).
   l.waves = stream && wgs <= 256 ? 8 : 4;
   const int64_t want = std::max<int64_t>(1, 256 / wgs);

@@ -229,10 +229,10 @@ __host__ __device__ constexpr int place_of(int c) {
 //
 // Both products run on the matrix cores with the keys as rows, S^T = K Q^T and
 // O^T = V^T P^T (v_mfma_f32_32x32x16_bf16).  A lane then holds scores, weights
-// and outputs of one query row (lane % 32) only: the running
-// maximum and the rescale need one exchange, with the lane's other half, and the
-// weights are the second product's operand where they are.  V comes back from
-// LDS transposed (ds_read_b64_tr_b16) in the order of keys the weights have.
+// and outputs of one query row (lane % 32) only: the running maximum and the
+// rescale need one exchange, with the lane's other half, and the weights are the
+// second product's operand where they are.  V comes back from LDS transposed
+// (ds_read_b64_tr_b16) in the order of keys the weights have.
 template <int D, bool F32, bool FP8>
 struct TreeWave {
   bf16x8 qf[D / 16];
@@ -259,7 +259,8 @@ struct TreeWave {
     l = 0.f;
   }
 
-  // Four keys from `key` on, 16 columns of block c: see kernels above.
+  // Four keys from `key` on of a lane's column of block c: of sixteen lanes that name
+  // four rows of 16 columns, each gets a column (ds_read_b64_tr_b16).
   static __device__ __forceinline__ uint2 vread(const uint16_t* lv, int lane, int key, int c) {
     const int s16 = lane & 15, r = key + (s16 >> 2);
     return __builtin_bit_cast(
@@ -529,6 +530,14 @@ constexpr int kTileKeys = 64;   // keys of a tile
 // A workgroup of four waves takes 128 query rows (node, query head of the KV
 // head's group) of one request and KV head, and a share of the keys.  Tiles of
 // 64 keys go through LDS for all four waves, two buffers in turn.
+//
+// Bound by the waves' own instructions: two images of 4096 tokens at once (32 heads
+// over 8, d = 128) take 372 us, 0.83 PFLOP/s, where a library product of 8192^3
+// reaches 1.19; without loads and stores to LDS the same arithmetic takes 286 (the
+// matrix cores are busy for a third of the time, the softmax's exponentials,
+// maxima and packing beside them), loads add 51, LDS stores 32.  Measured and left:
+// 64 rows per wave (490 us: one wave per SIMD), 32-key tiles with three waves per
+// SIMD (376), 256 rows per workgroup (377, and 52 us where 16 ragged prompts take 38).
 template <bool FP8, int D, bool F32>
 __global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
   constexpr int kTileRows = 128;
@@ -734,13 +743,18 @@ constexpr int kStreamKeys = 32;  // keys of a wave's tile
 template <int D>
 constexpr uint32_t kStreamLds = kStreamKeys * (kKRow<D> + kVRow<D>) * 2;  // a wave's K and V tile
 
-// At most 32 query rows per workgroup: bound by the cache's bytes.  Every wave
-// streams tiles of 32 keys of its own for all rows, through registers (the next
-// tiles are on their way while one is computed) and an LDS region of its own, so
-// the waves of a workgroup wait for each other only to join their results at
-// the end.  (K straight into the matrix operand, a row per lane, halves the LDS
-// traffic but reads 32 bytes of a row at a time: 67 us against 62 for 1024 pairs of
-// 290 to 800 keys, d = 128.)
+// At most 32 query rows per workgroup.  Every wave streams tiles of 32 keys of
+// its own for all rows, through registers (the next tiles are on their way while
+// one is computed) and an LDS region of its own, so the waves of a workgroup wait
+// for each other only to join their results at the end.
+//
+// Bound by the cache's bytes with one row tile and a full chip: 32 requests of 32
+// heads, 265 to 807 keys, d = 128, bf16, take 57 us (5.2 TB/s; a large copy reaches
+// 4.8).  K straight into the matrix operand, a row per lane, halves the LDS traffic
+// but reads 32 bytes of a row at a time (67 us); loads without the streaming hint
+// take 68.  With few workgroups bound by what a CU reads (32 workgroups of 552
+// keys: 13.9 us), with two row tiles over fp8 by widening and arithmetic, done for
+// both (32 requests, 8 KV heads, 4096 keys: 79 us, 51 with one).
 template <bool FP8, int D, bool F32, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void tree_stream_kernel(TreeArgs a) {
   constexpr int CPR = D / 8, RPP = 64 / CPR, NP = kStreamKeys / RPP;  // bf16 rows of V
