@@ -57,9 +57,8 @@ struct TreeArgs {
 // Launch of dsa_tree_attention.
 struct TreeLaunch {
   int rows;       // query rows per workgroup
-  int waves;      // waves per workgroup
-  int keys;       // keys per tile
-  int split_tiles;  // tiles per split, at least
+  int waves;      // waves per workgroup (streaming)
+  int split_tiles;  // tiles of 32 keys per split, at least
   int row_tiles;  // per (request, KV head)
   int splits;
   int64_t workgroups;

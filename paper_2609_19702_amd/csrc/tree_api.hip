@@ -64,38 +64,42 @@ dsa_status tree_derive(const dsa_params* p, const dsa_shape* s, int nodes, Deriv
 
 }  // namespace
 
-// Up to 64 query rows per (request, KV head) stream the keys for 32 rows at a
-// time (tree_stream_kernel); more go through LDS for 128 at a time
-// (tree_tile_kernel; 64 rows of d = 128 over fp8, 32 requests: 70 us a layer
-// streamed, 98 through it).  The keys of a row tile are split where the row tiles
-// alone would leave CUs without a workgroup (4096 keys of 8 KV heads, d = 128, 8
-// nodes of one request: 16 us with splits, 45 without; 256 nodes of 32 heads: 55
-// and 150), but not finer than two tiles of keys per streaming wave (four: 19 us, one:
-// 17) or four per workgroup otherwise (8100 keys of one head, 16 nodes: 26 us,
-// two: 31), and not at all up to four per wave (32 heads, d = 128, 552 keys, a layer:
-// 14.9 us in two splits, 13.9 in one): a split costs a row of partial results and the
-// wait for them.
+// Two kernels.  Up to 64 query rows per (request, KV head), and more of them where
+// the chip holds all their tiles at once (two workgroups on each of 256 CUs), stream
+// the keys for 32 rows at a time (tree_stream_kernel): 512 nodes of 32 heads over 8
+// after 2256 keys, d = 128: 49 us, 86 through LDS; 30 nodes of 16 requests: 35
+// and 54; but of 32 requests: 73 and 47 (with 13 nodes, two row tiles: bf16 75 and 70,
+// fp8 52 and 74).  The others go through LDS for 128 rows at a time
+// (tree_tile_kernel).
+//
+// The keys of a streaming row tile are split where the row tiles alone would leave
+// CUs without a workgroup (4096 keys of 8 KV heads, d = 128, 8 nodes of one request:
+// 16 us with splits, 45 without), but not finer than two tiles of keys per wave (four:
+// 19 us, one: 17), and not at all up to four per wave (32 heads, d = 128, 552 keys, a
+// layer: 14.9 us in two splits, 13.9 in one): a split costs a row of partial results
+// and the wait for them.
 TreeLaunch tree_launch(const Derived& d, int nodes) {
   TreeLaunch l{};
   const int64_t rows = static_cast<int64_t>(nodes) * d.G;
   const int64_t pairs = static_cast<int64_t>(d.B) * d.Hkv;
-  const bool stream = rows <= 64;
+  const bool stream = rows <= 64 || pairs * ((rows + 31) / 32) <= 512;
   l.rows = stream ? 32 : 128;
-  l.keys = stream ? 32 : 64;
   l.row_tiles = static_cast<int>((rows + l.rows - 1) / l.rows);
-  const int64_t keys = d.Lp + (d.mode == DSA_MODE_WINDOW ? std::min(d.Natt, d.Ldec) : d.Ldec) +
-                       int64_t{nodes};
-  const int64_t tiles = (keys + l.keys - 1) / l.keys + 2;
-  const int64_t wgs = pairs * l.row_tiles;
+  l.splits = 1;
+  l.workgroups = pairs * l.row_tiles;
+  if (!stream) return l;
   // Twice the waves on the keys where at most one workgroup per CU has work (32
   // heads, d = 128, 552 keys, 16 nodes: 13.9 us a layer with eight waves, 14.5 with four);
   // with more, what a CU holds at a time decides (32 such requests: 71 and 60).
-  l.waves = stream && wgs <= 256 ? 8 : 4;
-  const int64_t want = std::max<int64_t>(1, 256 / wgs);
-  const int64_t least = !stream ? 4 : tiles <= 4 * l.waves ? tiles : 2 * l.waves;
-  l.split_tiles = static_cast<int>(std::max<int64_t>(least, (tiles + want - 1) / want));
+  l.waves = l.workgroups <= 256 ? 8 : 4;
+  const int64_t keys = d.Lp + (d.mode == DSA_MODE_WINDOW ? std::min(d.Natt, d.Ldec) : d.Ldec) +
+                       int64_t{nodes};
+  const int64_t tiles = (keys + 31) / 32 + 2;
+  const int64_t want = std::max<int64_t>(1, 256 / l.workgroups);
+  const int64_t least = tiles <= 4 * l.waves ? tiles : 2 * l.waves;
+  l.split_tiles = static_cast<int>(std::max(least, (tiles + want - 1) / want));
   l.splits = static_cast<int>((tiles + l.split_tiles - 1) / l.split_tiles);
-  l.workgroups = wgs * l.splits;
+  l.workgroups *= l.splits;
   l.ws_bytes = l.splits > 1 ? static_cast<size_t>(l.workgroups) * l.rows * (d.D + 4) * 4 : 0;
   return l;
 }

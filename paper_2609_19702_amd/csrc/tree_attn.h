@@ -526,10 +526,11 @@ __device__ __forceinline__ int tree_cut(int tiles, int part, int parts) {
 // ---- many query rows -----------------------------------------------------------
 
 constexpr int kTileKeys = 64;   // keys of a tile
+constexpr int kTileRows = 128;  // query rows of a workgroup
 
 // A workgroup of four waves takes 128 query rows (node, query head of the KV
-// head's group) of one request and KV head, and a share of the keys.  Tiles of
-// 64 keys go through LDS for all four waves, two buffers in turn.
+// head's group) of one request and KV head.  Tiles of 64 keys go through LDS for all
+// four waves, two buffers in turn.
 //
 // Bound by the waves' own instructions: two images of 4096 tokens at once (32 heads
 // over 8, d = 128) take 372 us, 0.83 PFLOP/s, where a library product of 8192^3
@@ -540,7 +541,6 @@ constexpr int kTileKeys = 64;   // keys of a tile
 // SIMD (376), 256 rows per workgroup (377, and 52 us where 16 ragged prompts take 38).
 template <bool FP8, int D, bool F32>
 __global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
-  constexpr int kTileRows = 128;
   constexpr int CPR = D / 8;           // 16-byte chunks of a bf16 row
   constexpr int NP = CPR * kTileKeys / 256;
   constexpr int RPP = 256 / CPR;       // rows per pass of the workgroup
@@ -549,13 +549,13 @@ __global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
   __shared__ __align__(16) uint16_t lv[2][kTileKeys * kVRow<D>];
   __shared__ uint32_t lbad[2][4];  // V rows of a tile that are not finite, by wave (clean_rows)
 
-  const TreeItem item = tree_item(a.B * a.Hkv, a.row_tiles * a.splits);
+  const TreeItem item = tree_item(a.B * a.Hkv, a.row_tiles);
   if (item.pair < 0) return;
   const TreePlace place = tree_place<true>(a, item.pair / a.Hkv, kTileRows);
   const TreeReq rq = place.rq;
-  const int sub = item.sub, b = place.b;
+  const int b = place.b;
   const int h = item.pair % a.Hkv, pair = b * a.Hkv + h;
-  const int qt = a.row_tiles - 1 - sub / a.splits, sp = sub % a.splits;  // longest first
+  const int qt = a.row_tiles - 1 - item.sub;  // longest first
   const int rows = rq.n * a.G, r0 = qt * kTileRows;
   if (r0 >= rows) return;
   TreeTile tt{r0 / a.G, (min(r0 + kTileRows, rows) - 1) / a.G, 0, a.S - rq.base};
@@ -563,9 +563,6 @@ __global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
   const TreeKeys ks = tree_keys(a, rq, tt.n0, tt.n1);
   const int t_old = (ks.cached.n + kTileKeys - 1) / kTileKeys;
   const int tiles = t_old + (ks.fresh.n + kTileKeys - 1) / kTileKeys;
-  const int nsp = tree_splits(a, tiles);
-  if (sp >= nsp) return;
-  const int t0 = tree_cut(tiles, sp, nsp), t1 = tree_cut(tiles, sp + 1, nsp);
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -664,9 +661,9 @@ __global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
 
   // A tile's rows go into LDS at the start of the tile before, when they have had a
   // whole tile's time to arrive, and the tile after them is asked for.
-  int t = t0, buf = 0;
+  int t = 0, buf = 0;
   if constexpr (FP8) {
-    const int end = min(t1, t_old);
+    const int end = t_old;
     if (t < end) {
       load8(t);
       put8(t, 0);
@@ -687,15 +684,15 @@ __global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
       __syncthreads();
     }
   }
-  if (t < t1) {
+  if (t < tiles) {
     load(t);
     put(t, buf);
-    if (t + 1 < t1) load(t + 1);
+    if (t + 1 < tiles) load(t + 1);
     __syncthreads();
   }
-  for (; t < t1; ++t, buf ^= 1) {
-    if (t + 1 < t1) put(t + 1, buf ^ 1);
-    if (t + 2 < t1) load(t + 2);
+  for (; t < tiles; ++t, buf ^= 1) {
+    if (t + 1 < tiles) put(t + 1, buf ^ 1);
+    if (t + 2 < tiles) load(t + 2);
     asm volatile("" ::: "memory");  // the loads stay ahead of the tile
     if (wave_on) {
       uint32_t see[2] = {};
@@ -712,33 +709,21 @@ __global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
   const float l = l1 + l2;
   if (row >= rows) return;
   const int hh = lane >> 5;
-  if (nsp == 1) {
-    const float inv = 1.f / l;
-    const int64_t out =
-        ((static_cast<int64_t>(b) * a.N + my.node) * a.Hq + h * a.G + row % a.G) * D;
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        store4<F32>(a.out, out + out_col<D, FP8>(c, i / 4, hh), w.o[c][i] * inv,
-                    w.o[c][i + 1] * inv, w.o[c][i + 2] * inv, w.o[c][i + 3] * inv);
-    return;
-  }
-  float* part = a.part + ((static_cast<int64_t>(pair) * a.row_tiles + qt) * a.splits + sp) *
-                             kTileRows * kPartRow<D> +
-                (row - r0) * kPartRow<D>;
+  const float inv = 1.f / l;
+  const int64_t out =
+      ((static_cast<int64_t>(b) * a.N + my.node) * a.Hq + h * a.G + row % a.G) * D;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c)
 #pragma unroll
     for (int i = 0; i < 16; i += 4)
-      *reinterpret_cast<float4*>(part + out_col<D, FP8>(c, i / 4, hh)) = make_float4(
-          w.o[c][i], w.o[c][i + 1], w.o[c][i + 2], w.o[c][i + 3]);
-  if (lane < 32) *reinterpret_cast<float2*>(part + D) = make_float2(w.m, l);
+      store4<F32>(a.out, out + out_col<D, FP8>(c, i / 4, hh), w.o[c][i] * inv, w.o[c][i + 1] * inv,
+                  w.o[c][i + 2] * inv, w.o[c][i + 3] * inv);
 }
 
 // ---- few query rows --------------------------------------------------------------
 
 constexpr int kStreamKeys = 32;  // keys of a wave's tile
+constexpr int kStreamRows = 32;  // query rows of a workgroup
 
 template <int D>
 constexpr uint32_t kStreamLds = kStreamKeys * (kKRow<D> + kVRow<D>) * 2;  // a wave's K and V tile
@@ -976,17 +961,16 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_stream_kernel(TreeArgs a) {
 // One wave per query row.  Bound by its chain of memory latencies, so the first
 // kAhead splits are read before it is known how many there are.
 template <int D, bool F32>
-__global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a, int tile_rows,
-                                                           int tile_keys) {
+__global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
   constexpr int E = D / 64, kAhead = 8;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + wave;
-  const int per_pair = a.row_tiles * tile_rows;
+  const int per_pair = a.row_tiles * kStreamRows;
   const int pair = static_cast<int>(at / per_pair), row = static_cast<int>(at % per_pair);
   if (pair >= a.B * a.Hkv) return;
-  const int b = pair / a.Hkv, h = pair % a.Hkv, qt = row / tile_rows, r0 = qt * tile_rows;
-  const int64_t step = static_cast<int64_t>(tile_rows) * kPartRow<D>;
+  const int b = pair / a.Hkv, h = pair % a.Hkv, qt = row / kStreamRows, r0 = qt * kStreamRows;
+  constexpr int64_t step = kStreamRows * kPartRow<D>;
   const float* part = a.part + (static_cast<int64_t>(pair) * a.row_tiles + qt) * a.splits * step +
                       (row - r0) * kPartRow<D>;
   float pm[kAhead], pl[kAhead], px[kAhead][E];
@@ -1002,8 +986,9 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a, int tile_
   const TreeReq rq = tree_request(a.base, a.count, b, a.N, a.Lp, a.Ldec);
   const int rows = rq.n * a.G;
   if (row >= rows) return;
-  const TreeKeys ks = tree_keys(a, rq, r0 / a.G, (min(r0 + tile_rows, rows) - 1) / a.G);
-  const int tiles = (ks.cached.n + tile_keys - 1) / tile_keys + (ks.fresh.n + tile_keys - 1) / tile_keys;
+  const TreeKeys ks = tree_keys(a, rq, r0 / a.G, (min(r0 + kStreamRows, rows) - 1) / a.G);
+  const int tiles = (ks.cached.n + kStreamKeys - 1) / kStreamKeys +
+                    (ks.fresh.n + kStreamKeys - 1) / kStreamKeys;
   const int nsp = tree_splits(a, tiles);
   if (nsp <= 1) return;
   float M = kTreeMin, L = 0.f, acc[E] = {};
@@ -1041,29 +1026,20 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a, int tile_
   }
 }
 
-template <bool FP8, int D, bool F32, int NW>
-hipError_t launch_stream(const TreeLaunch& l, const TreeArgs& a, hipStream_t st) {
-  tree_stream_kernel<FP8, D, F32, NW>
-      <<<dim3(tree_grid(static_cast<int64_t>(a.B) * a.Hkv, a.row_tiles * a.splits)), dim3(64 * NW),
-         0, st>>>(a);
-  return hipGetLastError();
-}
-
 template <bool FP8, int D, bool F32>
 hipError_t launch_one(const TreeLaunch& l, const TreeArgs& a, hipStream_t st) {
-  hipError_t e;
-  const dim3 grid(tree_grid(static_cast<int64_t>(a.B) * a.Hkv, a.row_tiles * a.splits));
-  if (l.rows == 128) {
+  const int64_t pairs = static_cast<int64_t>(a.B) * a.Hkv;
+  const dim3 grid(tree_grid(pairs, a.row_tiles * a.splits));
+  if (l.rows == kTileRows)
     tree_tile_kernel<FP8, D, F32><<<grid, dim3(256), 0, st>>>(a);
-    e = hipGetLastError();
-  } else {
-    e = l.waves == 8 ? launch_stream<FP8, D, F32, 8>(l, a, st)
-                     : launch_stream<FP8, D, F32, 4>(l, a, st);
-  }
+  else if (l.waves == 8)
+    tree_stream_kernel<FP8, D, F32, 8><<<grid, dim3(512), 0, st>>>(a);
+  else
+    tree_stream_kernel<FP8, D, F32, 4><<<grid, dim3(256), 0, st>>>(a);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || l.splits == 1) return e;
-  const int64_t waves = static_cast<int64_t>(a.B) * a.Hkv * a.row_tiles * l.rows;
-  tree_combine_kernel<D, F32><<<dim3(static_cast<uint32_t>((waves + 3) / 4)), dim3(256), 0, st>>>(
-      a, l.rows, l.keys);
+  const int64_t waves = pairs * a.row_tiles * kStreamRows;
+  tree_combine_kernel<D, F32><<<dim3(static_cast<uint32_t>((waves + 3) / 4)), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }
 

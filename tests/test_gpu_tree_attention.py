@@ -120,6 +120,30 @@ def test_chunk(case):
     say("  worst error over its bound", pr.check(nodes))
 
 
+def query_rows(case):
+    hq, hkv = case.get("heads", (4, 4))
+    return case["nodes"] * hq // hkv
+
+
+MANY = [c for c in [dict(seed=3, **c) for c in TREES] +
+        [dict(seed=5, tree=False, **c) for c in CHUNKS] if query_rows(c) > 64]
+
+
+@pytest.mark.parametrize("case", MANY, ids=range(len(MANY)))
+def test_many_row_tiles(case):
+    """The same with so many heads that the rows go through LDS, 128 at a time."""
+    hq, hkv = case.get("heads", (4, 4))
+    tiles = -(-query_rows(case) // 32) * hkv * case.get("batch", 2)
+    f = 512 // tiles + 1
+    pr = Problem(**{**case, "heads": (hq * f, hkv * f)})
+    assert B.tree_launch_info(pr.p, pr.s, pr.nodes).rows_per_tile == 128
+    pr.run()
+    n = case["nodes"]
+    nodes = {0, 1, n // 3, n // 2 + 1, n - 2, n - 1, 31, 32, 63, 64, 65, 127, 128, 36, 37, 38}
+    say("  worst error over its bound",
+        pr.check(sorted(i for i in nodes if i < n), sorted({0, hkv * f // 2, hkv * f - 1})))
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_equals_a_decode_step(d):
     """A single node attends what a decode step at its position attends."""
@@ -212,7 +236,8 @@ def _poison(x, kind):
 
 @pytest.mark.parametrize("kind", ["nan", "inf", "-inf"])
 @pytest.mark.parametrize("tree,heads,out", [(True, (4, 4), "fp32"), (True, (8, 1), "bf16"),
-                                            (False, (4, 4), "bf16"), (False, (8, 1), "fp32")])
+                                            (False, (4, 4), "bf16"), (False, (8, 1), "fp32"),
+                                            (False, (160, 160), "bf16"), (True, (512, 64), "fp32")])
 def test_hidden_values_stay_hidden(kind, tree, heads, out):
     """What a node must not see may hold anything: rows past a request's count,
     cache rows that hold nothing yet, another branch's K and V, later tokens,
@@ -255,7 +280,7 @@ def test_hidden_values_stay_hidden(kind, tree, heads, out):
 
 
 @pytest.mark.parametrize("batch", [2, 31, 64, 65])
-@pytest.mark.parametrize("nodes", [5, 17])
+@pytest.mark.parametrize("nodes", [5, 17, 91])
 def test_ragged_batches(batch, nodes):
     """Every request gets its own output, whatever the order they are worked in:
     equal ones, unused ones, prompts and full images side by side."""
@@ -269,7 +294,7 @@ def test_ragged_batches(batch, nodes):
 
 
 @pytest.mark.parametrize("kv", ["bf16", "fp8"])
-@pytest.mark.parametrize("nodes,heads", [(7, (4, 4)), (40, (8, 2))])
+@pytest.mark.parametrize("nodes,heads", [(7, (4, 4)), (40, (8, 2)), (40, (256, 32))])
 def test_nonfinite_value_in_the_last_row(kv, nodes, heads):
     """The last row that a cache has, in a tile with no keys after it: seen by all
     nodes, as the last of the new rows is by one."""
@@ -302,7 +327,8 @@ def test_nonfinite_value_in_the_last_row(kv, nodes, heads):
 
 
 @pytest.mark.parametrize("nodes,heads,d", [(6, (4, 4), 64), (13, (8, 1), 128), (30, (8, 4), 128),
-                                           (50, (8, 2), 64)])
+                                           (50, (8, 2), 64), (50, (256, 32), 64),
+                                           (30, (512, 64), 128)])
 @pytest.mark.parametrize("ring", [0, 20])
 def test_hidden_fp8_codes_stay_hidden(nodes, heads, d, ring):
     """NaN codes of cached positions that some nodes' windows have left: those get
@@ -327,7 +353,7 @@ def test_hidden_fp8_codes_stay_hidden(nodes, heads, d, ring):
                 assert torch.equal(a[:, i, :, c], w[:, i, :, c]), (i, c)
 
 
-@pytest.mark.parametrize("nodes,heads", [(5, (4, 4)), (40, (8, 2))])
+@pytest.mark.parametrize("nodes,heads", [(5, (4, 4)), (40, (8, 2)), (40, (256, 32))])
 def test_visible_nan_is_a_nan(nodes, heads):
     """Also beside hidden keys, and next to infinities of one sign."""
     pr = Problem(nodes=nodes, heads=heads, tree=False, seed=2)
@@ -376,8 +402,10 @@ def test_strides_of_one_node_and_far_offsets():
 
 @pytest.mark.parametrize("case", [dict(nodes=16, d=128, batch=1, grid=(24, 24)),
                                   dict(nodes=64, heads=(8, 1), grid=(24, 24), kv="fp8"),
-                                  dict(nodes=300, tree=False, grid=(24, 24), bases=[-21, 5])],
-                         ids=["small", "grouped", "chunk"])
+                                  dict(nodes=300, tree=False, grid=(24, 24), bases=[-21, 5]),
+                                  dict(nodes=300, tree=False, grid=(24, 24), bases=[-21, 5],
+                                       heads=(64, 64), d=128, kv="fp8")],
+                         ids=["small", "grouped", "chunk", "many"])
 def test_runs_repeat_and_replay(case):
     """Calls repeat bit for bit: again, on another stream, and from a captured
     graph whose inputs and base positions change between replays."""

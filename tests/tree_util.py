@@ -118,7 +118,7 @@ class Problem:
             got.append(y[self.order] if x.dtype is torch.bfloat16 or sc is None else y)
         return got
 
-    def check(self, nodes=None):
+    def check(self, nodes=None, kv_heads=None):
         """Every node's output against fp64, within the bound of its arithmetic;
         what belongs to no node is as it was."""
         torch.cuda.synchronize()
@@ -138,7 +138,7 @@ class Problem:
                 held, up = otree.keys_of(self.parents[b], i, base, self.prompt, self.sinks,
                                          self.window)
                 rows = [self.row_of(j) for j in held]
-                for h in range(self.hkv):
+                for h in range(self.hkv) if kv_heads is None else kv_heads:
                     kk = np.concatenate([k[b, h, rows], kn[b, up, h]])
                     vv = np.concatenate([v[b, h, rows], vn[b, up, h]])
                     for e in range(g):
