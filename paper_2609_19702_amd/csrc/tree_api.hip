@@ -73,11 +73,12 @@ dsa_status tree_derive(const dsa_params* p, const dsa_shape* s, int nodes, Deriv
 // (tree_tile_kernel).
 //
 // The keys of a streaming row tile are split where the row tiles alone would leave
-// CUs without a workgroup (4096 keys of 8 KV heads, d = 128, 8 nodes of one request:
-// 16 us with splits, 45 without), but not finer than two tiles of keys per wave (four:
-// 19 us, one: 17), and not at all up to four per wave (32 heads, d = 128, 552 keys, a
-// layer: 14.9 us in two splits, 13.9 in one): a split costs a row of partial results
-// and the wait for them.
+// CUs without a workgroup: into about eight, a tile per wave or more (40 tiles of
+// d = 128, 32 heads: 12.4 us; at two tiles per wave 14.7), and more of them at two tiles
+// per wave (136 tiles, 8 heads: 16 us; at one 17, at four 19, unsplit 45).  A split
+// costs a row of partial results and a second kernel, so few bytes stay whole: at
+// d = 64, 17 tiles take 8.3 us whole and 8.8 split, 26 take 10.5 and 9.3; at d = 128,
+// 13 take 10.8 and 10.6, 29 take 13.9 and 12.3.
 TreeLaunch tree_launch(const Derived& d, int nodes) {
   TreeLaunch l{};
   const int64_t rows = static_cast<int64_t>(nodes) * d.G;
@@ -89,14 +90,16 @@ TreeLaunch tree_launch(const Derived& d, int nodes) {
   l.workgroups = pairs * l.row_tiles;
   if (!stream) return l;
   // Twice the waves on the keys where at most one workgroup per CU has work (32
-  // heads, d = 128, 552 keys, 16 nodes: 13.9 us a layer with eight waves, 14.5 with four);
+  // heads, d = 128, 552 keys, 16 nodes, whole: 13.9 us with eight waves, 14.5 with four);
   // with more, what a CU holds at a time decides (32 such requests: 71 and 60).
   l.waves = l.workgroups <= 256 ? 8 : 4;
   const int64_t keys = d.Lp + (d.mode == DSA_MODE_WINDOW ? std::min(d.Natt, d.Ldec) : d.Ldec) +
                        int64_t{nodes};
   const int64_t tiles = (keys + 31) / 32 + 2;
   const int64_t want = std::max<int64_t>(1, 256 / l.workgroups);
-  const int64_t least = tiles <= 4 * l.waves ? tiles : 2 * l.waves;
+  const int64_t least = tiles * d.D <= 1536
+                            ? tiles
+                            : std::clamp<int64_t>(tiles / 8, l.waves, 2 * l.waves);
   l.split_tiles = static_cast<int>(std::max(least, (tiles + want - 1) / want));
   l.splits = static_cast<int>((tiles + l.split_tiles - 1) / l.split_tiles);
   l.workgroups *= l.splits;

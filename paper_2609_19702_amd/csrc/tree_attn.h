@@ -738,7 +738,7 @@ constexpr uint32_t kStreamLds = kStreamKeys * (kKRow<D> + kVRow<D>) * 2;  // a w
 // 4.8).  K straight into the matrix operand, a row per lane, halves the LDS traffic
 // but reads 32 bytes of a row at a time (67 us); loads without the streaming hint
 // take 68.  With few workgroups bound by what a CU reads (32 workgroups of 552
-// keys: 13.9 us), with two row tiles over fp8 by widening and arithmetic, done for
+// keys, unsplit: 13.9 us), with two row tiles over fp8 by widening and arithmetic, done for
 // both (32 requests, 8 KV heads, 4096 keys: 79 us, 51 with one).
 template <bool FP8, int D, bool F32, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void tree_stream_kernel(TreeArgs a) {
