@@ -31,7 +31,7 @@ ROWS = B.NodeRows(4096, 512, 64, 65536)
 
 
 def layout(**kw):
-    a = dict(d_row_base=None, stride_batch=30720, stride_head=7680, stride_row=64, ring_rows=0,
+    a = dict(d_row_base=None, stride_batch=61440, stride_head=7680, stride_row=64, ring_rows=0,
              d_k_scale=None, d_v_scale=None, dtype=B.KV_BF16)
     a.update(kw)
     return B.KVLayout(*[a[f[0]] for f in B.KVLayout._fields_])
