@@ -569,8 +569,8 @@ DSA_API dsa_status dsa_tree_plan(int32_t batch, int32_t nodes, const int32_t* d_
                                  hipStream_t stream);
 
 /* Element types of dsa_tree_attention's output. */
-#define DSA_OUT_FP32 0 /* weights kept to fp32 in the product with V           */
-#define DSA_OUT_BF16 1 /* weights rounded to bf16 for that product             */
+#define DSA_OUT_FP32 0 /* weights kept to fp32 in the product with V             */
+#define DSA_OUT_BF16 1 /* weights in two bf16 terms there: off by 2^-16 at most  */
 
 /*
  * Attention of every node of every request in dense or window mode.  Node i

@@ -333,10 +333,11 @@ struct TreeWave {
   // O += P V of 32 keys, 16 a step.  Half hh's eight operand slots are the keys
   // 4 hh .. + 3 and 8 + 4 hh .. + 3 of the step, and V is read in that order.
   // For fp32 outputs the weights go in as three bf16 terms, which hold all their
-  // 24 bits; for bf16 outputs rounded to one, off by half a step as the outputs
-  // are.
+  // 24 bits; for bf16 outputs as two, each nearest, so that what is left out of a
+  // weight, 2^-16 of it, is a 256th of the output's own half step (with one term an
+  // element was off by up to 7 of those).
   __device__ __forceinline__ void values(int lane, const uint16_t* lv, const f32x16& p) {
-    constexpr int NE = F32 ? 3 : 1;
+    constexpr int NE = F32 ? 3 : 2;
     const int hh = lane >> 5;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -354,6 +355,8 @@ struct TreeWave {
           }
         } else {
           w[0][j] = pack_bf16(u, v);
+          w[1][j] = pack_bf16(u - __uint_as_float(w[0][j] << 16),
+                              v - __uint_as_float(w[0][j] & 0xffff0000u));
         }
       }
 #pragma unroll
@@ -533,12 +536,14 @@ constexpr int kTileRows = 128;  // query rows of a workgroup
 // four waves, two buffers in turn.
 //
 // Bound by the waves' own instructions: two images of 4096 tokens at once (32 heads
-// over 8, d = 128) take 372 us, 0.83 PFLOP/s, where a library product of 8192^3
-// reaches 1.19; without loads and stores to LDS the same arithmetic takes 286 (the
-// matrix cores are busy for a third of the time, the softmax's exponentials,
-// maxima and packing beside them), loads add 51, LDS stores 32.  Measured and left:
-// 64 rows per wave (490 us: one wave per SIMD), 32-key tiles with three waves per
-// SIMD (376), 256 rows per workgroup (377, and 52 us where 16 ragged prompts take 38).
+// over 8, d = 128, bf16 outputs) take 471 us, 0.66 PFLOP/s, where a library product
+// of 8192^3 reaches 1.19.  With the weights in one bf16 term they took 375: 286 for
+// the arithmetic without loads and stores to LDS (the matrix cores busy for a third
+// of the time, the softmax's exponentials, maxima and packing beside them), 51 for
+// the loads, 32 for the LDS stores; the second term's products and packing take the
+// rest.  Measured with one term and left: 64 rows per wave (490 us: one wave per
+// SIMD), 32-key tiles with three waves per SIMD (376), 256 rows per workgroup (377,
+// and 52 us where 16 ragged prompts take 38).
 template <bool FP8, int D, bool F32>
 __global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
   constexpr int CPR = D / 8;           // 16-byte chunks of a bf16 row

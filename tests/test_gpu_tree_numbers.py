@@ -1,0 +1,61 @@
+"""Numbers of ``tree_attention`` where roundings, infinities and unusual scales
+show: few keys, rows and codes that are not finite, every kernel."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import tree as otree
+from paper_2609_19702_amd import binding as B
+from tests.gpu_util import say
+from tests.tree_util import Problem
+
+pytestmark = pytest.mark.gpu
+
+
+# One request's short tree, with a workgroup per pair and with keys in splits,
+# and rows that go through LDS 128 at a time.
+KERNELS = {"whole": dict(batch=2, nodes=9), "split": dict(batch=1, nodes=9, grid=(40, 40)),
+           "tiles": dict(batch=2, nodes=70, heads=(172, 172), tree=False)}
+
+
+def problem(kernel, **kw):
+    pr = Problem(**{**KERNELS[kernel], **kw})
+    info = B.tree_launch_info(pr.p, pr.s, pr.nodes)
+    assert (info.rows_per_tile == 128) == (kernel == "tiles")
+    assert (info.splits > 1) == (kernel == "split")
+    return pr
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kernel", list(KERNELS))
+def test_bf16_outputs_round_the_result_alone(kernel, d, kv):
+    """Few keys, so that no average hides what a weight is off by.  An element may
+    be off by half a step of its own size, 2^-8 of it, by what fp32 arithmetic is
+    (``band``), and by the weights' part: two bf16 terms, each nearest, leave
+    2^-8 * 2^-8 of a weight, and the second term's products add n roundings of
+    2^-24 to the sum over n keys."""
+    pr = problem(kernel, d=d, kv=kv, out="bf16", prompt=2, bases=[1, 3][:KERNELS[kernel]["batch"]],
+                 seed=d)
+    pr.run()
+    torch.cuda.synchronize()
+    out = pr.out.double().cpu().numpy()
+    k, v = pr.caches64()
+    q, kn, vn = (x.double().cpu().numpy() for x in (pr.q, pr.kn, pr.vn))
+    worst = 0.0
+    for b in range(pr.batch):
+        for i in range(min(9, pr.nodes)):
+            held, up = otree.keys_of(pr.parents[b], i, pr.bases[b], pr.prompt, 0, None)
+            rows = [pr.row_of(j) for j in held]
+            for h in sorted({0, 1, pr.hkv - 1}):
+                kk = np.concatenate([k[b, h, rows], kn[b, up, h]])
+                vv = np.concatenate([v[b, h, rows], vn[b, up, h]])
+                ref, band = otree.attend(q[b, i, h], kk, vv, pr.scale)
+                e = (band + 2.0 ** -16 + len(kk) * 2.0 ** -24) * np.abs(vv).max()
+                err = np.abs(out[b, i, h] - ref) / (2.0 ** -8 * (np.abs(ref) + e) + e)
+                worst = max(worst, err.max())
+    say("  worst error over its bound", worst)
+    assert worst <= 1.0
