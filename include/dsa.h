@@ -580,7 +580,9 @@ DSA_API dsa_status dsa_tree_plan(int32_t batch, int32_t nodes, const int32_t* d_
  * no bound and S = 0 in dense mode.  That is what dsa_decode_attention gives for
  * a token whose predecessors are all in the cache.  A prompt's rows attend the
  * prompt up to themselves in every mode.  What a mask hides does not reach the
- * output, NaN and infinities included.
+ * output, NaN and infinities included.  An infinity in a V row that a node attends
+ * makes that element of its output the infinity, however small its weight, and a
+ * NaN, or infinities of both signs, make it a NaN.
  *   d_q              bf16 rows (q_rows), query head h of node i
  *   d_k_new, d_v_new bf16 rows (new_rows), KV head h of node i
  *   d_k, d_v, kv     caches as for dsa_decode_attention, holding the positions

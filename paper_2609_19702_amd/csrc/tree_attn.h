@@ -401,6 +401,28 @@ struct TreeWave {
     values(lane, lv + 32 * kVRow<D>, s1);
   }
 
+  // Whether the lane's outputs are finite, and its n-th four of them.
+  __device__ __forceinline__ bool all_finite() const {
+    float s[4] = {};
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i & 3] = fmaf(o[c][i], 0.f, s[i & 3]);
+    return s[0] + s[1] + s[2] + s[3] == 0.f;
+  }
+  __device__ __forceinline__ void four(int n, float (&x)[4]) const {
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i & 3] = n == 4 * c + i / 4 ? o[c][i] : x[i & 3];
+  }
+  __device__ __forceinline__ void set_four(int n, const float (&x)[4]) {
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[c][i] = n == 4 * c + i / 4 ? x[i & 3] : o[c][i];
+  }
+
   // Adds the infinities and NaN of V row v (fp8 where CODES) to the rows that see
   // its key: as products of 1 and the largest bf16 values, whose sum overflows, and of
   // 0 where the key is hidden.  A NaN is both infinities, one after the other.  (Summed
@@ -510,6 +532,64 @@ __device__ __forceinline__ uint32_t clean_codes(uint4* x) {
       rows |= (who >> (g * CPR)) & ((1ull << CPR) - 1) ? 1u << (i * RPW + g) : 0u;
   }
   return rows;
+}
+
+// A weight's terms, or a weight that underflows, make NaN of an infinity in V
+// where one of them is 0.  So four elements of a row that are not all finite are
+// settled once more: what each sees of infinities and NaN, over the tiles of 32 keys
+// t0 .. t1 - 1, takes its place.  v_old, v_new: the elements' columns of V.
+template <bool FP8>
+__device__ __forceinline__ void settle_nonfinite(const TreeArgs& a, const TreeKeys& ks,
+                                                 const TreeTile& tt, const TreeRow& my, int b,
+                                                 const uint8_t* v_old, const uint8_t* v_new, int t0,
+                                                 int t1, float (&x)[4]) {
+  const int t_old = (ks.cached.n + 31) / 32;
+  uint32_t up = 0, down = 0;  // bit per element: an infinity, or both for a NaN
+#pragma unroll 1
+  for (int t = t0; t < t1; ++t) {
+    const bool old = t < t_old;
+    const int e0 = (t - (old ? 0 : t_old)) * 32;
+    const KeyList list = pick_list(old, ks.cached, ks.fresh);
+    const uint8_t* v = old ? v_old : v_new;
+    const int64_t step = old ? a.sr : a.nsn * 2;
+    const uint32_t see = old ? see_cached(ks, my, e0) : see_fresh(a, ks, tt, my, b, e0);
+#pragma unroll 1
+    for (int i = 0; i < 32; i += 8) {
+      uint32_t h[8][2];  // bf16 bits; of fp8 codes the NaN ones alone
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint8_t* at = v + list.near(e0 + i + e) * step;
+        if (FP8 && old) {
+          const uint32_t n = nan_bytes(*reinterpret_cast<const uint32_t*>(at)) >> 7;
+          h[e][0] = ((n & 1u) | (n & 0x100u) << 8) * 0x7fc0u;
+          h[e][1] = ((n >> 16 & 1u) | (n >> 8 & 0x10000u)) * 0x7fc0u;
+        } else {
+          const uint2 y = *reinterpret_cast<const uint2*>(at);
+          h[e][0] = y.x;
+          h[e][1] = y.y;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t y = h[e][k / 2] >> (16 * (k & 1)), size = y & 0x7fffu;
+          if (size < 0x7f80u || !(see >> (i + e) & 1u)) continue;
+          if (size > 0x7f80u || !(y & 0x8000u)) up |= 1u << k;
+          if (size > 0x7f80u || (y & 0x8000u)) down |= 1u << k;
+        }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const bool u = up >> k & 1u, d = down >> k & 1u;
+    if (u || d) x[k] = u && d ? __builtin_nanf("") : u ? __builtin_inff() : -__builtin_inff();
+  }
+}
+
+// Whether four values are finite numbers.
+__device__ __forceinline__ bool all_finite(float a, float b, float c, float d) {
+  return fmaf(a, 0.f, fmaf(b, 0.f, fmaf(c, 0.f, d * 0.f))) == 0.f;
 }
 
 // Columns of output registers 4 k .. of block c (k = 0 .. 3), half hh's four.
@@ -715,6 +795,18 @@ __global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
   if (row >= rows) return;
   const int hh = lane >> 5;
   const float inv = 1.f / l;
+  if (__builtin_expect(!w.all_finite(), 0) && l - l == 0.f && cs.vs - cs.vs == 0.f) {
+#pragma unroll 1
+    for (int n = 0; n < D / 8; ++n) {
+      const int col = out_col<D, FP8>(n / 4, n % 4, hh);
+      float x[4] = {};
+      w.four(n, x);
+      if (all_finite(x[0], x[1], x[2], x[3])) continue;
+      settle_nonfinite<FP8>(a, ks, tt, my, b, vc + col * (FP8 ? 1 : 2), vn + col * 2, 0,
+                            (ks.cached.n + 31) / 32 + (ks.fresh.n + 31) / 32, x);
+      w.set_four(n, x);
+    }
+  }
   const int64_t out =
       ((static_cast<int64_t>(b) * a.N + my.node) * a.Hq + h * a.G + row % a.G) * D;
 #pragma unroll
@@ -950,6 +1042,13 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_stream_kernel(TreeArgs a) {
       s.z += x.z;
       s.w += x.w;
     }
+    if (__builtin_expect(!all_finite(s.x, s.y, s.z, s.w), 0) && lr - lr == 0.f && cs.vs - cs.vs == 0.f) {
+      float x[4] = {s.x, s.y, s.z, s.w};
+      settle_nonfinite<FP8>(a, ks, tt, tree_row(a, rq, ks, b, row), b, vc + 4 * g * (FP8 ? 1 : 2),
+                            vn + 8 * g, tree_cut(tiles, sp * NW, nsp * NW),
+                            tree_cut(tiles, sp * NW + NW, nsp * NW), x);
+      s = make_float4(x[0], x[1], x[2], x[3]);
+    }
     if (split) {
       float* p = part + (row - r0) * kPartRow<D>;
       *reinterpret_cast<float4*>(p + 4 * g) = s;
@@ -960,6 +1059,12 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_stream_kernel(TreeArgs a) {
       store4<F32>(a.out, out * D + 4 * g, s.x * inv, s.y * inv, s.z * inv, s.w * inv);
     }
   }
+}
+
+// acc plus a split's value x of weight w; an infinity or NaN counts whole, also
+// where w has underflowed.
+__device__ __forceinline__ float add_split(float x, float w, float acc) {
+  return x - x == 0.f ? fmaf(x, w, acc) : acc + x;
 }
 
 // Joins a row's splits: out = sum_s 2^(m_s - M) acc_s / sum_s 2^(m_s - M) l_s.
@@ -1007,7 +1112,7 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
       const float w = fast_exp2(pm[s] - M);
       L = fmaf(pl[s], w, L);
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = fmaf(px[s][e], w, acc[e]);
+      for (int e = 0; e < E; ++e) acc[e] = add_split(px[s][e], w, acc[e]);
     }
 #pragma unroll 4
   for (int s = kAhead; s < nsp; ++s) {
@@ -1015,7 +1120,7 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
     const float w = fast_exp2(x[D] - M);
     L = fmaf(x[D + 1], w, L);
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = fmaf(x[lane * E + e], w, acc[e]);
+    for (int e = 0; e < E; ++e) acc[e] = add_split(x[lane * E + e], w, acc[e]);
   }
   const float inv = 1.f / L;
   const int64_t to =

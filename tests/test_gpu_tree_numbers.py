@@ -59,3 +59,55 @@ def test_bf16_outputs_round_the_result_alone(kernel, d, kv):
                 worst = max(worst, err.max())
     say("  worst error over its bound", worst)
     assert worst <= 1.0
+
+
+CHAINS = {"stream": dict(batch=2, nodes=70, heads=(40, 40), grid=(15, 15), bases=[40, 90]),
+          "split": dict(batch=1, nodes=70, heads=(4, 4), grid=(40, 40), bases=[900]),
+          "four waves": dict(batch=1, nodes=70, heads=(100, 100), grid=(15, 15), bases=[90]),
+          "tiles": dict(batch=2, nodes=200, heads=(172, 172), grid=(20, 20), bases=[40, 90])}
+
+
+def chain(kernel, **kw):
+    pr = Problem(tree=False, prompt=200, **CHAINS[kernel], **kw)
+    info = B.tree_launch_info(pr.p, pr.s, pr.nodes)
+    assert (info.rows_per_tile == 128) == (kernel == "tiles")
+    assert (info.splits > 1) == (kernel == "split")
+    assert (info.workgroups > 256) == (kernel in ("four waves", "tiles"))
+    return pr
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+@pytest.mark.parametrize("out", ["fp32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kernel", list(CHAINS))
+def test_seen_infinities_are_infinities_in_any_tile(kernel, d, out, kv):
+    """Infinities and NaN of V rows in tiles that hide nothing, and where the
+    weights underflow: node 60's key outweighs all others by hundreds of powers of
+    two for about half of the queries.  What an element sees of them is what it is,
+    the other elements are as without."""
+    clean, pr = chain(kernel, d=d, out=out, kv=kv, seed=7), chain(kernel, d=d, out=out, kv=kv, seed=7)
+    for x in (clean, pr):
+        x.kn[:, 60] *= 1000
+    if kv == "bf16":
+        pr.v[:, :, 40, 5] = math.inf
+        pr.v[:, :, 41, 6] = -math.inf
+        pr.v[:, :, 42, 7] = math.inf
+        pr.v[:, :, 100, 7] = -math.inf
+        pr.v[:, :, 150, 8] = math.nan
+    else:
+        pr.v.view(torch.uint8)[:, :, 150, 8] = 0x7F
+        pr.vn[:, 2, :, 8] = math.inf
+    pr.vn[:, 3, :, 9] = math.inf
+    pr.vn[:, 4, :, 10] = -math.inf
+    pr.vn[:, 61, :, 10] = math.inf
+    want, got = clean.run().cpu(), pr.run().cpu()
+    full = {8: math.nan} if kv == "fp8" else {5: math.inf, 6: -math.inf, 7: math.nan, 8: math.nan}
+    for c, x in full.items():
+        assert (got[..., c].isnan() if math.isnan(x) else got[..., c] == x).all(), c
+    assert (got[:, 3:, :, 9] == math.inf).all()
+    assert (got[:, 4:61, :, 10] == -math.inf).all() and got[:, 61:, :, 10].isnan().all()
+    same = torch.ones_like(got, dtype=torch.bool)
+    same[..., list(full)] = False
+    same[:, 3:, :, 9] = False
+    same[:, 4:, :, 10] = False
+    assert torch.equal(got[same], want[same]) and want.isfinite().all()
