@@ -270,8 +270,8 @@ struct TreeWave {
   }
 
   // S^T of 32 keys: lane (lq, hh) gets row lq's scores of keys 8 (i / 4) + 4 hh +
-  // i % 4, negated where `flip`, -inf where `hides` and the row does not see them.
-  __device__ __forceinline__ void scores(int lane, const uint16_t* lk, bool flip, bool hides,
+  // i % 4, times `turn`, -inf where `hides` and the row does not see them.
+  __device__ __forceinline__ void scores(int lane, const uint16_t* lk, float turn, bool hides,
                                          uint32_t see, f32x16& sc) {
     const int hh = lane >> 5;
 #pragma unroll
@@ -281,9 +281,9 @@ struct TreeWave {
       const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lk + (lane & 31) * kKRow<D> + 16 * s + 8 * hh);
       sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], sc, 0, 0, 0);
     }
-    if (flip) {
+    if (turn != 1.f) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[i] = -sc[i];
+      for (int i = 0; i < 16; ++i) sc[i] *= turn;
     }
     if (hides) {
       const uint32_t w = see >> (4 * hh);
@@ -374,12 +374,12 @@ struct TreeWave {
     }
   }
 
-  // A tile of 32 keys.  sl: score scale (positive), flip: of negated scores; vs:
-  // scale of V; see: the keys each row sees, used where `hides`.
+  // A tile of 32 keys.  sl: score scale (positive), turn: what it lacks, -1 or NaN
+  // (else 1); vs: scale of V; see: the keys each row sees, used where `hides`.
   __device__ __forceinline__ void tile(int lane, const uint16_t* lk, const uint16_t* lv, float sl,
-                                       bool flip, float vs, bool hides, uint32_t see) {
+                                       float turn, float vs, bool hides, uint32_t see) {
     f32x16 sc;
-    scores(lane, lk, flip, hides, see, sc);
+    scores(lane, lk, turn, hides, see, sc);
     raise<false>(sl, sc, sc);
     weights(sl, vs, sc);
     values(lane, lv, sc);
@@ -388,12 +388,12 @@ struct TreeWave {
   // 64 keys: the second half's scores are under way while the first's
   // weights are computed, and the first half's values while the second's are.
   __device__ __forceinline__ void tile2(int lane, const uint16_t* lk, const uint16_t* lv, float sl,
-                                        bool flip, float vs, bool hides,
+                                        float turn, float vs, bool hides,
                                         const uint32_t (&see)[2]) {
     f32x16 s0, s1;
-    scores(lane, lk, flip, hides, see[0], s0);
+    scores(lane, lk, turn, hides, see[0], s0);
     raise<false>(sl, s0, s0);
-    scores(lane, lk + 32 * kKRow<D>, flip, hides, see[1], s1);
+    scores(lane, lk + 32 * kKRow<D>, turn, hides, see[1], s1);
     weights(sl, vs, s0);
     raise<true>(sl, s1, s0);
     values(lane, lv, s0);
@@ -458,20 +458,20 @@ struct TreeWave {
 };
 
 // Scales of the scores and of V over the cache.  Scores are compared before they
-// are scaled, so the scale is positive: a negative one flips the scores, a
-// zero one is as good as the smallest.
+// are scaled, so the scale is positive: a negative one turns the scores, a
+// zero one is as good as the smallest, and a NaN makes the scores NaN before the
+// hidden ones are left out.
 struct CacheScale {
-  float sl, vs;
-  bool flip;
+  float sl, vs, turn;
 };
 template <bool FP8>
 __device__ __forceinline__ CacheScale cache_scale(const TreeArgs& a, int pair) {
-  CacheScale c{a.scale_log2, 1.f, false};
+  CacheScale c{a.scale_log2, 1.f, 1.f};
   if constexpr (FP8) {
     if (a.ks) c.sl *= a.ks[pair];
     if (a.vs) c.vs = a.vs[pair];
-    c.flip = c.sl < 0.f;
-    c.sl = fmaxf(fabsf(c.sl), kTreeMinScale);
+    c.turn = c.sl != c.sl ? c.sl : c.sl < 0.f ? -1.f : 1.f;
+    c.sl = fmaxf(fabsf(c.sl), kTreeMinScale);  // (the smallest for a NaN)
   }
   return c;
 }
@@ -763,7 +763,7 @@ __global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
         uint32_t see[2] = {};
         const bool hide = hides(t);
         if (hide) see_of(t, see);
-        w.tile2(lane, lk[buf], lv[buf], cs.sl, cs.flip, cs.vs, hide, see);
+        w.tile2(lane, lk[buf], lv[buf], cs.sl, cs.turn, cs.vs, hide, see);
         if (hide) add_hidden(t, buf, see, std::true_type());
       }
       __syncthreads();
@@ -783,7 +783,7 @@ __global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
       uint32_t see[2] = {};
       const bool hide = hides(t);
       if (hide) see_of(t, see);
-      w.tile2(lane, lk[buf], lv[buf], a.scale_log2, false, 1.f, hide, see);
+      w.tile2(lane, lk[buf], lv[buf], a.scale_log2, 1.f, 1.f, hide, see);
       if (hide) add_hidden(t, buf, see, std::false_type());
     }
     __syncthreads();
@@ -945,7 +945,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_stream_kernel(TreeArgs a) {
       bad = clean_rows<D, NP>(rv + set, lv + (lane / CPR) * kVRow<D> + c * 8, RPP * kVRow<D>);
     next();
     fence_wave();
-    w.tile(lane, lk, lv, a.scale_log2, false, 1.f, hide, see);
+    w.tile(lane, lk, lv, a.scale_log2, 1.f, 1.f, hide, see);
     add_hidden(bad, see, std::false_type(), [&](int e) {
       return old ? vc + ks.cached.near(e0 + e) * a.sr : vn + ks.fresh.near(e0 + e) * a.nsn * 2;
     });
@@ -974,7 +974,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_stream_kernel(TreeArgs a) {
         }
         if (t + j + PF < end8) load8(t + j + PF, j * N);
         fence_wave();
-        w.tile(lane, lk, lv, cs.sl, cs.flip, cs.vs, hide, see);
+        w.tile(lane, lk, lv, cs.sl, cs.turn, cs.vs, hide, see);
         add_hidden(bad, see, std::true_type(),
                    [&](int e) { return vc + ks.cached.near(e0 + e) * a.sr; });
         fence_wave();

@@ -111,3 +111,34 @@ def test_seen_infinities_are_infinities_in_any_tile(kernel, d, out, kv):
     same[:, 3:, :, 9] = False
     same[:, 4:, :, 10] = False
     assert torch.equal(got[same], want[same]) and want.isfinite().all()
+
+
+SCALED = {"stream": dict(nodes=30, heads=(4, 4)), "groups": dict(nodes=40, heads=(8, 2)),
+          "split": dict(batch=1, nodes=30, heads=(4, 4), grid=(40, 40)),
+          "tiles": dict(nodes=90, heads=(172, 172))}
+
+
+@pytest.mark.parametrize("which", ["k_scale"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kernel", list(SCALED))
+def test_nan_cache_scale_is_a_nan(kernel, d, which):
+    """Of an fp8 cache: in every node that attends a cached row of the pair, and in
+    no other one."""
+    case = dict(grid=(12, 12), bases=[100, 60][:SCALED[kernel].get("batch", 2)], d=d, kv="fp8",
+                tree=False, mode="dense", seed=d)
+    case.update(SCALED[kernel])
+    for window in (None, 7):
+        if window:  # nodes from the seventh on attend new rows alone
+            case.update(mode="window", n_att=7, prompt=0)
+        clean, pr = Problem(**case), Problem(**case)
+        pairs = torch.arange(pr.batch * pr.hkv, device=pr.k.device)
+        getattr(pr, which)[pairs % 2 == 1] = math.nan
+        want, got = clean.run().cpu(), pr.run().cpu()
+        g = pr.hq // pr.hkv
+        for b in range(pr.batch):
+            for h in range(pr.hkv):
+                bad = (b * pr.hkv + h) % 2 == 1
+                n = min(pr.nodes, window - 1 if window else pr.nodes) if bad else 0
+                assert got[b, :n, h * g:h * g + g].isnan().all(), (b, h)
+                assert torch.equal(got[b, n:, h * g:h * g + g], want[b, n:, h * g:h * g + g]), (b, h)
+        assert want.isfinite().all()
