@@ -320,13 +320,21 @@ struct TreeWave {
     }
   }
 
-  // Scores to weights, in place.
+  // Scores to weights, in place, times V's scale.  A hidden key's weight of 0 stays one
+  // where that is infinite or NaN.
   __device__ __forceinline__ void weights(float sl, float vs, f32x16& sc) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       sc[i] = fast_exp2(fmaf(sc[i], sl, -m));
       l += sc[i];
-      if (vs != 1.f) sc[i] *= vs;
+    }
+    if (vs == 1.f) return;
+    if (__builtin_expect(vs - vs == 0.f, 1)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] *= vs;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = sc[i] == 0.f ? 0.f : sc[i] * vs;
     }
   }
 

@@ -118,7 +118,7 @@ SCALED = {"stream": dict(nodes=30, heads=(4, 4)), "groups": dict(nodes=40, heads
           "tiles": dict(nodes=90, heads=(172, 172))}
 
 
-@pytest.mark.parametrize("which", ["k_scale"])
+@pytest.mark.parametrize("which", ["k_scale", "v_scale"])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("kernel", list(SCALED))
 def test_nan_cache_scale_is_a_nan(kernel, d, which):
