@@ -430,7 +430,8 @@ def _own_pass(st):
                       for i in range(c["layers"])]
             h["layouts"] = [B.kv_layout(st.k[i], ring_rows=_ring_rows(c), k_scale=scales[i][0],
                                         v_scale=scales[i][1]) for i in range(c["layers"])]
-            h["layout"] = h["layouts"][0]
+            h["layout"] = B.kv_layout(st.k[0], ring_rows=_ring_rows(c), k_scale=st.k_scale,
+                                      v_scale=st.v_scale)  # an append's, of all layers
             if c["op"] != "append":
                 n = B.tree_workspace_bytes(h["p"], h["s"], c["nodes"])
                 h["ws"] = torch.empty(n, dtype=torch.uint8, device="cuda") if n else None
