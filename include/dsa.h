@@ -586,7 +586,8 @@ DSA_API dsa_status dsa_tree_plan(int32_t batch, int32_t nodes, const int32_t* d_
  *   d_q              bf16 rows (q_rows), query head h of node i
  *   d_k_new, d_v_new bf16 rows (new_rows), KV head h of node i
  *   d_k, d_v, kv     caches as for dsa_decode_attention, holding the positions
- *                    before base_b that a node can attend
+ *                    before base_b that a node can attend (kv's scales: the
+ *                    layer's, [B*Hkv])
  *   d_out            [B][N][Hq][d] in out_type, 16-byte aligned; rows of nodes
  *                    past a request's count are left as they are
  *   d_ws, ws_bytes   dsa_tree_workspace_bytes() bytes, 16-byte aligned; need not be
@@ -651,7 +652,8 @@ DSA_API dsa_status dsa_tree_verify(int32_t batch, int32_t vocab, const dsa_tree*
  *               outside the request's nodes is skipped.
  *   d_accepted  int32 [B] (clamped to the request's count), or NULL: the count
  *   d_k, d_v    caches; layer l starts l * stride_layer elements in.  kv's
- *               scales are [layers][B*Hkv].
+ *               scales are those of all layers, [layers][B*Hkv]: another
+ *               layout than the attention's of a layer.
  * In a ring, of rows that share a slot the last is written.  Positions at or
  * past H*W and unused slots write nothing.
  * All modes are allowed (a decode step appends its token with N = 1).

@@ -63,6 +63,8 @@ class KVLayout(C.Structure):
                 ("stride_head", C.c_int64), ("stride_row", C.c_int64),
                 ("ring_rows", C.c_int64), ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p),
                 ("dtype", C.c_int32)]
+    # values of the tensors that ``kv_layout`` was given (no bound is known of raw pointers)
+    scales = bases = 1 << 62
 
 
 class PlanLayout(C.Structure):
@@ -242,6 +244,15 @@ def _sizes(p, s):
     return z
 
 
+def _need_extents(layout, requests, heads, layers=1):
+    """The layout's scales and row bases are those of all pairs that the call reads."""
+    if layout.scales < layers * requests * heads:
+        raise ValueError(f"the layout holds {layout.scales} scales, the call reads {layers} layers "
+                         f"x {requests} requests x {heads} KV heads of them")
+    if layout.bases < requests:
+        raise ValueError(f"the layout holds {layout.bases} row bases of {requests} requests")
+
+
 def _need_state(z, state):
     _check(z[0], "dsa_get_state_layout")
     _need(state, "state", None, z[3])
@@ -257,6 +268,7 @@ def _check_decode_args(p, s, q, k, v, layout, decode_pos, out, window_logits):
     _need(window_logits, "window_logits", torch.float32, z[1])
     _need(k, "k", _KV_DTYPES, contiguous=False)
     _need(v, "v", _KV_DTYPES, contiguous=False)
+    _need_extents(layout, B_, Hkv)
     if isinstance(k, torch.Tensor) and isinstance(v, torch.Tensor):
         shape = k.shape
         if k.dtype != v.dtype or shape != v.shape or k.stride() != v.stride():
@@ -354,18 +366,31 @@ def kv_layout(k: torch.Tensor, row_base: Optional[torch.Tensor] = None,
     for the ``S`` sinks and at ``L_p + S + (j - S) % (R - S)`` after them.
     A bf16 cache is ``torch.bfloat16``; an fp8 (OCP E4M3) cache is
     ``torch.float8_e4m3fn`` or its bytes as ``torch.uint8``, with optional
-    fp32 ``k_scale``/``v_scale`` of ``B * Hkv`` values."""
+    fp32 ``k_scale``/``v_scale`` of ``B * Hkv`` values; a layout for
+    ``kv_append`` of several layers takes those of all of them, ``[layers,
+    B * Hkv]``, and each layer's attention a layout with its own.  The layout
+    keeps the tensors it points to."""
     sb, sh, sr, sd = k.stride()
     if sd != 1:
         raise ValueError("head_dim must be contiguous")
+    _need(row_base, "row_base", torch.int64)
+    _need(k_scale, "k_scale", torch.float32)
+    _need(v_scale, "v_scale", torch.float32)
     if k.dtype == torch.bfloat16:
         dtype = KV_BF16
     elif k.dtype in (torch.uint8, torch.float8_e4m3fn):
         dtype = KV_FP8_E4M3
     else:
         raise ValueError(f"unsupported KV dtype {k.dtype}")
-    return KVLayout(_ptr(row_base), sb, sh, sr, int(ring_rows), _ptr(k_scale), _ptr(v_scale),
-                    dtype)
+    out = KVLayout(_ptr(row_base), sb, sh, sr, int(ring_rows), _ptr(k_scale), _ptr(v_scale),
+                   dtype)
+    out._held = (row_base, k_scale, v_scale)
+    held = [x.numel() for x in (k_scale, v_scale) if isinstance(x, torch.Tensor)]
+    if held:
+        out.scales = min(held)
+    if isinstance(row_base, torch.Tensor):
+        out.bases = row_base.numel()
+    return out
 
 
 def decode_attention(p, s, q, k, v, layout: KVLayout, decode_pos, plan_buf, sm_scale, out,
@@ -564,6 +589,7 @@ def _check_caches(p, s, k, v, layout, rows_needed, layers, device):
         raise ValueError(f"the layout is not of a {k.dtype} cache")
     if layers is not None and (len(shape) != 5 or shape[0] != layers):
         raise ValueError(f"the caches must be of {layers} layers, got shape {tuple(shape)}")
+    _need_extents(layout, s.batch, s.num_kv_heads, layers or 1)
     if len(shape) >= 4 and layout.d_row_base is None:
         nb, nh, rows, nd = shape[-4:]
         if (nb < s.batch or nh < s.num_kv_heads or nd != s.head_dim or rows < rows_needed

@@ -142,3 +142,46 @@ def test_nan_cache_scale_is_a_nan(kernel, d, which):
                 assert got[b, :n, h * g:h * g + g].isnan().all(), (b, h)
                 assert torch.equal(got[b, n:, h * g:h * g + g], want[b, n:, h * g:h * g + g]), (b, h)
         assert want.isfinite().all()
+
+
+def test_layouts_with_too_few_scales_are_refused():
+    """Before any kernel reads them: one layer's scales for an append of three layers,
+    one request's for two, row bases likewise; scales of another type or order."""
+    pr = Problem(nodes=6, kv="fp8")
+    layers = 3
+    k, v = (x.unsqueeze(0).repeat(layers, 1, 1, 1, 1) for x in (pr.k.view(torch.uint8),
+                                                               pr.v.view(torch.uint8)))
+    kn, vn = (x.unsqueeze(0).repeat(layers, 1, 1, 1, 1) for x in (pr.kn, pr.vn))
+    scales = pr.k_scale.repeat(layers, 1)
+    n = pr.k_scale.numel()
+
+    def append(**kw):
+        B.kv_append(pr.p, pr.s, pr.tree, kn, vn, k, v, B.kv_layout(k[0], **kw))
+
+    for ks, vs in ((scales[0], scales[0]), (scales, scales[0]), (scales[1], None),
+                   (scales[:2], scales)):
+        with pytest.raises(ValueError):
+            append(k_scale=ks, v_scale=vs)
+    before = k.clone()
+    append(k_scale=scales, v_scale=scales)
+    assert not torch.equal(k, before)
+
+    def attend(**kw):
+        B.tree_attention(pr.p, pr.s, pr.tree, pr.q, pr.kn, pr.vn, pr.k, pr.v,
+                         B.kv_layout(pr.k, **kw), pr.scale, pr.out, pr.ws)
+
+    base = torch.zeros(1, dtype=torch.int64, device=pr.k.device)
+    for kw in (dict(k_scale=pr.k_scale[:n - 1]), dict(v_scale=pr.v_scale[:1]),
+               dict(row_base=base)):
+        with pytest.raises(ValueError):
+            attend(**kw)
+    bufs = B.alloc_buffers(pr.p, pr.s)
+    with pytest.raises(ValueError):
+        B.decode_attention(pr.p, pr.s, pr.q[:, 0].contiguous(), pr.k, pr.v,
+                           B.kv_layout(pr.k, k_scale=pr.k_scale[:1]), pr.base, None, pr.scale,
+                           bufs.out, None, bufs.workspace)
+    for kw in (dict(k_scale=pr.k_scale.half()), dict(v_scale=scales.t()),
+               dict(k_scale=pr.k_scale.cpu()), dict(row_base=base.int())):
+        with pytest.raises(ValueError):
+            B.kv_layout(pr.k, **kw)
+    attend(k_scale=pr.k_scale, v_scale=pr.v_scale)

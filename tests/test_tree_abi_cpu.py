@@ -204,3 +204,18 @@ def test_a_tree_keeps_its_tensors():
 def test_plan_needs_a_buffer():
     with pytest.raises(ValueError):
         B.tree_plan(torch.zeros((2, 4), dtype=torch.int32), None, None)
+
+
+def test_layouts_know_how_many_scales_they_hold():
+    """A layout of one layer's scales is not one for an append of several layers."""
+    lay = B.kv_layout(torch.zeros((2, 4, 120, 64), dtype=torch.uint8))
+    B._need_extents(lay, 2, 4, 1000)  # none: nothing is read
+    lay.scales, lay.bases = 8, 2
+    B._need_extents(lay, 2, 4)
+    B._need_extents(lay, 1, 4, 2)
+    for wrong in ((2, 4, 2), (3, 4), (2, 8)):
+        with pytest.raises(ValueError):
+            B._need_extents(lay, *wrong)
+    lay.scales = 1 << 20
+    with pytest.raises(ValueError):
+        B._need_extents(lay, 3, 4)
