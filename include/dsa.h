@@ -654,8 +654,8 @@ DSA_API dsa_status dsa_tree_verify(int32_t batch, int32_t vocab, const dsa_tree*
  *   d_k, d_v    caches; layer l starts l * stride_layer elements in.  kv's
  *               scales are those of all layers, [layers][B*Hkv]: another
  *               layout than the attention's of a layer.
- * In a ring, of rows that share a slot the last is written.  Positions at or
- * past H*W and unused slots write nothing.
+ * In a ring, of rows that share a slot the last is written (a skipped entry is
+ * none).  Positions at or past H*W and unused slots write nothing.
  * All modes are allowed (a decode step appends its token with N = 1).
  * Errors: INVALID_ARG, UNSUPPORTED, HIP.
  */

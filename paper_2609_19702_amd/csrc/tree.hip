@@ -353,13 +353,16 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, int chunks, i
   if (e >= n) return;
   const int pos = rq.base + e, last = min(rq.base + n, a.Ldec) - 1;
   if (pos >= a.Ldec) return;
+  const int32_t* path = a.path ? a.path + b * static_cast<int64_t>(a.N) : nullptr;
+  const int node = path ? path[e] : e;
+  if (node < 0 || node >= rq.n) return;
   int row = a.Lp + pos;
   if (a.ring && pos >= a.S) {
-    if (pos + a.ring <= last) return;  // a later row of this call takes the slot
+    // a later row of this call takes the slot, but for one that is skipped
+    for (int f = e + a.ring; rq.base + f <= last; f += a.ring)
+      if (!path || (path[f] >= 0 && path[f] < rq.n)) return;
     row = a.Lp + a.S + (pos - a.S) % a.ring;
   }
-  const int node = a.path ? a.path[b * static_cast<int64_t>(a.N) + e] : e;
-  if (node < 0 || node >= rq.n) return;
   const int64_t from = layer * a.nsl + b * a.nsb + node * a.nsn + h * a.nsh + c * 8;
   const int64_t base = layer * a.sl + (a.row_base ? a.row_base[b] * (FP8 ? 1 : 2) : b * a.sb) +
                        h * a.sh + row * a.sr + c * (FP8 ? 8 : 16);
