@@ -488,7 +488,9 @@ DSA_API dsa_status dsa_select(const dsa_params* p, const dsa_shape* s, const int
  *            dsa_tree_verify, else at most 1 << 20
  *   d_base   int32 [B]: base_b.  A request with base_b < -L_p is an unused
  *            slot (as one with count 0); base_b > H*W is taken as H*W.
- *            dsa_tree_verify does not read it (may be NULL there).
+ *            dsa_tree_verify does not read it (may be NULL there): an unused
+ *            slot of a step with verification has count 0, so that nothing of
+ *            it is accepted and base_b, advanced by that, stays.
  *   d_count  int32 [B]: request b has nodes 0 .. d_count[b] - 1 (clamped to
  *            [0, N]); NULL: all N.  Nothing is read or written for the others.
  *   d_plan   buffer filled by dsa_tree_plan from the nodes' parents, or NULL:
@@ -627,9 +629,9 @@ DSA_API dsa_status dsa_tree_attention(const dsa_params* p, const dsa_shape* s,
  *                 children of node c were drawn from
  *   d_uniform     fp32 [B][N + 1] in [0, 1): one per node, one for the next token
  *   d_path        int32 [B][N], out: the accepted nodes, node 0 first, then -1
- *   d_accepted    int32 [B], out: how many (0 for an unused slot)
- *   d_next        int32 [B], out: the next token (-1 for an unused slot, or a
- *                 target row without any mass)
+ *   d_accepted    int32 [B], out: how many (0 for a request of count 0)
+ *   d_next        int32 [B], out: the next token (-1 for a request of count 0, or
+ *                 a target row without any mass)
  * Where max(P - draft, 0) has no mass left, P keeps its last value with mass
  * for the next token, and no further child of c is accepted.  Negative and NaN
  * probabilities count as 0.

@@ -470,8 +470,9 @@ _OUT_TYPES = {torch.float32: 0, torch.bfloat16: 1}  # DSA_OUT_FP32, DSA_OUT_BF16
 class Tree:
     """New tokens of every request (``dsa_tree``): ``nodes`` per request at
     most, ``base`` the decode position of each request's first (int32 [B]),
-    ``count`` how many of them each has (int32 [B]; all), ``plan`` a buffer
-    filled by ``tree_plan`` (a chain).  Keeps the tensors it points to; they
+    ``count`` how many of them each has (int32 [B]; all; 0 for an unused slot,
+    which ``tree_verify`` knows by nothing else), ``plan`` a buffer filled by
+    ``tree_plan`` (a chain).  Keeps the tensors it points to; they
     can be written, not exchanged."""
 
     def __init__(self, nodes, base=None, count=None, plan=None):
