@@ -595,7 +595,10 @@ DSA_API dsa_status dsa_tree_plan(int32_t batch, int32_t nodes, const int32_t* d_
  *   d_ws, ws_bytes   dsa_tree_workspace_bytes() bytes, 16-byte aligned; need not be
  *                    cleared
  * Algorithm 1 chooses what a token keeps from the step before it, one token
- * at a time: DSA_MODE_DIAGONAL is refused (a prompt goes in dense mode).
+ * at a time: DSA_MODE_DIAGONAL is refused.  What goes in before a diagonal run
+ * goes in dense mode: the prompt, and up to N_att - 1 of the image's tokens, whose
+ * steps keep everything and select nothing.  After more of them the selection
+ * state lacks their entries, and the next step is flagged DSA_FLAG_STATE_BEHIND.
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
  */
 DSA_API dsa_status dsa_tree_attention(const dsa_params* p, const dsa_shape* s,

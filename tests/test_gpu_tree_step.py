@@ -257,3 +257,55 @@ def test_appended_rows_feed_a_decode_step():
                 outs.append(bufs.out.clone())
         results.append(torch.stack(outs))
     assert torch.equal(results[0], results[1])
+
+
+@pytest.mark.parametrize("given", [1, 5, 8, 9, 12])
+def test_known_tokens_before_a_diagonal_run(given):
+    """An image's first tokens in one dense chunk, then diagonal steps: with up to
+    N_att - 1 of them every later step is what it is after single steps, and the
+    chunk's outputs are the steps' (both fp32, the steps' weights in two bf16 terms:
+    2^-15 apart); with more the next step is flagged."""
+    batch, hkv, d, lp, grid, n_att = 2, 4, 64, 11, (8, 8), 9
+    p = B.make_params(lp, *grid, 24, n_att, B.MODE_DIAGONAL, 2)
+    dense = B.make_params(lp, *grid, 1, 1, B.MODE_DENSE)
+    s = B.make_shape(batch, hkv, hkv, d)
+    g = torch.Generator().manual_seed(6)
+    x = torch.randn((batch, lp + 40, 2 * hkv, d), generator=g).bfloat16().to(DEV)
+    q = torch.randn((40, batch, hkv, d), generator=g).bfloat16().to(DEV)
+    results, flags = [], []
+    for n in (0, given):
+        k, v = (torch.zeros((batch, hkv, lp + 64, d), dtype=torch.bfloat16, device=DEV)
+                for _ in range(2))
+        lay = B.kv_layout(k)
+        bufs = B.alloc_buffers(p, s, DEV)
+        B.state_reset(p, s, bufs.state)
+        append = lambda a, b: B.kv_append(  # noqa: E731
+            p, s, B.make_tree(b - a, ints([a - lp] * batch)), x[:, a:b, :hkv], x[:, a:b, hkv:], k,
+            v, lay)
+        append(0, lp)
+        out = torch.zeros((batch, 40, hkv, d), device=DEV)
+        if n:
+            size = B.tree_workspace_bytes(dense, s, n)
+            ws = torch.empty(size, dtype=torch.uint8, device=DEV) if size else None
+            part = torch.empty((batch, n, hkv, d), device=DEV)
+            B.tree_attention(dense, s, B.make_tree(n, ints([0] * batch)),
+                             q[:n].transpose(0, 1).contiguous(), x[:, lp:lp + n, :hkv],
+                             x[:, lp:lp + n, hkv:], k, v, lay, 0.125, part, ws)
+            out[:, :n] = part
+            append(lp, lp + n)
+        behind = []
+        for t in range(n, 40):
+            append(lp + t, lp + t + 1)
+            B.decode_step(p, s, q[t], k, v, lay, ints([t] * batch), bufs.state, bufs.plan, 0.125,
+                          bufs.out, bufs.logits, bufs.workspace)
+            out[:, t] = bufs.out
+            behind.append(bool((B.state_views(p, s, bufs.state)[1] & B.FLAG_STATE_BEHIND).any()))
+        results.append(out)
+        flags.append(behind)
+    assert not any(flags[0])
+    if given < n_att:
+        assert not any(flags[1])
+        assert torch.equal(results[0][:, given:], results[1][:, given:])
+        assert (results[0] - results[1]).abs().max() <= 2 ** -15 * x[..., hkv:, :].abs().max()
+    else:
+        assert flags[1][0]
