@@ -44,3 +44,26 @@ def test_two_graphs_share_a_workspace():
         torch.cuda.synchronize()
         assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])
         a.ws.fill_(255)
+
+
+def test_each_of_two_calls_at_once_writes_its_results():
+    """An output of its own, filled before, for every call on either stream; the
+    expected ones are checked against fp64."""
+    a, b = Problem(seed=1, bases=[900], **SPLIT), Problem(seed=2, kv="fp8", out="bf16", bases=[1200],
+                                                         **SPLIT)
+    want = []
+    for x in (a, b):
+        x.run()
+        x.check(nodes=[0, 7, 15], kv_heads=[0, 7])
+        want.append(x.out.clone())
+    outs = [[torch.full_like(x.out, 7.0) for _ in range(20)] for x in (a, b)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    for i in range(20):
+        for x, st, got in zip((a, b), streams, outs):
+            x.out = got[i]
+            x.run(stream=st)
+    torch.cuda.synchronize()
+    for got, w in zip(outs, want):
+        assert all(torch.equal(y, w) for y in got)
