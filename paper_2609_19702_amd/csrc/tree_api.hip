@@ -75,10 +75,16 @@ dsa_status tree_derive(const dsa_params* p, const dsa_shape* s, int nodes, Deriv
 // The keys of a streaming row tile are split where the row tiles alone would leave
 // CUs without a workgroup: into about eight, a tile per wave or more (40 tiles of
 // d = 128, 32 heads: 12.4 us; at two tiles per wave 14.7), and more of them at two tiles
-// per wave (136 tiles, 8 heads: 16 us; at one 17, at four 19, unsplit 45).  A split
-// costs a row of partial results and a second kernel, so few bytes stay whole: at
-// d = 64, 17 tiles take 8.3 us whole and 8.8 split, 26 take 10.5 and 9.3; at d = 128,
-// 13 take 10.8 and 10.6, 29 take 13.9 and 12.3.
+// per wave (136 tiles, 8 heads: 16 us; at one 17, at four 19, unsplit 45).
+//
+// A split costs a row of partial results and a second kernel: 2.9 us more for a call
+// from the host (19.8 us whole and 22.7 split, up to 40 tiles), and on replays what two
+// tiles per wave take.  One more tile per wave costs a replay 1.0 us at d = 64 and 2.3
+// at d = 128, the next one as much again; so up to three stay whole at d = 64, where
+// that is a third of a launch, and up to two at d = 128.  Replayed, 20 heads, whole and
+// split: d = 64, 16 tiles 8.9 and 9.1 us, 18 to 24 9.8 to 10.5 and 9.1 to 9.3, 26 11.5
+// and 9.2; d = 128, 10 to 16 tiles 10.9 to 11.6 and 10.7 to 11.5, 18 13.5 and 11.3.
+// (4, 32 and 64 heads, and 8 with four query heads each, step at the same places.)
 TreeLaunch tree_launch(const Derived& d, int nodes) {
   TreeLaunch l{};
   const int64_t rows = static_cast<int64_t>(nodes) * d.G;
@@ -97,7 +103,8 @@ TreeLaunch tree_launch(const Derived& d, int nodes) {
                        int64_t{nodes};
   const int64_t tiles = (keys + 31) / 32 + 2;
   const int64_t want = std::max<int64_t>(1, 256 / l.workgroups);
-  const int64_t least = tiles * d.D <= 1536
+  const int64_t per_wave = (tiles + l.waves - 1) / l.waves;
+  const int64_t least = (per_wave - 2) * d.D <= 64
                             ? tiles
                             : std::clamp<int64_t>(tiles / 8, l.waves, 2 * l.waves);
   l.split_tiles = static_cast<int>(std::max(least, (tiles + want - 1) / want));

@@ -219,3 +219,15 @@ def test_layouts_know_how_many_scales_they_hold():
     lay.scales = 1 << 20
     with pytest.raises(ValueError):
         B._need_extents(lay, 3, 4)
+
+
+@pytest.mark.parametrize("heads", [1, 4, 20, 32, 64])
+def test_few_tiles_per_wave_stay_whole(heads):
+    """Up to three of d = 64 and two of d = 128, whatever the number of heads."""
+    for d, most in ((64, 24), (128, 16)):
+        for tiles in range(4, 60):
+            keys = (tiles - 2) * 32  # two more where lists end inside a tile
+            for more in (0, -31):
+                p = params(prompt_len=keys + more - 7 - 4, grid_h=2, grid_w=2)
+                i = B.tree_launch_info(p, shape(1, heads, heads, d), 7)
+                assert (i.splits == 1) == (tiles <= most), (d, tiles)
