@@ -66,16 +66,17 @@ dsa_status tree_derive(const dsa_params* p, const dsa_shape* s, int nodes, Deriv
 
 // Two kernels.  Up to 64 query rows per (request, KV head), and more of them where
 // the chip holds all their tiles at once (two workgroups on each of 256 CUs), stream
-// the keys for 32 rows at a time (tree_stream_kernel): 512 nodes of 32 heads over 8
-// after 2256 keys, d = 128: 49 us, 86 through LDS; 30 nodes of 16 requests: 35
-// and 54; but of 32 requests: 73 and 47 (with 13 nodes, two row tiles: bf16 75 and 70,
-// fp8 52 and 74).  The others go through LDS for 128 rows at a time
-// (tree_tile_kernel).
+// the keys for 32 rows at a time (tree_stream_kernel).  32 heads over 8, d = 128, bf16
+// outputs, streamed and through LDS: 512 nodes after 2256 keys 57 and 94 us; 30
+// nodes of 16 requests (512 tiles) after 256 to 802 keys 26 and 37, after 256 to 4322 77
+// and 140; of 32 requests 46 and 41, 137 and 143, of 48 67 and 49, 206 and 161; 13
+// nodes of 32 requests (two row tiles) 89 and 141, fp8 67 and 151.  The others go
+// through LDS for 128 rows at a time (tree_tile_kernel).
 //
 // The keys of a streaming row tile are split where the row tiles alone would leave
 // CUs without a workgroup: into about eight, a tile per wave or more (40 tiles of
-// d = 128, 32 heads: 12.4 us; at two tiles per wave 14.7), and more of them at two tiles
-// per wave (136 tiles, 8 heads: 16 us; at one 17, at four 19, unsplit 45).
+// d = 128, 32 heads: 14.1 us; at two tiles per wave 15.4), and more of them at two tiles
+// per wave (139 tiles, 8 heads: 17.5 us; at one 19.3, at four 21.3, unsplit 48.5).
 //
 // A split costs a row of partial results and a second kernel: 2.9 us more for a call
 // from the host (19.8 us whole and 22.7 split, up to 40 tiles), and on replays what two
@@ -96,8 +97,8 @@ TreeLaunch tree_launch(const Derived& d, int nodes) {
   l.workgroups = pairs * l.row_tiles;
   if (!stream) return l;
   // Twice the waves on the keys where at most one workgroup per CU has work (32
-  // heads, d = 128, 552 keys, 16 nodes, whole: 13.9 us with eight waves, 14.5 with four);
-  // with more, what a CU holds at a time decides (32 such requests: 71 and 60).
+  // heads, d = 128, 552 keys, 16 nodes, whole: 14.6 us with eight waves, 15.2 with four);
+  // with more, what a CU holds at a time decides (32 such requests: 62.3 and 57.3).
   l.waves = l.workgroups <= 256 ? 8 : 4;
   const int64_t keys = d.Lp + (d.mode == DSA_MODE_WINDOW ? std::min(d.Natt, d.Ldec) : d.Ldec) +
                        int64_t{nodes};

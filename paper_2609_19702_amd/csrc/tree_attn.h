@@ -80,9 +80,10 @@ __device__ __forceinline__ uint32_t low_bits(int x) {
 // per_pair workgroups, which share K and V.  Workgroup ids go round the eight XCDs,
 // each with an L2 of its own, so a pair stays on one XCD, and neighbouring pairs (a
 // request's heads, with its length) go to different ones.  Where the pairs do not
-// go evenly round, the workgroups are cut into eight equal runs instead.  (All
-// heads of a request on one XCD: 62.3 us where this takes 59.9 for 32 ragged
-// requests of 32 heads, 41.9 and 38.8 for 16 ragged prompts.)
+// go evenly round, the workgroups are cut into eight equal runs instead.  (Equal
+// runs for all, a request's heads on one XCD: 49.5 us where this takes 43.4 for 16
+// ragged prompts, 68.2 and 61.8 for 24 trees of 61 nodes, 76.3 and 73.5 for 32 ragged
+// fp8 requests; 60.0 both for 32 ragged requests of one row tile.)
 struct TreeItem {
   int pair, sub;  // pair < 0: nothing to do
 };
@@ -107,8 +108,8 @@ inline uint32_t tree_grid(int64_t pairs, int64_t per_pair) {
 // most work (row tiles times keys) first, so that long ones neither share a CU nor
 // come last; every wave ranks them for itself, a request per lane.  Where
 // arithmetic and not bytes bound the kernel: 32 ragged requests of 8 KV heads, 13
-// nodes, fp8: 66.5 us a layer instead of 69; 24 of 61 nodes over a ring: 56.4 and
-// 62.7; equal requests lose 1 us.
+// nodes, fp8: 73.5 us a layer instead of 75.7; 24 of 61 nodes over a ring: 61.8 and
+// 67.1; 16 ragged prompts: 43.4 and 47.1.
 struct TreePlace {
   int b;
   TreeReq rq;
@@ -624,12 +625,12 @@ constexpr int kTileRows = 128;  // query rows of a workgroup
 // four waves, two buffers in turn.
 //
 // Bound by the waves' own instructions: two images of 4096 tokens at once (32 heads
-// over 8, d = 128, bf16 outputs) take 471 us, 0.66 PFLOP/s, where a library product
-// of 8192^3 reaches 1.19.  With the weights in one bf16 term they took 375: 286 for
-// the arithmetic without loads and stores to LDS (the matrix cores busy for a third
-// of the time, the softmax's exponentials, maxima and packing beside them), 51 for
-// the loads, 32 for the LDS stores; the second term's products and packing take the
-// rest.  Measured with one term and left: 64 rows per wave (490 us: one wave per
+// over 8, d = 128, bf16 outputs) take 465 to 478 us, 0.66 PFLOP/s, where a library
+// product of 8192^3 reaches 1.19; the matrix cores are busy for 43 % of the time, the
+// softmax's exponentials, maxima and packing beside them.  With the weights in one
+// bf16 term they took 375: 286 for the arithmetic without loads and stores to LDS, 51
+// for the loads, 32 for the LDS stores.  The second term adds half as many products
+// and 49 instructions per 32 keys.  Measured with one term and left: 64 rows per wave (490 us: one wave per
 // SIMD), 32-key tiles with three waves per SIMD (376), 256 rows per workgroup (377,
 // and 52 us where 16 ragged prompts take 38).
 template <bool FP8, int D, bool F32>
@@ -839,12 +840,13 @@ constexpr uint32_t kStreamLds = kStreamKeys * (kKRow<D> + kVRow<D>) * 2;  // a w
 // for each other only to join their results at the end.
 //
 // Bound by the cache's bytes with one row tile and a full chip: 32 requests of 32
-// heads, 265 to 807 keys, d = 128, bf16, take 57 us (5.2 TB/s; a large copy reaches
-// 4.8).  K straight into the matrix operand, a row per lane, halves the LDS traffic
-// but reads 32 bytes of a row at a time (67 us); loads without the streaming hint
-// take 68.  With few workgroups bound by what a CU reads (32 workgroups of 552
-// keys, unsplit: 13.9 us), with two row tiles over fp8 by widening and arithmetic, done for
-// both (32 requests, 8 KV heads, 4096 keys: 79 us, 51 with one).
+// heads, 265 to 807 keys, d = 128, bf16, fp32 outputs, take 57 us (5.1 TB/s; a large
+// copy reaches 4.8, a stream that only reads 6.6).  K straight into the matrix
+// operand, a row per lane, halves the LDS traffic but reads 32 bytes of a row at a time
+// (67 us); loads without the streaming hint take 66 where these take 60, replayed.
+// With few workgroups bound by what a CU reads (32 workgroups of 552 keys, unsplit: 14.6
+// us), with two row tiles over fp8 by widening and arithmetic, done for both (32
+// requests of 8 KV heads, 256 to 4339 keys: 67 us for 13 nodes of four heads, 48 for 7).
 template <bool FP8, int D, bool F32, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void tree_stream_kernel(TreeArgs a) {
   constexpr int CPR = D / 8, RPP = 64 / CPR, NP = kStreamKeys / RPP;  // bf16 rows of V
