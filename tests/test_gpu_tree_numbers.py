@@ -2,6 +2,7 @@
 show: few keys, rows and codes that are not finite, every kernel."""
 
 import math
+import random
 
 import numpy as np
 import pytest
@@ -185,3 +186,104 @@ def test_layouts_with_too_few_scales_are_refused():
         with pytest.raises(ValueError):
             B.kv_layout(pr.k, **kw)
     attend(k_scale=pr.k_scale, v_scale=pr.v_scale)
+
+
+ANYWHERE = [
+    dict(batch=3, nodes=40, heads=(8, 2), bases=[40, 3, 95], counts=[40, 33, 1]),
+    dict(batch=1, nodes=31, heads=(4, 4), bases=[700], grid=(40, 40), branch=1),
+    dict(batch=2, nodes=61, heads=(256, 64), bases=[70, 12], branch=2),
+    dict(batch=2, nodes=150, heads=(4, 1), bases=[-21, 60], grid=(15, 15), tree=False),
+    dict(batch=2, nodes=150, heads=(172, 172), bases=[-13, 60], grid=(15, 15), tree=False),
+]
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+@pytest.mark.parametrize("view", ["dense", "window", "ring"])
+@pytest.mark.parametrize("case", range(len(ANYWHERE)))
+def test_what_is_seen_of_rows_that_are_not_finite(case, view, kv):
+    """Infinities and NaN in V rows anywhere, cached and new: an element is what its
+    node sees of them, or as without them."""
+    more = {"dense": {}, "window": dict(mode="window", n_att=25, sinks=4),
+            "ring": dict(mode="window", n_att=25, sinks=4, ring=29)}[view]
+    for d, out in ((64, "bf16"), (128, "fp32")):
+        kw = dict(ANYWHERE[case], **more, kv=kv, d=d, out=out, seed=40 + case)
+        clean, pr = Problem(**kw), Problem(**kw)
+        rng = random.Random(case)
+        kinds = {"inf": (1, 0), "-inf": (0, 1), "nan": (1, 1)}
+        marks = []  # (request, position or None, node or None, column, what it gives)
+        window = pr.window
+        for b in range(pr.batch):
+            base = pr.bases[b]
+            for _ in range(8):
+                lo = -pr.prompt if not pr.ring else max(-pr.prompt, base - 20)
+                j, c = rng.randrange(lo, base) if base > lo else None, rng.randrange(d)
+                if j is not None:
+                    kind = "nan" if kv == "fp8" else rng.choice(list(kinds))
+                    if kv == "fp8":
+                        pr.v.view(torch.uint8)[b, :, pr.row_of(j), c] = 0x7F
+                    else:
+                        pr.v[b, :, pr.row_of(j), c] = float(kind)
+                    marks = [m for m in marks if m[:2] + m[3:4] != (b, j, c)]
+                    marks.append((b, j, None, c, kinds[kind]))
+            for _ in range(8):
+                m, c, kind = rng.randrange(pr.nodes), rng.randrange(d), rng.choice(list(kinds))
+                pr.vn[b, m, :, c] = float(kind)
+                marks = [x for x in marks if (x[0], x[2], x[3]) != (b, m, c)]
+                marks.append((b, None, m, c, kinds[kind]))
+        want, got = clean.run().float().cpu(), pr.run().float().cpu()
+        for b in range(pr.batch):
+            n = pr.nodes if pr.counts is None else pr.counts[b]
+            for i in range(n):
+                held, up = otree.keys_of(pr.parents[b], i, pr.bases[b], pr.prompt, pr.sinks, window)
+                held, up = set(held), set(up)
+                see = {}
+                for _, j, m, c, what in (x for x in marks if x[0] == b):
+                    if (m in up) if j is None else (j in held):
+                        a = see.get(c, (0, 0))
+                        see[c] = (a[0] | what[0], a[1] | what[1])
+                w = want[b, i].clone()
+                for c, (plus, minus) in see.items():
+                    w[:, c] = math.nan if plus and minus else math.inf if plus else -math.inf
+                assert torch.equal(got[b, i].nan_to_num(7e30), w.nan_to_num(7e30)), (b, i)
+                assert torch.equal(got[b, i].isnan(), w.isnan()), (b, i)
+
+
+@pytest.mark.parametrize("kernel", ["whole", "split", "tiles"])
+@pytest.mark.parametrize("out", ["fp32", "bf16"])
+def test_infinite_keys(kernel, out):
+    """A score of -inf takes its key out, one of +inf makes the row NaN, as the
+    softmax does."""
+    kw = dict(tree=False, out=out, prompt=40, bases=[30, 7][:KERNELS[kernel]["batch"]], seed=5)
+    pr = problem(kernel, **kw)
+    pr.k[:, :, 5, 0] = math.inf  # a score of the query's first element's sign
+    sign = (pr.q[..., 0] > 0).cpu()
+    got = pr.run().cpu()
+    k, v = pr.caches64()
+    q, kn, vn = (x.double().cpu().numpy() for x in (pr.q, pr.kn, pr.vn))
+    for b in range(pr.batch):
+        for i in sorted({0, 3, pr.nodes - 1}):
+            held, up = otree.keys_of(pr.parents[b], i, pr.bases[b], pr.prompt, 0, None)
+            rows = [r for r in (pr.row_of(j) for j in held) if r != 5]
+            for h in sorted({0, 1, pr.hkv - 1}):
+                x = got[b, i, h]
+                if sign[b, i, h]:
+                    assert x.isnan().all(), (b, i, h)
+                    continue
+                kk = np.concatenate([k[b, h, rows], kn[b, up, h]])
+                vv = np.concatenate([v[b, h, rows], vn[b, up, h]])
+                ref, band = otree.attend(q[b, i, h], kk, vv, pr.scale)
+                e = (band + 2.0 ** -16 + len(kk) * 2.0 ** -24) * np.abs(vv).max()
+                if out == "bf16":
+                    e = 2.0 ** -8 * (np.abs(ref) + e) + e
+                assert (np.abs(x.double().numpy() - ref) <= e).all(), (b, i, h)
+
+
+@pytest.mark.parametrize("nodes,heads", [(9, (4, 4)), (40, (8, 2)), (90, (172, 172))])
+def test_fp8_caches_without_scales(nodes, heads):
+    """Scales of 1, exactly."""
+    kw = dict(nodes=nodes, heads=heads, kv="fp8", grid=(15, 15), bases=[100, 60], seed=3)
+    a, b = Problem(**kw), Problem(**kw)
+    a.k_scale.fill_(1.0)
+    a.v_scale.fill_(1.0)
+    b.layout = B.kv_layout(b.k)
+    assert torch.equal(a.run(), b.run())
