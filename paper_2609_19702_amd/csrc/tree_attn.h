@@ -546,7 +546,8 @@ __device__ __forceinline__ uint32_t clean_codes(uint4* x) {
 // A weight's terms, or a weight that underflows, make NaN of an infinity in V
 // where one of them is 0.  So four elements of a row that are not all finite are
 // settled once more: what each sees of infinities and NaN, over the tiles of 32 keys
-// t0 .. t1 - 1, takes its place.  v_old, v_new: the elements' columns of V.
+// t0 .. t1 - 1 or until all of them are NaN, takes its place.  v_old, v_new: the
+// elements' columns of V.
 template <bool FP8>
 __device__ __forceinline__ void settle_nonfinite(const TreeArgs& a, const TreeKeys& ks,
                                                  const TreeTile& tt, const TreeRow& my, int b,
@@ -554,8 +555,11 @@ __device__ __forceinline__ void settle_nonfinite(const TreeArgs& a, const TreeKe
                                                  int t1, float (&x)[4]) {
   const int t_old = (ks.cached.n + 31) / 32;
   uint32_t up = 0, down = 0;  // bit per element: an infinity, or both for a NaN
+  uint32_t open = 0;          // those to settle
+#pragma unroll
+  for (int k = 0; k < 4; ++k) open |= x[k] - x[k] == 0.f ? 0u : 1u << k;
 #pragma unroll 1
-  for (int t = t0; t < t1; ++t) {
+  for (int t = t0; t < t1 && (open & ~(up & down)); ++t) {
     const bool old = t < t_old;
     const int e0 = (t - (old ? 0 : t_old)) * 32;
     const KeyList list = pick_list(old, ks.cached, ks.fresh);
@@ -591,7 +595,7 @@ __device__ __forceinline__ void settle_nonfinite(const TreeArgs& a, const TreeKe
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const bool u = up >> k & 1u, d = down >> k & 1u;
+    const bool u = up & open & 1u << k, d = down & open & 1u << k;
     if (u || d) x[k] = u && d ? __builtin_nanf("") : u ? __builtin_inff() : -__builtin_inff();
   }
 }
@@ -630,9 +634,9 @@ constexpr int kTileRows = 128;  // query rows of a workgroup
 // softmax's exponentials, maxima and packing beside them.  With the weights in one
 // bf16 term they took 375: 286 for the arithmetic without loads and stores to LDS, 51
 // for the loads, 32 for the LDS stores.  The second term adds half as many products
-// and 49 instructions per 32 keys.  Measured with one term and left: 64 rows per wave (490 us: one wave per
-// SIMD), 32-key tiles with three waves per SIMD (376), 256 rows per workgroup (377,
-// and 52 us where 16 ragged prompts take 38).
+// and 49 instructions per 32 keys.  Measured with one term and left: 64 rows per wave
+// (490 us: one wave per SIMD), 32-key tiles with three waves per SIMD (376), 256 rows
+// per workgroup (377, and 52 us where 16 ragged prompts take 38).
 template <bool FP8, int D, bool F32>
 __global__ __launch_bounds__(256, 2) void tree_tile_kernel(TreeArgs a) {
   constexpr int CPR = D / 8;           // 16-byte chunks of a bf16 row
