@@ -671,6 +671,230 @@ DSA_API dsa_status dsa_kv_append(const dsa_params* p, const dsa_shape* s, const 
                                  const dsa_kv_layout* kv, int64_t stride_layer,
                                  hipStream_t stream);
 
+/* ---- a KV cache in pages ---------------------------------------------------- */
+
+/*
+ * Requests that come and go, and images that share their prompt's rows, keep
+ * their K/V rows in pages of P rows (all KV heads), taken from one pool that all
+ * layers' caches are cut into alike.  Row r of request b (its prompt rows first,
+ * then decode position j in row prompt_b + j) is row r mod P of page
+ * d_table[b][r / P].  The calls of a step are
+ *
+ *     dsa_page_reorder     requests that go on from others' rows (beams, several
+ *                          images of one prompt)
+ *     dsa_page_update      pages for the new rows, their slots, and the pages that
+ *                          ended or fell behind the window back into the pool
+ *     dsa_paged_append     the new K/V rows into their slots (each layer, or all)
+ *     dsa_paged_attention  one token's attention over the pages (each layer)
+ *
+ * and dsa_beam_select chooses what a beam search goes on with.  A prompt's own
+ * attention is dsa_tree_attention's, over nothing but the prompt (base -L_p).
+ *
+ *   page_rows  P, a power of two in [1, 1024]
+ *   max_pages  M >= 1, entries of a request's row of the table, M * P < 2^31
+ *   num_pages  pages of the pool, num_pages * P < 2^31
+ *   d_table    int32 [B][M]: the page of rows i * P .. i * P + P - 1; a value
+ *              outside [0, num_pages) names none (the calls here write -1)
+ *   d_refs     int32 [num_pages]: how many entries name each page; 0: it is free
+ *              (dsa_page_update, dsa_page_reorder; else it may be NULL)
+ *   d_cursor   int32 [1]: the page that the search for free ones starts from, any
+ *              value to begin with (dsa_page_update; else it may be NULL)
+ *   d_prompt   int32 [B]: prompt rows of each request, clamped to [0, L_p];
+ *              NULL: all L_p
+ * Tables and counts that only these calls change stay consistent.  A program
+ * that starts empty fills d_table with -1 and d_refs with 0.
+ */
+typedef struct dsa_pages {
+  int32_t page_rows;
+  int32_t max_pages;
+  int32_t num_pages;
+  int32_t* d_table;
+  int32_t* d_refs;
+  int32_t* d_cursor;
+  const int32_t* d_prompt;
+} dsa_pages;
+
+#define DSA_MAX_PAGED_BATCH 4096 /* requests of dsa_page_update and dsa_page_reorder */
+
+/* Where row o of page g and KV head h starts in a layer's K and V arrays, in
+ * elements: g * stride_page + h * stride_head + o * stride_row; a row holds
+ * head_dim contiguous elements of type dtype (as in dsa_kv_layout).  Strides
+ * are >= 0 and multiples of 16 bytes, the arrays 16-byte aligned.  Pages have
+ * several users, so an fp8 cache has a scale per KV head: d_k_scale[h],
+ * d_v_scale[h] (those of the layer; 1 where the pointer is NULL; both NULL for
+ * bf16). */
+typedef struct dsa_page_layout {
+  int32_t num_pages;
+  int32_t page_rows;
+  int64_t stride_page;
+  int64_t stride_head;
+  int64_t stride_row;
+  const float* d_k_scale;
+  const float* d_v_scale;
+  int32_t dtype;
+} dsa_page_layout;
+
+/* dsa_page_update flag bits (per request). */
+#define DSA_PAGE_FLAG_NO_PAGES 1 /* the pool had too few free pages               */
+#define DSA_PAGE_FLAG_TOO_LONG 2 /* rows past the M * P that a table's row can name */
+
+/* How dsa_paged_attention splits the rows (for reports and tests): a function of
+ * parameters, shape and cache type. */
+typedef struct dsa_paged_launch_info {
+  int32_t rows_per_split;
+  int32_t max_splits;      /* splits per (request, KV head) at most             */
+  int32_t waves_per_group;
+  int32_t workgroups;
+  size_t workspace_bytes;  /* fp32 partials for the combine (0 with one split)  */
+} dsa_paged_launch_info;
+
+DSA_API dsa_status dsa_get_paged_launch_info(const dsa_params* p, const dsa_shape* s,
+                                             int32_t dtype, dsa_paged_launch_info* out);
+/* Workspace of dsa_paged_attention over a cache of either type (0 when the
+ * arguments are invalid). */
+DSA_API size_t dsa_paged_workspace_bytes(const dsa_params* p, const dsa_shape* s);
+
+/*
+ * Pages for a step's new rows.  For every request b of length len = d_length[b]
+ * (rows 0 .. len - 1 hold tokens) and new_b = d_new[b] new rows:
+ *   - len < 0: the slot is unused; its pages go back to the pool.
+ *   - Else the pages whose rows all lie in [prompt_b + S, len - W + 1) do: no step
+ *     from here on attends them (W = N_r in diagonal and N_att - S in window mode;
+ *     none in dense mode, S = 0).
+ *   - Rows len .. len + new_b - 1 get pages: an entry that names none, and one
+ *     whose page other entries name too, takes the next free page.  (The shared
+ *     page stays with its other users, or goes back after its last.)
+ * Free pages are taken in the order of the pool from *d_cursor on and around, by
+ * requests in order, a request's entries in order; *d_cursor becomes the page
+ * after the last one taken.  Pages given back in this call can be taken in it;
+ * shared ones that their last user left here cannot.  A request gets its pages where the needs of the
+ * requests up to it add up to no more than there are free, or it needs none; else
+ * it gets nothing, as with len + new_b > M * P.
+ *   p         prompt_len, mode, window, n_att and sinks are read; valid as for
+ *             every call
+ *   batch     B in [1, DSA_MAX_PAGED_BATCH]
+ *   pages     all fields but d_prompt required
+ *   d_length  int32 [B]; not changed (a program adds d_new when its step is done)
+ *   d_new     int32 [B], clamped to [0, most_new]; NULL: 1 each
+ *   most_new  N >= 1, B * N < 2^31
+ *   d_slots   int32 [B][N], out: page * P + row in the page of row len + i; -1 for
+ *             i >= new_b and for requests that got nothing
+ *   d_pos     int32 [B], out: decode position of the request's last row,
+ *             len + new_b - 1 - prompt_b, -1 where that is below 0, for unused
+ *             slots and for requests that got nothing (as d_decode_pos)
+ *   d_copies  int32 [B][3], out: (page, new page, len mod P) where the new rows
+ *             begin inside a shared page, whose first rows dsa_paged_append then
+ *             copies; else -1 each
+ *   d_flags   int32 [B], out: DSA_PAGE_FLAG_* bits
+ * Errors: INVALID_ARG, UNSUPPORTED (batch), HIP.
+ */
+DSA_API dsa_status dsa_page_update(const dsa_params* p, int32_t batch, const dsa_pages* pages,
+                                   const int32_t* d_length, const int32_t* d_new,
+                                   int32_t most_new, int32_t* d_slots, int32_t* d_pos,
+                                   int32_t* d_copies, int32_t* d_flags, hipStream_t stream);
+
+/*
+ * Request b goes on from the rows of request d_parent[b]: row b of the table
+ * becomes what row d_parent[b] was, for all b at once, and d_refs follows.  No row
+ * is moved; dsa_page_update gives a request that writes into a shared page its
+ * own.  A parent outside [0, B) leaves the request without pages.  (Lengths,
+ * prompt lengths and selection states are the caller's to reorder.)
+ *   batch     B in [1, DSA_MAX_PAGED_BATCH]
+ *   pages     d_table and d_refs required
+ *   d_parent  int32 [B]
+ * Errors: INVALID_ARG, UNSUPPORTED (batch), HIP.
+ */
+DSA_API dsa_status dsa_page_reorder(int32_t batch, const dsa_pages* pages,
+                                    const int32_t* d_parent, hipStream_t stream);
+
+/*
+ * New K/V rows into their slots: row i of request b goes to row d_slots[b][i] mod P
+ * of page d_slots[b][i] / P in each of `layers` layers, and rows 0 .. n - 1 of page
+ * x to page y for every (x, y, n) of d_copies.  bf16 rows are copied; for an
+ * fp8 cache each element is divided by its scale, clamped to +-448 and rounded
+ * to the nearest E4M3 value, ties to even (NaN stays NaN).
+ *   s            batch, num_kv_heads and head_dim are read
+ *   most_new     N >= 1
+ *   d_slots      int32 [B][N]; values outside [0, num_pages * P) write nothing.
+ *                Slots that occur twice get one of their rows, or parts of both.
+ *   d_k_new ..   bf16 rows (new_rows, its nodes the N rows, with stride_layer)
+ *   layers       >= 1; layer l of the caches starts l * stride_layer elements in
+ *                (a multiple of 16 bytes)
+ *   d_k, d_v     caches in `layout`, whose scales are those of all layers,
+ *                [layers][Hkv]
+ *   d_copies     int32 [B][3] as dsa_page_update leaves them, or NULL; n is
+ *                clamped to P, and a page outside the pool copies nothing.  No slot
+ *                may lie in the copied rows, nor in the copies.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+DSA_API dsa_status dsa_paged_append(const dsa_shape* s, int32_t most_new, const int32_t* d_slots,
+                                    const void* d_k_new, const void* d_v_new,
+                                    const dsa_node_rows* new_rows, int32_t layers, void* d_k,
+                                    void* d_v, const dsa_page_layout* layout,
+                                    int64_t stride_layer, const int32_t* d_copies,
+                                    hipStream_t stream);
+
+/*
+ * dsa_decode_attention over pages: softmax(sm_scale * q . k) V for one token per
+ * request over its prompt rows and the decode rows that the mode keeps at
+ * position t = d_decode_pos[b]: all up to t (dense), those of the plan (diagonal),
+ * the sinks and the N_att - S most recent ones (window; no plan is read).  Rows
+ * whose entry of the table names no page, or that lie past the table's row, are
+ * left out.  What is left out does not reach the output, NaN and infinities
+ * included; a NaN or an infinity in a row that is attended makes the outputs it
+ * reaches NaN or infinite.  Where no row is left, or every score is -infinity, the
+ * output is 0.
+ *   pages            page_rows, max_pages, d_table, d_prompt
+ *   layout           of d_k and d_v; of pages of the same page_rows
+ *   d_q              bf16 [B][Hq][d]
+ *   d_decode_pos     int32 [B], as for dsa_plan (t < 0: an unused slot, zeros out)
+ *   d_plan           plan of the same step in diagonal mode (else not read)
+ *   sm_scale         any finite value
+ *   d_out            [B][Hq][d] in out_type (DSA_OUT_FP32, DSA_OUT_BF16)
+ *   d_window_logits  NULL, or fp32 [B][Hq][cap] in diagonal mode, as for
+ *                    dsa_decode_attention; a row without a page has -infinity
+ *   d_ws, ws_bytes   dsa_paged_workspace_bytes() bytes, 16-byte aligned; need not
+ *                    be cleared
+ * All arrays of rows are 16-byte aligned.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
+ */
+DSA_API dsa_status dsa_paged_attention(const dsa_params* p, const dsa_shape* s,
+                                       const dsa_pages* pages, const void* d_q, const void* d_k,
+                                       const void* d_v, const dsa_page_layout* layout,
+                                       const int32_t* d_decode_pos, const void* d_plan,
+                                       float sm_scale, void* d_out, int32_t out_type,
+                                       float* d_window_logits, void* d_ws, size_t ws_bytes,
+                                       hipStream_t stream);
+
+/*
+ * One step of a beam search: of the candidates (w, v) of request b, with scores
+ *     d_score[b][w] + x[v] - log sum_u exp x[u],   x = row (b, w) of the logits,
+ * the W best in order, equal ones by the lowest w * V + v.  Candidates of score
+ * -infinity or NaN are none: a beam that has not begun has d_score -infinity, a
+ * finished one logits of -infinity but for one token.  Where fewer than W are left,
+ * the rest of the beams end: score -infinity, parent and token -1.
+ *   batch, beams   B >= 1, W in [1, DSA_MAX_BEAMS], B * W < 2^22
+ *   vocab          V in [1, 1 << 24]
+ *   d_logits       row (b, w) of V contiguous values of logits_type
+ *                  (DSA_OUT_FP32, DSA_OUT_BF16) starts (b * W + w) * stride_row
+ *                  values in; stride_row >= V
+ *   d_score        fp32 [B][W]
+ *   d_next_score   fp32 [B][W], out; may be d_score
+ *   d_parent       int32 [B][W], out: b * W + w, as dsa_page_reorder takes it
+ *   d_token        int32 [B][W], out
+ *   d_ws, ws_bytes dsa_beam_workspace_bytes() bytes, 16-byte aligned; need not be
+ *                  cleared
+ * Sums of exponentials are kept in fp64, and scores compared in fp64.
+ * Errors: INVALID_ARG, WORKSPACE, HIP.
+ */
+#define DSA_MAX_BEAMS 16
+DSA_API size_t dsa_beam_workspace_bytes(int32_t batch, int32_t beams, int32_t vocab);
+DSA_API dsa_status dsa_beam_select(int32_t batch, int32_t beams, int32_t vocab,
+                                   const void* d_logits, int64_t stride_row, int32_t logits_type,
+                                   const float* d_score, float* d_next_score, int32_t* d_parent,
+                                   int32_t* d_token, void* d_ws, size_t ws_bytes,
+                                   hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,6 +33,10 @@ FLAG_BAD_OFFSET = 8
 FLAG_COUNT = 16
 TREE_FLAG_BAD_PARENT = 1
 MAX_TREE_NODES = 256
+PAGE_FLAG_NO_PAGES = 1
+PAGE_FLAG_TOO_LONG = 2
+MAX_PAGED_BATCH = 4096
+MAX_BEAMS = 16
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = 0, -1, -2, -3, -4
 
@@ -107,9 +111,28 @@ class TreeLaunchInfo(C.Structure):
                 ("workgroups", C.c_int32), ("workspace_bytes", C.c_size_t)]
 
 
+class PagesStruct(C.Structure):  # dsa_pages
+    _fields_ = [("page_rows", C.c_int32), ("max_pages", C.c_int32), ("num_pages", C.c_int32),
+                ("d_table", C.c_void_p), ("d_refs", C.c_void_p), ("d_cursor", C.c_void_p),
+                ("d_prompt", C.c_void_p)]
+
+
+class PageLayout(C.Structure):
+    _fields_ = [("num_pages", C.c_int32), ("page_rows", C.c_int32), ("stride_page", C.c_int64),
+                ("stride_head", C.c_int64), ("stride_row", C.c_int64), ("d_k_scale", C.c_void_p),
+                ("d_v_scale", C.c_void_p), ("dtype", C.c_int32)]
+
+
+class PagedLaunchInfo(C.Structure):
+    _fields_ = [("rows_per_split", C.c_int32), ("max_splits", C.c_int32),
+                ("waves_per_group", C.c_int32), ("workgroups", C.c_int32),
+                ("workspace_bytes", C.c_size_t)]
+
+
 # name -> (restype, argtypes); mirrors include/dsa.h
 _P, _S = C.POINTER(Params), C.POINTER(Shape)
 _T, _R = C.POINTER(TreeRequest), C.POINTER(NodeRows)
+_G, _L = C.POINTER(PagesStruct), C.POINTER(PageLayout)
 _VP = C.c_void_p
 SIGNATURES = {
     "dsa_abi_version": (C.c_int32, []),
@@ -149,6 +172,17 @@ SIGNATURES = {
     "dsa_tree_verify": (C.c_int32, [C.c_int32, C.c_int32, _T] + [_VP] * 8),
     "dsa_kv_append": (C.c_int32, [_P, _S, _T, _VP, _VP, _R, _VP, _VP, C.c_int32, _VP, _VP,
                                   C.POINTER(KVLayout), C.c_int64, _VP]),
+    "dsa_get_paged_launch_info": (C.c_int32, [_P, _S, C.c_int32, C.POINTER(PagedLaunchInfo)]),
+    "dsa_paged_workspace_bytes": (C.c_size_t, [_P, _S]),
+    "dsa_page_update": (C.c_int32, [_P, C.c_int32, _G, _VP, _VP, C.c_int32] + [_VP] * 5),
+    "dsa_page_reorder": (C.c_int32, [C.c_int32, _G, _VP, _VP]),
+    "dsa_paged_append": (C.c_int32, [_S, C.c_int32, _VP, _VP, _VP, _R, C.c_int32, _VP, _VP, _L,
+                                     C.c_int64, _VP, _VP]),
+    "dsa_paged_attention": (C.c_int32, [_P, _S, _G, _VP, _VP, _VP, _L, _VP, _VP, C.c_float, _VP,
+                                        C.c_int32, _VP, _VP, C.c_size_t, _VP]),
+    "dsa_beam_workspace_bytes": (C.c_size_t, [C.c_int32] * 3),
+    "dsa_beam_select": (C.c_int32, [C.c_int32] * 3 + [_VP, C.c_int64, C.c_int32] + [_VP] * 5
+                        + [C.c_size_t, _VP]),
 }
 
 NOALLOC_SCRATCH_BYTES = 16 << 20  # DSA_NOALLOC_SCRATCH_BYTES
@@ -706,6 +740,236 @@ def tree_plan_views(batch: int, nodes: int, plan_buf: torch.Tensor):
             i32(L.depth_offset, bn).view(batch, nodes),
             i32(L.parent_offset, bn).view(batch, nodes),
             i32(L.ancestors_offset, bn * L.words).view(batch, nodes, L.words))
+
+
+# ---- a KV cache in pages -----------------------------------------------------------
+
+class Pages:
+    """Page tables of all requests (``dsa_pages``): ``table`` int32 [B, M], the
+    page of each ``page_rows`` rows or -1; ``refs`` int32 [num_pages], how many
+    entries name each page, and ``cursor`` int32 [1], both for ``page_update``
+    (``page_reorder`` needs ``refs``); ``prompt`` int32 [B], prompt rows of each
+    request (all ``prompt_len``).  Keeps the tensors it points to; they can be
+    written, not exchanged."""
+
+    def __init__(self, page_rows, table, refs=None, cursor=None, prompt=None):
+        for x, name in ((table, "table"), (refs, "refs"), (cursor, "cursor"), (prompt, "prompt")):
+            _need(x, name, torch.int32)
+        if table.dim() != 2:
+            raise ValueError(f"table must be [B, pages], got {tuple(table.shape)}")
+        if refs is not None and refs.dim() != 1:
+            raise ValueError(f"refs must be [num_pages], got {tuple(refs.shape)}")
+        _need(cursor, "cursor", torch.int32, 4)
+        _need(prompt, "prompt", torch.int32, 4 * table.shape[0])
+        for x, name in ((refs, "refs"), (cursor, "cursor"), (prompt, "prompt")):
+            if x is not None and x.device != table.device:
+                raise ValueError(f"{name} is on {x.device}, the table on {table.device}")
+        self._held = (table, refs, cursor, prompt)
+        self.c = PagesStruct(int(page_rows), table.shape[1], 0 if refs is None else refs.numel(),
+                             _ptr(table), _ptr(refs), _ptr(cursor), _ptr(prompt))
+        self.ref = C.byref(self.c)
+        self.batch, self.device = table.shape[0], table.get_device()
+
+    table = property(lambda self: self._held[0])
+    refs = property(lambda self: self._held[1])
+    cursor = property(lambda self: self._held[2])
+    prompt = property(lambda self: self._held[3])
+    page_rows = property(lambda self: self.c.page_rows)
+
+
+def make_pages(page_rows, table, refs=None, cursor=None, prompt=None) -> Pages:
+    return Pages(page_rows, table, refs, cursor, prompt)
+
+
+def page_layout(k: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                v_scale: Optional[torch.Tensor] = None) -> PageLayout:
+    """Layout of a layer's cache ``[num_pages, Hkv, page_rows, d]`` (any strides
+    with unit stride along d), in bf16 or fp8 (as for ``kv_layout``) with
+    optional fp32 scales of its KV heads, ``[Hkv]``; for ``paged_append`` of
+    several layers those of all of them, ``[layers, Hkv]``.  The layout keeps the
+    tensors it points to."""
+    if k.dim() != 4:
+        raise ValueError(f"a cache is [num_pages, Hkv, page_rows, d], got {tuple(k.shape)}")
+    sp, sh, sr, sd = k.stride()
+    if sd != 1:
+        raise ValueError("head_dim must be contiguous")
+    _need(k_scale, "k_scale", torch.float32)
+    _need(v_scale, "v_scale", torch.float32)
+    if k.dtype not in _KV_DTYPES:
+        raise ValueError(f"unsupported KV dtype {k.dtype}")
+    out = PageLayout(k.shape[0], k.shape[2], sp, sh, sr, _ptr(k_scale), _ptr(v_scale),
+                     KV_BF16 if k.dtype == torch.bfloat16 else KV_FP8_E4M3)
+    out._held = (k_scale, v_scale)
+    out.scales = min([x.numel() for x in out._held if x is not None], default=1 << 62)
+    return out
+
+
+def paged_launch_info(p: Params, s: Shape, dtype: int = KV_BF16) -> PagedLaunchInfo:
+    out = PagedLaunchInfo()
+    _check(lib().dsa_get_paged_launch_info(C.byref(p), C.byref(s), dtype, C.byref(out)),
+           "dsa_get_paged_launch_info")
+    return out
+
+
+def paged_workspace_bytes(p: Params, s: Shape) -> int:
+    return lib().dsa_paged_workspace_bytes(C.byref(p), C.byref(s))
+
+
+def _need_pages(pages, device, batch, where, refs=False, cursor=False):
+    if pages.device != device:
+        raise _elsewhere(pages.table, "the table", device)
+    if batch != pages.batch:
+        raise ValueError(f"the table has {pages.batch} requests, the call {batch}")
+    if refs and pages.refs is None or cursor and pages.cursor is None:
+        raise ValueError(f"{where} needs the pages' refs" + " and cursor" * cursor)
+
+
+def page_update(p, pages: Pages, length, new, slots, pos, copies, flags, stream=None):
+    """Pages for a step's new rows: ``length`` int32 [B] (below 0: an unused slot),
+    ``new`` int32 [B] or None (1 each); out: ``slots`` int32 [B, N], ``pos`` [B],
+    ``copies`` [B, 3], ``flags`` [B], all int32."""
+    device = torch.cuda.current_device() if length.is_cuda else None
+    batch = length.shape[0]
+    _need_dense(length, "length", torch.int32, (batch,), device)
+    _need_pages(pages, device, batch, "page_update", refs=True, cursor=True)
+    if new is not None:
+        _need_dense(new, "new", torch.int32, (batch,), device)
+    if slots.dim() != 2:
+        raise ValueError(f"slots must be [B, N], got {tuple(slots.shape)}")
+    _need_dense(slots, "slots", torch.int32, (batch, slots.shape[1]), device)
+    _need_dense(pos, "pos", torch.int32, (batch,), device)
+    _need_dense(copies, "copies", torch.int32, (batch, 3), device)
+    _need_dense(flags, "flags", torch.int32, (batch,), device)
+    _check(lib().dsa_page_update(
+        C.byref(p), batch, pages.ref, length.data_ptr(), _ptr(new), slots.shape[1],
+        slots.data_ptr(), pos.data_ptr(), copies.data_ptr(), flags.data_ptr(), _stream(stream)),
+        "dsa_page_update")
+
+
+def page_reorder(pages: Pages, parent, stream=None):
+    """Every request goes on from the pages of request ``parent[b]`` (int32 [B])."""
+    device = torch.cuda.current_device() if parent.is_cuda else None
+    _need_dense(parent, "parent", torch.int32, (pages.batch,), device)
+    _need_pages(pages, device, pages.batch, "page_reorder", refs=True)
+    _check(lib().dsa_page_reorder(pages.batch, pages.ref, parent.data_ptr(), _stream(stream)),
+           "dsa_page_reorder")
+
+
+def _check_paged(s, k, v, layout, layers, device):
+    """The caches against their layout, their scales and the shape."""
+    shape, st = k.shape, k.stride()
+    if k.dtype not in _KV_DTYPES or k.dtype is not v.dtype or shape != v.shape or st != v.stride():
+        raise ValueError("k and v must share element type (bf16 or fp8), shape and strides")
+    for x, name in ((k, "k"), (v, "v")):
+        if x.get_device() != device:
+            _need(x, name, contiguous=False)
+            raise _elsewhere(x, name, device)
+    if (layout.dtype == KV_BF16) != (k.dtype is torch.bfloat16):
+        raise ValueError(f"the layout is not of a {k.dtype} cache")
+    if len(shape) != (4 if layers is None else 5) or (layers is not None and shape[0] != layers):
+        raise ValueError(f"caches of shape {tuple(shape)} are not of "
+                         + ("one layer" if layers is None else f"{layers} layers"))
+    n, heads, rows, d = shape[-4:]
+    if (n < layout.num_pages or heads < s.num_kv_heads or rows != layout.page_rows
+            or d != s.head_dim or st[-4:] != (layout.stride_page, layout.stride_head,
+                                              layout.stride_row, 1)):
+        raise ValueError(f"cache of shape {tuple(shape)} does not hold {layout.num_pages} pages of "
+                         f"{layout.page_rows} rows x {s.num_kv_heads} KV heads of {s.head_dim} "
+                         "elements as the layout says")
+    if layout.scales < (layers or 1) * s.num_kv_heads:
+        raise ValueError(f"the layout holds {layout.scales} scales, the call reads {layers or 1} "
+                         f"layers x {s.num_kv_heads} KV heads of them")
+    for x in layout._held:
+        if x is not None and x.get_device() != device:
+            raise _elsewhere(x, "a scale", device)
+
+
+def paged_append(s, slots, k_new, v_new, k, v, layout: PageLayout, copies=None, stream=None):
+    """K/V rows into their slots (int32 [B, N], -1: nowhere), after the rows of shared
+    pages that ``copies`` (int32 [B, 3]) names.  One layer (``k_new`` [B, N, Hkv,
+    d], ``k`` [num_pages, Hkv, page_rows, d]) or all of them (both with layers in
+    front, ``layout`` of one layer's cache but with the scales of all)."""
+    device = torch.cuda.current_device() if k_new.is_cuda else None
+    B_, Hkv, d = s.batch, s.num_kv_heads, s.head_dim
+    layers = k_new.shape[0] if k_new.dim() == 5 else None
+    if slots.dim() != 2:
+        raise ValueError(f"slots must be [B, N], got {tuple(slots.shape)}")
+    n = slots.shape[1]
+    _need_dense(slots, "slots", torch.int32, (B_, n), device)
+    shape = (B_, n, Hkv, d) if layers is None else (layers, B_, n, Hkv, d)
+    rows = _new_rows(k_new, v_new, shape, device)
+    _check_paged(s, k, v, layout, layers, device)
+    if copies is not None:
+        _need_dense(copies, "copies", torch.int32, (B_, 3), device)
+    _check(lib().dsa_paged_append(
+        C.byref(s), n, slots.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), C.byref(rows),
+        layers or 1, k.data_ptr(), v.data_ptr(), C.byref(layout), k.stride(0) if layers else 0,
+        _ptr(copies), _stream(stream)), "dsa_paged_append")
+
+
+def paged_attention(p, s, pages: Pages, q, k, v, layout: PageLayout, decode_pos, sm_scale, out,
+                    plan_buf=None, window_logits=None, workspace=None, stream=None):
+    """Attention of one token per request (``q`` bf16 [B, Hq, d]) over its pages;
+    ``out`` [B, Hq, d] in fp32 or bf16.  Diagonal mode takes the step's plan, and
+    the window logits fp32 [B, Hq, cap] where the selection is to read them."""
+    device = torch.cuda.current_device() if q.is_cuda else None
+    B_, shape = s.batch, (s.batch, s.num_q_heads, s.head_dim)
+    _need_dense(q, "q", torch.bfloat16, shape, device)
+    _need_pages(pages, device, B_, "paged_attention")
+    out_type = _OUT_TYPES.get(out.dtype)
+    if out_type is None:
+        raise ValueError(f"out must be fp32 or bf16, got {out.dtype}")
+    _need_dense(out, "out", out.dtype, shape, device)
+    _need_dense(decode_pos, "decode_pos", torch.int32, (B_,), device)
+    _check_paged(s, k, v, layout, None, device)
+    if p.mode == MODE_DIAGONAL:
+        z = _sizes(p, s)
+        _need(plan_buf, "plan", None, z[2])
+        _need_bytes(plan_buf, "plan", device)
+        if window_logits is not None:
+            _need(window_logits, "window_logits", torch.float32, z[1])
+            _need_bytes(window_logits, "window_logits", device)
+    _need_bytes(workspace, "workspace", device)
+    _check(lib().dsa_paged_attention(
+        C.byref(p), C.byref(s), pages.ref, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        C.byref(layout), decode_pos.data_ptr(), _ptr(plan_buf), sm_scale, out.data_ptr(), out_type,
+        _ptr(window_logits), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
+        _stream(stream)), "dsa_paged_attention")
+
+
+def beam_workspace_bytes(batch: int, beams: int, vocab: int) -> int:
+    return lib().dsa_beam_workspace_bytes(batch, beams, vocab)
+
+
+def beam_select(logits, score, next_score, parent, token, workspace, stream=None):
+    """The best ``beams`` candidates of every request: ``logits`` [B, beams, V] in
+    fp32 or bf16 (rows dense and evenly apart), ``score`` fp32 [B, beams]; out:
+    ``next_score`` fp32 (may be ``score``), ``parent`` and ``token`` int32, all
+    [B, beams]; parents as ``page_reorder`` takes them, flattened."""
+    device = torch.cuda.current_device() if logits.is_cuda else None
+    if logits.dim() != 3:
+        raise ValueError(f"logits must be [B, beams, V], got {tuple(logits.shape)}")
+    batch, beams, vocab = logits.shape
+    kind = _OUT_TYPES.get(logits.dtype)
+    if kind is None:
+        raise ValueError(f"logits must be fp32 or bf16, got {logits.dtype}")
+    if logits.get_device() != device:
+        _need(logits, "logits", contiguous=False)
+        raise _elsewhere(logits, "logits", device)
+    sb, sw, sv = logits.stride()
+    row = sw if beams > 1 else sb if batch > 1 else vocab
+    if (vocab > 1 and sv != 1) or (batch > 1 and sb != beams * row) or row < vocab:
+        raise ValueError("logits must have dense rows, evenly apart")
+    shape = (batch, beams)
+    _need_dense(score, "score", torch.float32, shape, device)
+    _need_dense(next_score, "next_score", torch.float32, shape, device)
+    _need_dense(parent, "parent", torch.int32, shape, device)
+    _need_dense(token, "token", torch.int32, shape, device)
+    _need_bytes(workspace, "workspace", device)
+    _check(lib().dsa_beam_select(
+        batch, beams, vocab, logits.data_ptr(), row, kind, score.data_ptr(), next_score.data_ptr(),
+        parent.data_ptr(), token.data_ptr(), _ptr(workspace),
+        0 if workspace is None else workspace.nbytes, _stream(stream)), "dsa_beam_select")
 
 
 # ---- buffers (torch allocations) and views --------------------------------------
