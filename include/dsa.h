@@ -739,7 +739,7 @@ typedef struct dsa_page_layout {
 #define DSA_PAGE_FLAG_TOO_LONG 2 /* rows past the M * P that a table's row can name */
 
 /* How dsa_paged_attention splits the rows (for reports and tests): a function of
- * parameters, shape and cache type. */
+ * parameters and shape. */
 typedef struct dsa_paged_launch_info {
   int32_t rows_per_split;
   int32_t max_splits;      /* splits per (request, KV head) at most             */
@@ -749,9 +749,8 @@ typedef struct dsa_paged_launch_info {
 } dsa_paged_launch_info;
 
 DSA_API dsa_status dsa_get_paged_launch_info(const dsa_params* p, const dsa_shape* s,
-                                             int32_t dtype, dsa_paged_launch_info* out);
-/* Workspace of dsa_paged_attention over a cache of either type (0 when the
- * arguments are invalid). */
+                                             dsa_paged_launch_info* out);
+/* Workspace of dsa_paged_attention (0 when the arguments are invalid). */
 DSA_API size_t dsa_paged_workspace_bytes(const dsa_params* p, const dsa_shape* s);
 
 /*

@@ -172,7 +172,7 @@ SIGNATURES = {
     "dsa_tree_verify": (C.c_int32, [C.c_int32, C.c_int32, _T] + [_VP] * 8),
     "dsa_kv_append": (C.c_int32, [_P, _S, _T, _VP, _VP, _R, _VP, _VP, C.c_int32, _VP, _VP,
                                   C.POINTER(KVLayout), C.c_int64, _VP]),
-    "dsa_get_paged_launch_info": (C.c_int32, [_P, _S, C.c_int32, C.POINTER(PagedLaunchInfo)]),
+    "dsa_get_paged_launch_info": (C.c_int32, [_P, _S, C.POINTER(PagedLaunchInfo)]),
     "dsa_paged_workspace_bytes": (C.c_size_t, [_P, _S]),
     "dsa_page_update": (C.c_int32, [_P, C.c_int32, _G, _VP, _VP, C.c_int32] + [_VP] * 5),
     "dsa_page_reorder": (C.c_int32, [C.c_int32, _G, _VP, _VP]),
@@ -804,9 +804,9 @@ def page_layout(k: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
     return out
 
 
-def paged_launch_info(p: Params, s: Shape, dtype: int = KV_BF16) -> PagedLaunchInfo:
+def paged_launch_info(p: Params, s: Shape) -> PagedLaunchInfo:
     out = PagedLaunchInfo()
-    _check(lib().dsa_get_paged_launch_info(C.byref(p), C.byref(s), dtype, C.byref(out)),
+    _check(lib().dsa_get_paged_launch_info(C.byref(p), C.byref(s), C.byref(out)),
            "dsa_get_paged_launch_info")
     return out
 

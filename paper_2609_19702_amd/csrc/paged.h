@@ -61,17 +61,17 @@ struct PagedArgs {
   float* part;  // split partials (splits > 1)
   int B, Hq, Hkv, G, Lp, Ldec, mode, Ns, W, cap;
   int M, pool, lg;
-  int C, S;  // rows of a split, splits of a (request, KV head) at most
-  int f32;   // output in fp32
+  int C;    // rows of a split
+  int f32;  // output in fp32
 };
 
 // Launch of dsa_paged_attention.
 struct PagedLaunch {
-  int C, S, waves;
+  int C, S, waves;  // rows of a split, splits at most
   int64_t workgroups;
   size_t ws_bytes;
 };
-PagedLaunch paged_launch(const Derived& d, int dtype);
+PagedLaunch paged_launch(const Derived& d);
 
 struct BeamArgs {
   const void* x;
@@ -83,14 +83,15 @@ struct BeamArgs {
   double* sums;     // [B * W][chunks] sums of exp(x - max)
   float* tops;      // [B * W][chunks] maxima
   uint64_t* cands;  // [B * W][chunks][W] the largest values and their places
-  int B, W, V, chunks, per;  // per: values of a row that a workgroup takes
-  int bf16;
+  int B, W, V, chunks, per;  // per: 16-byte pieces of a row that a workgroup takes
+  bool bf16, many;
 };
 struct BeamLaunch {
   int per, chunks;
+  bool many;  // values per thread
   size_t sums, tops, cands, bytes;  // offsets in the workspace
 };
-BeamLaunch beam_launch(int B, int W, int V);
+BeamLaunch beam_launch(int B, int W, int V, bool bf16);
 
 hipError_t launch_page_update(const PageUpdateArgs& a, hipStream_t st);
 hipError_t launch_page_reorder(const PageReorderArgs& a, hipStream_t st);

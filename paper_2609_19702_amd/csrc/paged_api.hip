@@ -48,23 +48,31 @@ dsa_status check_layout(const dsa_page_layout* l) {
 dsa_status paged_derive(const dsa_params* p, const dsa_shape* s, Derived* d, PagedLaunch* l) {
   const dsa_status st = derive(p, s, d);
   if (st != DSA_OK) return st;
-  l[0] = paged_launch(*d, DSA_KV_BF16);
-  l[1] = paged_launch(*d, DSA_KV_FP8_E4M3);
-  if (std::max(l[0].workgroups, l[1].workgroups) > kInt) return DSA_ERR_INVALID_ARG;
-  return DSA_OK;
+  *l = paged_launch(*d);
+  return l->workgroups > kInt ? DSA_ERR_INVALID_ARG : DSA_OK;
 }
 
 }  // namespace
 
-PagedLaunch paged_launch(const Derived& d, int dtype) {
+// Eight waves to a workgroup.  Splits down to 256 rows, a tile per wave, where the
+// (request, KV head) pairs alone are fewer than the CUs, in all about one workgroup per
+// CU (per layer, replayed, at 256, 512 and 128 workgroups: one request of 8 heads and
+// 9472 rows at most, fp8, d = 128, 12.8, 13.7 and 14.9 us; 24 of 4 heads, 1105 rows,
+// 20.0, 24.7 and 24.8).  Up to 896 rows, three or four tiles per wave, are not split:
+// the second kernel costs more (20 pairs, 696 rows, d = 64: 7.0 us whole, 8.8 in
+// three; 32 pairs, 832 rows, d = 128: 10.6 and 10.2 in four, but 3 us less from the
+// host).  2048 rows at most, for their places in LDS.
+PagedLaunch paged_launch(const Derived& d) {
+  constexpr int64_t kWhole = 14, kLeast = 4, kMost = 32;  // units of 64 rows
   PagedLaunch l{};
   const int64_t pairs = static_cast<int64_t>(d.B) * d.Hkv;
-  const int64_t rows = d.rows_max, tiles = (rows + 31) / 32;
-  l.waves = 4;
-  const int64_t want = std::max<int64_t>(1, 1024 / pairs);
-  const int64_t per = std::clamp<int64_t>((tiles + want - 1) / want, l.waves, 64);
-  l.C = static_cast<int>(per * 32);
-  l.S = static_cast<int>(std::max<int64_t>(1, (tiles + per - 1) / per));
+  const int64_t units = (int64_t{d.rows_max} + 63) / 64;
+  const int64_t want = std::max<int64_t>(1, 256 / pairs);
+  const int64_t per =
+      units <= kWhole ? units : std::clamp<int64_t>((units + want - 1) / want, kLeast, kMost);
+  l.C = static_cast<int>(per * 64);
+  l.S = static_cast<int>((units + per - 1) / per);
+  l.waves = 8;
   l.workgroups = pairs * l.S;
   l.ws_bytes = l.S > 1 ? static_cast<size_t>(l.workgroups) * d.G * (d.D + 2) * 4 : 0;
   return l;
@@ -78,26 +86,24 @@ using dsa::PagedLaunch;
 extern "C" {
 
 DSA_API dsa_status dsa_get_paged_launch_info(const dsa_params* p, const dsa_shape* s,
-                                             int32_t dtype, dsa_paged_launch_info* out) {
+                                             dsa_paged_launch_info* out) {
   Derived d;
-  PagedLaunch l[2];
-  const dsa_status st = dsa::paged_derive(p, s, &d, l);
+  PagedLaunch l;
+  const dsa_status st = dsa::paged_derive(p, s, &d, &l);
   if (st != DSA_OK) return st;
   if (!out) return DSA_ERR_INVALID_ARG;
-  if (dtype != DSA_KV_BF16 && dtype != DSA_KV_FP8_E4M3) return DSA_ERR_INVALID_ARG;
-  const PagedLaunch& x = l[dtype == DSA_KV_FP8_E4M3];
-  out->rows_per_split = x.C;
-  out->max_splits = x.S;
-  out->waves_per_group = x.waves;
-  out->workgroups = static_cast<int32_t>(x.workgroups);
-  out->workspace_bytes = x.ws_bytes;
+  out->rows_per_split = l.C;
+  out->max_splits = l.S;
+  out->waves_per_group = l.waves;
+  out->workgroups = static_cast<int32_t>(l.workgroups);
+  out->workspace_bytes = l.ws_bytes;
   return DSA_OK;
 }
 
 DSA_API size_t dsa_paged_workspace_bytes(const dsa_params* p, const dsa_shape* s) {
   Derived d;
-  PagedLaunch l[2];
-  return dsa::paged_derive(p, s, &d, l) == DSA_OK ? std::max(l[0].ws_bytes, l[1].ws_bytes) : 0;
+  PagedLaunch l;
+  return dsa::paged_derive(p, s, &d, &l) == DSA_OK ? l.ws_bytes : 0;
 }
 
 DSA_API dsa_status dsa_page_update(const dsa_params* p, int32_t batch, const dsa_pages* pages,
@@ -214,8 +220,8 @@ DSA_API dsa_status dsa_paged_attention(const dsa_params* p, const dsa_shape* s,
                                        float* d_window_logits, void* d_ws, size_t ws_bytes,
                                        hipStream_t stream) {
   Derived d;
-  PagedLaunch both[2];
-  dsa_status st = dsa::paged_derive(p, s, &d, both);
+  PagedLaunch l;
+  dsa_status st = dsa::paged_derive(p, s, &d, &l);
   if (st != DSA_OK) return st;
   if ((st = dsa::check_pages(pages, false)) != DSA_OK) return st;
   if ((st = dsa::check_layout(layout)) != DSA_OK) return st;
@@ -227,7 +233,6 @@ DSA_API dsa_status dsa_paged_attention(const dsa_params* p, const dsa_shape* s,
   if (diagonal ? !d_plan : d_window_logits != nullptr) return DSA_ERR_INVALID_ARG;
   for (const void* x : {d_q, d_k, d_v, static_cast<const void*>(d_out)})
     if (!dsa::aligned16(x)) return DSA_ERR_INVALID_ARG;
-  const PagedLaunch& l = both[layout->dtype == DSA_KV_FP8_E4M3];
   if (l.ws_bytes && (!d_ws || ws_bytes < l.ws_bytes)) return DSA_ERR_WORKSPACE;
   if (l.ws_bytes && !dsa::aligned16(d_ws)) return DSA_ERR_INVALID_ARG;
 
@@ -263,12 +268,11 @@ DSA_API dsa_status dsa_paged_attention(const dsa_params* p, const dsa_shape* s,
   a.mode = d.mode;
   a.Ns = d.Ns;
   a.W = d.Nr;
-  a.cap = d.plan_cap;
+  a.cap = d.mode == DSA_MODE_DENSE ? d.Ldec : d.plan_cap;
   a.M = pages->max_pages;
   a.pool = layout->num_pages;
   a.lg = dsa::log_rows(pages->page_rows);
   a.C = l.C;
-  a.S = l.S;
   a.f32 = out_type == DSA_OUT_FP32;
   return dsa::hip_status(layout->dtype == DSA_KV_FP8_E4M3 ? dsa::launch_paged_fp8(d, l, a, stream)
                                                           : dsa::launch_paged_bf16(d, l, a, stream));
@@ -278,7 +282,8 @@ DSA_API size_t dsa_beam_workspace_bytes(int32_t batch, int32_t beams, int32_t vo
   if (batch < 1 || beams < 1 || beams > DSA_MAX_BEAMS || vocab < 1 || vocab > 1 << 24 ||
       int64_t{batch} * beams >= 1 << 22)
     return 0;
-  return dsa::beam_launch(batch, beams, vocab).bytes;
+  return std::max(dsa::beam_launch(batch, beams, vocab, false).bytes,
+                  dsa::beam_launch(batch, beams, vocab, true).bytes);
 }
 
 DSA_API dsa_status dsa_beam_select(int32_t batch, int32_t beams, int32_t vocab,
@@ -293,7 +298,8 @@ DSA_API dsa_status dsa_beam_select(int32_t batch, int32_t beams, int32_t vocab,
   if (stride_row < vocab) return DSA_ERR_INVALID_ARG;
   if (!d_ws || ws_bytes < need) return DSA_ERR_WORKSPACE;
   if (!dsa::aligned16(d_ws)) return DSA_ERR_INVALID_ARG;
-  const dsa::BeamLaunch l = dsa::beam_launch(batch, beams, vocab);
+  const bool bf16 = logits_type == DSA_OUT_BF16;
+  const dsa::BeamLaunch l = dsa::beam_launch(batch, beams, vocab, bf16);
   if (int64_t{batch} * beams * l.chunks > dsa::kInt) return DSA_ERR_INVALID_ARG;
   char* ws = static_cast<char*>(d_ws);
   dsa::BeamArgs a{};
@@ -311,7 +317,8 @@ DSA_API dsa_status dsa_beam_select(int32_t batch, int32_t beams, int32_t vocab,
   a.V = vocab;
   a.chunks = l.chunks;
   a.per = l.per;
-  a.bf16 = logits_type == DSA_OUT_BF16;
+  a.bf16 = bf16;
+  a.many = l.many;
   return dsa::hip_status(dsa::launch_beam(a, stream));
 }
 

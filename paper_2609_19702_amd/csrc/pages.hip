@@ -1,7 +1,5 @@
 // Page tables: pages for new rows and back, requests that go on from others'
 // pages, and the new K/V rows' way into their slots.
-#include <type_traits>
-
 #include "device.h"
 #include "paged.h"
 
@@ -10,55 +8,71 @@ namespace {
 
 constexpr int kUpdateThreads = 1024;
 constexpr int kUpdateWaves = kUpdateThreads / 64;
+constexpr int kLook = 4;  // pages that a thread looks at together
 
 // Counts that other waves change in the same launch: past the CU's cache.
 __device__ __forceinline__ int load_ref(const int32_t* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// A request of the update.
+// A request of the update, as it waits in LDS: length (below 0: unused), new rows and
+// prompt rows, and the pages needed up to it.
 struct PageReq {
-  int64_t end;  // rows after the call
-  int len, fresh, prompt;
-  int e0, e1;   // entries of the new rows
-  bool fits;    // in use, and its rows in the table
+  int len, fresh, prompt, upto;
 };
 
-__device__ __forceinline__ PageReq page_request(const PageUpdateArgs& a, int b) {
-  PageReq r;
-  r.len = a.length[b];
-  r.fresh = a.fresh ? min(max(a.fresh[b], 0), a.N) : 1;
-  r.prompt = a.prompt ? min(max(a.prompt[b], 0), a.Lp) : a.Lp;
-  r.end = static_cast<int64_t>(r.len) + r.fresh;
-  r.fits = r.len >= 0 && r.end <= static_cast<int64_t>(a.M) << a.lg;
-  const bool some = r.fits && r.fresh > 0;
-  r.e0 = some ? r.len >> a.lg : 0;
-  r.e1 = some ? static_cast<int>((r.end + (1 << a.lg) - 1) >> a.lg) : 0;
-  return r;
+// Its entries of new rows, [e0, e1); fits: it is in use, and its rows have entries.
+struct PageSpan {
+  int e0, e1;
+  bool fits;
+};
+__device__ __forceinline__ PageSpan page_span(const PageUpdateArgs& a, const PageReq& r) {
+  const int64_t end = static_cast<int64_t>(r.len) + r.fresh;
+  PageSpan s;
+  s.fits = r.len >= 0 && end <= static_cast<int64_t>(a.M) << a.lg;
+  const bool some = s.fits && r.fresh > 0;
+  s.e0 = some ? r.len >> a.lg : 0;
+  s.e1 = some ? static_cast<int>((end + (1 << a.lg) - 1) >> a.lg) : 0;
+  return s;
 }
 
 __device__ __forceinline__ bool in_pool(int page, int pool) {
   return static_cast<unsigned>(page) < static_cast<unsigned>(pool);
 }
 
-// One workgroup.  Its parts, with a barrier after each:
-//   1. a wave per request gives back the pages that ended or fell behind
-//   2. a wave per request counts the pages that its new rows need; an entry whose
-//      page is shared becomes -2 - page until part 5
-//   3. running sums of the needs
-//   4. free pages from the cursor on, 1024 looked at a time; the k-th goes to
+// One workgroup, 16 lanes to a request.  Its parts, with a barrier after each:
+//   1. lengths, new and prompt rows into LDS
+//   2. pages that ended or fell behind go back
+//   3. the pages that the new rows need are counted; an entry whose page is shared
+//      becomes -2 - page until part 6
+//   4. running sums of the needs
+//   5. free pages from the cursor on, 4096 looked at a time; the k-th goes to
 //      the request whose share of the sums k lies in, and waits in its slots
 //      (a request has a new row for every page that it needs)
-//   5. a wave per request puts them into the table
-//   6. slots
+//   6. they go into the table, and slots come out
+// Bound by the way to memory and back, some 0.7 us for each part but 4: 5 us for one
+// request.
 __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateArgs a) {
-  __shared__ int upto[DSA_MAX_PAGED_BATCH];  // needs, then their running sums
-  __shared__ int part[kUpdateWaves];
+  extern __shared__ PageReq req[];
+  __shared__ int part[kLook][kUpdateWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int sub = tid & 15, group = tid >> 4, shift = lane & 48;  // shift: of a group's ballot
   const int rows = 1 << a.lg;
 
-  for (int b = wave; b < a.B; b += kUpdateWaves) {
-    const PageReq r = page_request(a, b);
+  for (int b = tid; b < a.B; b += kUpdateThreads) {
+    PageReq r;
+    r.len = a.length[b];
+    r.fresh = a.fresh ? a.fresh[b] : 1;
+    r.prompt = a.prompt ? a.prompt[b] : a.Lp;
+    r.fresh = min(max(r.fresh, 0), a.N);
+    r.prompt = min(max(r.prompt, 0), a.Lp);
+    r.upto = 0;
+    req[b] = r;
+  }
+  __syncthreads();
+
+  for (int b = group; b < a.B; b += kUpdateThreads / 16) {
+    const PageReq r = req[b];
     int32_t* row = a.table + static_cast<int64_t>(b) * a.M;
     int lo = 0, hi = r.len < 0 ? a.M : 0;
     if (r.len >= 0 && a.W > 0) {
@@ -67,7 +81,7 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
       lo = static_cast<int>(min((front + rows - 1) >> a.lg, static_cast<int64_t>(a.M)));
       hi = back > 0 ? static_cast<int>(min(back >> a.lg, static_cast<int64_t>(a.M))) : 0;
     }
-    for (int i = lo + lane; i < hi; i += 64) {
+    for (int i = lo + sub; i < hi; i += 16) {
       const int page = row[i];
       if (in_pool(page, a.pool)) atomicSub(a.refs + page, 1);
       if (page != -1) row[i] = -1;
@@ -76,14 +90,13 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
   __threadfence();  // the counts have changed before anyone reads them
   __syncthreads();
 
-  for (int b = wave; b < a.B; b += kUpdateWaves) {
-    const PageReq r = page_request(a, b);
+  for (int b = group; b < a.B; b += kUpdateThreads / 16) {
+    const PageSpan s = page_span(a, req[b]);
     int32_t* row = a.table + static_cast<int64_t>(b) * a.M;
     int need = 0;
-    for (int i0 = r.e0; i0 < r.e1; i0 += 64) {
-      const int i = i0 + lane;
+    for (int i = s.e0 + sub; i - sub < s.e1; i += 16) {
       int want = 0;  // what the entry becomes, if anything
-      if (i < r.e1) {
+      if (i < s.e1) {
         const int page = row[i];
         if (!in_pool(page, a.pool))
           want = -1;
@@ -91,131 +104,141 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
           want = -2 - page;
         if (want && want != page) row[i] = want;
       }
-      need += __popcll(__ballot(want != 0));
+      need += __popc(static_cast<uint32_t>(__ballot(want != 0) >> shift) & 0xffffu);
     }
-    if (lane == 0) upto[b] = need;
+    if (sub == 0) req[b].upto = need;
   }
   __syncthreads();
 
   int total = 0;
   for (int b0 = 0; b0 < a.B; b0 += kUpdateThreads) {
     const int b = b0 + tid;
-    const int x = wave_scan(b < a.B ? upto[b] : 0);
-    if (lane == 63) part[wave] = x;
+    const int x = wave_scan(b < a.B ? req[b].upto : 0);
+    if (lane == 63) part[0][wave] = x;
     __syncthreads();
     int before = total;
     for (int w = 0; w < kUpdateWaves; ++w) {
-      before += w < wave ? part[w] : 0;
-      total += part[w];
+      before += w < wave ? part[0][w] : 0;
+      total += part[0][w];
     }
-    if (b < a.B) upto[b] = before + x;
+    if (b < a.B) req[b].upto = before + x;
     __syncthreads();
   }
 
   int found = 0;
   if (total > 0) {
     const int c = a.cursor[0] % a.pool, start = c < 0 ? c + a.pool : c;
-    for (int i0 = 0; i0 < a.pool && found < total; i0 += kUpdateThreads) {
-      int page = start + min(i0 + tid, a.pool - 1);
-      page = page >= a.pool ? page - a.pool : page;
-      const bool free = i0 + tid < a.pool && load_ref(a.refs + page) == 0;
-      const uint64_t mask = __ballot(free);
-      if (lane == 0) part[wave] = __popcll(mask);
+    for (int i0 = 0; i0 < a.pool && found < total; i0 += kLook * kUpdateThreads) {
+      int page[kLook], rank[kLook];
+      bool free[kLook];
+#pragma unroll
+      for (int k = 0; k < kLook; ++k) {
+        const int i = i0 + k * kUpdateThreads + tid;
+        page[k] = start + min(i, a.pool - 1);
+        page[k] = page[k] >= a.pool ? page[k] - a.pool : page[k];
+        free[k] = load_ref(a.refs + page[k]) == 0 && i < a.pool;
+      }
+#pragma unroll
+      for (int k = 0; k < kLook; ++k) {
+        const uint64_t mask = __ballot(free[k]);
+        rank[k] = __popcll(mask & ((uint64_t(1) << lane) - 1));
+        if (lane == 0) part[k][wave] = __popcll(mask);
+      }
       __syncthreads();
-      int rank = found + __popcll(mask & ((uint64_t(1) << lane) - 1));
-      for (int w = 0; w < kUpdateWaves; ++w) {
-        rank += w < wave ? part[w] : 0;
-        found += part[w];
-      }
-      if (free && rank < total) {
-        int lo = 0, hi = a.B - 1;  // the first request whose sum passes the rank
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (upto[mid] > rank) hi = mid; else lo = mid + 1;
+      // The counts of 16 waves four times over, a lane each, and their sums up to it.
+      const int mine = part[lane >> 4][lane & 15];
+      const int sums = wave_scan(mine);
+#pragma unroll
+      for (int k = 0; k < kLook; ++k) {
+        const int at = 16 * k + wave;
+        rank[k] += found + __shfl(sums - mine, at, 64);
+        if (free[k] && rank[k] < total) {
+          int lo = 0, hi = a.B - 1;  // the first request whose sum passes the rank
+          while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (req[mid].upto > rank[k]) hi = mid; else lo = mid + 1;
+          }
+          a.slots[static_cast<int64_t>(lo) * a.N + rank[k] - (lo ? req[lo - 1].upto : 0)] = page[k];
         }
-        a.slots[static_cast<int64_t>(lo) * a.N + rank - (lo ? upto[lo - 1] : 0)] = page;
       }
+      found += __shfl(sums, 63, 64);
       __syncthreads();
     }
   }
   found = min(found, total);
 
-  for (int b = wave; b < a.B; b += kUpdateWaves) {
-    const PageReq r = page_request(a, b);
-    const int before = b ? upto[b - 1] : 0, need = upto[b] - before;
-    const bool pages = need == 0 || upto[b] <= found, ok = r.fits && pages;
+  for (int b = group; b < a.B; b += kUpdateThreads / 16) {
+    const PageReq r = req[b];
+    const PageSpan s = page_span(a, r);
+    const int need = r.upto - (b ? req[b - 1].upto : 0);
+    const bool pages = need == 0 || r.upto <= found, ok = s.fits && pages;
     int32_t* row = a.table + static_cast<int64_t>(b) * a.M;
-    const int32_t* got = a.slots + static_cast<int64_t>(b) * a.N;
+    int32_t* slots = a.slots + static_cast<int64_t>(b) * a.N;
     int x = -1, y = -1;  // the first entry's old and new page, where rows are copied
-    int rank = 0;
-    if (need > 0) {
-      for (int i0 = r.e0; i0 < r.e1; i0 += 64) {
-        const int i = i0 + lane;
-        const int old = i < r.e1 ? row[i] : 0;
-        const uint64_t mask = __ballot(old < 0);
-        const int page = -2 - old;  // the shared one, or -1
-        if (old < 0 && ok) {
-          const int mine = got[rank + __popcll(mask & ((uint64_t(1) << lane) - 1))];
-          row[i] = mine;
-          atomicExch(a.refs + mine, 1);
-          if (page >= 0) atomicSub(a.refs + page, 1);
-          if (i == r.e0 && page >= 0 && (r.len & (rows - 1))) {
-            x = page;
-            y = mine;
-          }
-        } else if (old < -1) {
-          row[i] = page;
-        }
-        rank += __popcll(mask);
-      }
-      // The last page that anyone was given.
-      if (ok && lane == 0) {
-        bool last = true;
-        if (found == total) {
-          last = upto[b] == total;
-        } else {
-          for (int f = b + 1; f < a.B && last; ++f) {
-            if (upto[f] == upto[f - 1]) continue;  // needs none
-            last = upto[f] > found;
-            break;
+    int last = 0;        // the last page that the request is given
+    int got = -1;        // page of entry e0 + sub
+    for (int i = s.e0 + sub, rank = 0; i - sub < s.e1; i += 16) {
+      int now = i < s.e1 ? row[i] : 0;
+      const uint32_t mask = static_cast<uint32_t>(__ballot(now < 0) >> shift) & 0xffffu;
+      if (now < 0) {
+        const int old = -2 - now;  // the shared page, or -1
+        now = old;
+        if (ok) {
+          now = slots[rank + __popc(mask & ((1u << sub) - 1))];
+          atomicExch(a.refs + now, 1);
+          if (old >= 0) atomicSub(a.refs + old, 1);
+          if (i == s.e0 && old >= 0 && (r.len & (rows - 1))) {
+            x = old;
+            y = now;
           }
         }
-        if (last) {
-          const int next = got[need - 1] + 1;
-          a.cursor[0] = next == a.pool ? 0 : next;
-        }
+        row[i] = now;
       }
+      if (mask) last = __shfl(now, shift + 31 - __clz(mask), 64);
+      rank += __popc(mask);
+      if (i - sub == s.e0) got = now;
     }
-    if (lane == 0) {
+    if (sub == 0) {
+      // The last page that anyone was given?
+      bool end = ok && need > 0;
+      if (found == total) {
+        end &= r.upto == total;
+      } else {
+        for (int f = b + 1; f < a.B && end; ++f) {
+          if (req[f].upto == req[f - 1].upto) continue;  // needs none
+          end = req[f].upto > found;
+          break;
+        }
+      }
+      if (end) a.cursor[0] = last + 1 == a.pool ? 0 : last + 1;
       a.flags[b] = r.len < 0 ? 0
-                             : (r.fits ? (pages ? 0 : DSA_PAGE_FLAG_NO_PAGES)
+                             : (s.fits ? (pages ? 0 : DSA_PAGE_FLAG_NO_PAGES)
                                        : DSA_PAGE_FLAG_TOO_LONG);
-      const int64_t pos = r.end - 1 - r.prompt;
-      a.pos[b] = ok && pos >= 0 ? static_cast<int>(pos) : -1;
+      const int pos = r.len + r.fresh - 1 - r.prompt;  // of rows that fit
+      a.pos[b] = ok && pos >= 0 ? pos : -1;
       int32_t* told = a.copies + 3 * static_cast<int64_t>(b);
-      told[0] = x;  // lane 0 holds the first entry
+      told[0] = x;
       told[1] = y;
       told[2] = x >= 0 ? r.len & (rows - 1) : -1;
     }
     // What waited in the slots has been read: they become the rows' places.
     fence_wave();
-    int32_t* to = a.slots + static_cast<int64_t>(b) * a.N;
-    for (int i = lane; i < a.N; i += 64) {
-      int slot = -1;
-      if (ok && i < r.fresh) {
-        const int at = r.len + i;
-        slot = (row[at >> a.lg] << a.lg) + (at & (rows - 1));
-      }
-      to[i] = slot;
+    const int n = ok ? r.fresh : 0;
+    const bool few = s.e1 - s.e0 <= 16;
+    for (int i = sub; i - sub < n; i += 16) {
+      const int at = r.len + min(i, n - 1), e = at >> a.lg;
+      const int held = __shfl(got, shift + ((e - s.e0) & 15), 64);
+      if (i < n) slots[i] = ((few ? held : row[e]) << a.lg) + (at & (rows - 1));
     }
+    for (int i = n + sub; i < a.N; i += 16) slots[i] = -1;
   }
 }
 
 constexpr int kReorderThreads = 512;
-constexpr int kReorderLds = 32768;  // bytes of the columns that a workgroup holds
+constexpr int kReorderMost = 2048;  // entries that a workgroup holds, about
 
-// A workgroup takes `cols` columns of the table: all their entries into LDS, then
-// every row its parent's.
+// A workgroup takes some columns of the table: all their entries into LDS, then
+// every row its parent's.  Bound by the way to memory and back.
 __global__ __launch_bounds__(kReorderThreads) void page_reorder_kernel(PageReorderArgs a,
                                                                       int lg_cols) {
   extern __shared__ int32_t held[];  // [B][cols]
@@ -225,10 +248,11 @@ __global__ __launch_bounds__(kReorderThreads) void page_reorder_kernel(PageReord
     const int i = first + (e & (cols - 1));
     held[e] = i < a.M ? a.table[static_cast<int64_t>(e >> lg_cols) * a.M + i] : -1;
   }
+  int parent = threadIdx.x < n ? a.parent[threadIdx.x >> lg_cols] : 0;
   __syncthreads();
   for (int e = threadIdx.x; e < n; e += kReorderThreads) {
     const int b = e >> lg_cols, i = first + (e & (cols - 1));
-    const int parent = a.parent[b];
+    if (e != static_cast<int>(threadIdx.x)) parent = a.parent[b];
     if (i >= a.M || parent == b) continue;
     const int old = held[e];
     const bool there = static_cast<unsigned>(parent) < static_cast<unsigned>(a.B);
@@ -240,94 +264,113 @@ __global__ __launch_bounds__(kReorderThreads) void page_reorder_kernel(PageReord
   }
 }
 
-// bf16 values to E4M3 codes of value / scale.
-__device__ __forceinline__ uint2 fp8_codes(const uint4& x, float scale) {
-  float f[8];
+// bf16 values over a scale, within +-448 (NaN stays NaN).  With the rounded reciprocal y
+// of s and q = x * y, q + (x - q * s) * y is the rounded quotient: three operations
+// where the compiler's division takes ten.  Quotients past 1024 end at 448 by
+// either, those below 2^-12 at a zero of their sign; scales far from 1 are divided by.
+__device__ __forceinline__ void over_scale(const uint4& x, float s, float (&f)[8]) {
   unpack8(x, f);
+  const float y = 1.f / s, size = fabsf(s);
+  if (size > 0x1p-80f && size < 0x1p80f) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float y = f[i] / scale;
-    f[i] = y != y ? y : fminf(fmaxf(y, -448.f), 448.f);
+    for (int i = 0; i < 8; ++i) {
+      const float q = f[i] * y;
+      f[i] = fabsf(q) < 1024.f && fabsf(q) > 0x1p-12f ? fmaf(fmaf(-q, s, f[i]), y, q) : q;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] /= s;
   }
-  uint2 w;
-  w.x = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-  w.x = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w.x, true);
-  w.y = __builtin_amdgcn_cvt_pk_fp8_f32(f[4], f[5], 0, false);
-  w.y = __builtin_amdgcn_cvt_pk_fp8_f32(f[6], f[7], w.y, true);
-  return w;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = f[i] != f[i] ? f[i] : fminf(fmaxf(f[i], -448.f), 448.f);
 }
 
-// Eight elements of a K row and of its V row per thread.  The first `blocks`
+__device__ __forceinline__ uint4 fp8_codes(const uint4& a, const uint4& b, float scale) {
+  uint32_t w[4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float f[8];
+    over_scale(h ? b : a, scale, f);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      int c = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i], f[4 * i + 1], 0, false);
+      c = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i + 2], f[4 * i + 3], c, true);
+      w[2 * h + i] = static_cast<uint32_t>(c);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// 16 bytes of a K row and of its V row in the cache per thread.  The first `blocks`
 // workgroups of a (layer, request) take new rows, the others rows of its copy.
-template <bool FP8>
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a, int chunks,
-                                                           int blocks, int copy_blocks) {
+template <bool FP8, int D>
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a, int blocks,
+                                                           int copy_blocks) {
+  constexpr int chunks = D * (FP8 ? 1 : 2) / 16;
   const int per = blocks + copy_blocks;
-  const int64_t lb = blockIdx.x / per;
-  const int b = static_cast<int>(lb % a.B), layer = static_cast<int>(lb / a.B);
+  const int lb = blockIdx.x / per, b = lb % a.B, layer = lb / a.B;
   const int block = blockIdx.x % per;
   const int rows = 1 << a.lg;
+  const unsigned at = (block < blocks ? block : block - blocks) * 256u + threadIdx.x;
+  const int c = at % chunks, h = at / chunks % static_cast<unsigned>(a.Hkv);
+  const int i = at / chunks / static_cast<unsigned>(a.Hkv);
+  const int64_t cache = layer * a.sl + h * a.sh + c * 16;
   if (block < blocks) {
-    const int at = block * 256 + threadIdx.x;
-    const int c = at % chunks, h = at / chunks % a.Hkv, i = at / chunks / a.Hkv;
     if (i >= a.N) return;
     const int slot = a.slots[static_cast<int64_t>(b) * a.N + i];
     if (!in_pool(slot >> a.lg, a.pool)) return;  // a negative slot is of no page
-    const int64_t from = layer * a.nsl + b * a.nsb + i * a.nsn + h * a.nsh + c * 8;
-    const int64_t to = layer * a.sl + (slot >> a.lg) * a.sp + h * a.sh +
-                       (slot & (rows - 1)) * a.sr + c * (FP8 ? 8 : 16);
-    const uint4 xk = *reinterpret_cast<const uint4*>(a.kn + from);
-    const uint4 xv = *reinterpret_cast<const uint4*>(a.vn + from);
+    const int64_t from = layer * a.nsl + b * a.nsb + i * a.nsn + h * a.nsh + c * (FP8 ? 16 : 8);
+    const int64_t to = cache + (slot >> a.lg) * a.sp + (slot & (rows - 1)) * a.sr;
+    uint4 k = load_stream16(a.kn + from), v = load_stream16(a.vn + from);
     if constexpr (FP8) {
+      const uint4 k1 = load_stream16(a.kn + from + 8), v1 = load_stream16(a.vn + from + 8);
       const int s = layer * a.Hkv + h;
-      *reinterpret_cast<uint2*>(a.k + to) = fp8_codes(xk, a.ks ? a.ks[s] : 1.f);
-      *reinterpret_cast<uint2*>(a.v + to) = fp8_codes(xv, a.vs ? a.vs[s] : 1.f);
-    } else {
-      *reinterpret_cast<uint4*>(a.k + to) = xk;
-      *reinterpret_cast<uint4*>(a.v + to) = xv;
+      k = fp8_codes(k, k1, a.ks ? a.ks[s] : 1.f);
+      v = fp8_codes(v, v1, a.vs ? a.vs[s] : 1.f);
     }
+    *reinterpret_cast<uint4*>(a.k + to) = k;
+    *reinterpret_cast<uint4*>(a.v + to) = v;
     return;
   }
   const int32_t* told = a.copies + 3 * static_cast<int64_t>(b);
   const int x = told[0], y = told[1], n = min(told[2], rows);
-  if (!in_pool(x, a.pool) || !in_pool(y, a.pool) || x == y) return;
-  const int at = (block - blocks) * 256 + threadIdx.x;
-  const int c = at % chunks, h = at / chunks % a.Hkv, i = at / chunks / a.Hkv;
-  if (i >= n) return;
-  using Raw = std::conditional_t<FP8, uint2, uint4>;
-  const int64_t in = layer * a.sl + h * a.sh + i * a.sr + c * static_cast<int>(sizeof(Raw));
-  const Raw rk = *reinterpret_cast<const Raw*>(a.k + in + x * a.sp);
-  const Raw rv = *reinterpret_cast<const Raw*>(a.v + in + x * a.sp);
-  *reinterpret_cast<Raw*>(a.k + in + y * a.sp) = rk;
-  *reinterpret_cast<Raw*>(a.v + in + y * a.sp) = rv;
+  if (!in_pool(x, a.pool) || !in_pool(y, a.pool) || x == y || i >= n) return;
+  const int64_t in = cache + i * a.sr;
+  const uint4 k = *reinterpret_cast<const uint4*>(a.k + in + x * a.sp);
+  const uint4 v = *reinterpret_cast<const uint4*>(a.v + in + x * a.sp);
+  *reinterpret_cast<uint4*>(a.k + in + y * a.sp) = k;
+  *reinterpret_cast<uint4*>(a.v + in + y * a.sp) = v;
+}
+
+template <bool FP8, int D>
+void append_grid(const PagedAppendArgs& a, hipStream_t st) {
+  const int64_t row = static_cast<int64_t>(a.Hkv) * (D * (FP8 ? 1 : 2) / 16);
+  const int blocks = static_cast<int>((a.N * row + 255) / 256);
+  const int copies = a.copies ? static_cast<int>(((row << a.lg) + 255) / 256) : 0;
+  const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(blocks + copies) * a.layers * a.B));
+  paged_append_kernel<FP8, D><<<grid, dim3(256), 0, st>>>(a, blocks, copies);
 }
 
 }  // namespace
 
 hipError_t launch_page_update(const PageUpdateArgs& a, hipStream_t st) {
-  page_update_kernel<<<dim3(1), dim3(kUpdateThreads), 0, st>>>(a);
+  page_update_kernel<<<dim3(1), dim3(kUpdateThreads), a.B * sizeof(PageReq), st>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_page_reorder(const PageReorderArgs& a, hipStream_t st) {
   int lg = 0;
-  while (lg < 4 && (static_cast<int64_t>(a.B) << (lg + 1)) * 4 <= kReorderLds && (1 << lg) < a.M)
-    ++lg;
+  while (lg < 4 && (a.B << (lg + 1)) <= kReorderMost && (1 << lg) < a.M) ++lg;
   const int groups = (a.M + (1 << lg) - 1) >> lg;
   page_reorder_kernel<<<dim3(groups), dim3(kReorderThreads), (a.B << lg) * 4, st>>>(a, lg);
   return hipGetLastError();
 }
 
 hipError_t launch_paged_append(const PagedAppendArgs& a, int dtype, hipStream_t st) {
-  const int chunks = a.D / 8;
-  const int64_t row = static_cast<int64_t>(a.Hkv) * chunks;
-  const int blocks = static_cast<int>((a.N * row + 255) / 256);
-  const int copies = a.copies ? static_cast<int>(((row << a.lg) + 255) / 256) : 0;
-  const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(blocks + copies) * a.layers * a.B));
   if (dtype == DSA_KV_FP8_E4M3)
-    paged_append_kernel<true><<<grid, dim3(256), 0, st>>>(a, chunks, blocks, copies);
+    a.D == 64 ? append_grid<true, 64>(a, st) : append_grid<true, 128>(a, st);
   else
-    paged_append_kernel<false><<<grid, dim3(256), 0, st>>>(a, chunks, blocks, copies);
+    a.D == 64 ? append_grid<false, 64>(a, st) : append_grid<false, 128>(a, st);
   return hipGetLastError();
 }
 
