@@ -801,6 +801,7 @@ def page_layout(k: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                      KV_BF16 if k.dtype == torch.bfloat16 else KV_FP8_E4M3)
     out._held = (k_scale, v_scale)
     out.scales = min([x.numel() for x in out._held if x is not None], default=1 << 62)
+    out._fits = None  # the caches' values that _check_paged last let through
     return out
 
 
@@ -813,6 +814,16 @@ def paged_launch_info(p: Params, s: Shape) -> PagedLaunchInfo:
 
 def paged_workspace_bytes(p: Params, s: Shape) -> int:
     return lib().dsa_paged_workspace_bytes(C.byref(p), C.byref(s))
+
+
+def _device_of(x):
+    """The current device, where x is on a GPU (its context is there)."""
+    return torch._C._cuda_getDevice() if x.is_cuda else None
+
+
+def _stream_on(stream, device):
+    return (torch._C._cuda_getCurrentRawStream(device) if stream is None
+            else stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
 def _need_pages(pages, device, batch, where, refs=False, cursor=False):
@@ -828,7 +839,7 @@ def page_update(p, pages: Pages, length, new, slots, pos, copies, flags, stream=
     """Pages for a step's new rows: ``length`` int32 [B] (below 0: an unused slot),
     ``new`` int32 [B] or None (1 each); out: ``slots`` int32 [B, N], ``pos`` [B],
     ``copies`` [B, 3], ``flags`` [B], all int32."""
-    device = torch.cuda.current_device() if length.is_cuda else None
+    device = _device_of(length)
     batch = length.shape[0]
     _need_dense(length, "length", torch.int32, (batch,), device)
     _need_pages(pages, device, batch, "page_update", refs=True, cursor=True)
@@ -842,30 +853,34 @@ def page_update(p, pages: Pages, length, new, slots, pos, copies, flags, stream=
     _need_dense(flags, "flags", torch.int32, (batch,), device)
     _check(lib().dsa_page_update(
         C.byref(p), batch, pages.ref, length.data_ptr(), _ptr(new), slots.shape[1],
-        slots.data_ptr(), pos.data_ptr(), copies.data_ptr(), flags.data_ptr(), _stream(stream)),
+        slots.data_ptr(), pos.data_ptr(), copies.data_ptr(), flags.data_ptr(), _stream_on(stream, device)),
         "dsa_page_update")
 
 
 def page_reorder(pages: Pages, parent, stream=None):
     """Every request goes on from the pages of request ``parent[b]`` (int32 [B])."""
-    device = torch.cuda.current_device() if parent.is_cuda else None
+    device = _device_of(parent)
     _need_dense(parent, "parent", torch.int32, (pages.batch,), device)
     _need_pages(pages, device, pages.batch, "page_reorder", refs=True)
-    _check(lib().dsa_page_reorder(pages.batch, pages.ref, parent.data_ptr(), _stream(stream)),
+    _check(lib().dsa_page_reorder(pages.batch, pages.ref, parent.data_ptr(), _stream_on(stream, device)),
            "dsa_page_reorder")
 
 
 def _check_paged(s, k, v, layout, layers, device):
     """The caches against their layout, their scales and the shape."""
-    shape, st = k.shape, k.stride()
-    if k.dtype not in _KV_DTYPES or k.dtype is not v.dtype or shape != v.shape or st != v.stride():
+    shape, st, dtype = k.shape, k.stride(), k.dtype
+    if (dtype is v.dtype and shape == v.shape and st == v.stride() and k.get_device() == device
+            and v.get_device() == device
+            and layout._fits == (dtype, shape, st, layers, s.num_kv_heads, s.head_dim, device)):
+        return  # what follows has been looked at for these values
+    if dtype not in _KV_DTYPES or dtype is not v.dtype or shape != v.shape or st != v.stride():
         raise ValueError("k and v must share element type (bf16 or fp8), shape and strides")
     for x, name in ((k, "k"), (v, "v")):
         if x.get_device() != device:
             _need(x, name, contiguous=False)
             raise _elsewhere(x, name, device)
-    if (layout.dtype == KV_BF16) != (k.dtype is torch.bfloat16):
-        raise ValueError(f"the layout is not of a {k.dtype} cache")
+    if (layout.dtype == KV_BF16) != (dtype is torch.bfloat16):
+        raise ValueError(f"the layout is not of a {dtype} cache")
     if len(shape) != (4 if layers is None else 5) or (layers is not None and shape[0] != layers):
         raise ValueError(f"caches of shape {tuple(shape)} are not of "
                          + ("one layer" if layers is None else f"{layers} layers"))
@@ -882,6 +897,7 @@ def _check_paged(s, k, v, layout, layers, device):
     for x in layout._held:
         if x is not None and x.get_device() != device:
             raise _elsewhere(x, "a scale", device)
+    layout._fits = (dtype, shape, st, layers, s.num_kv_heads, s.head_dim, device)
 
 
 def paged_append(s, slots, k_new, v_new, k, v, layout: PageLayout, copies=None, stream=None):
@@ -889,7 +905,7 @@ def paged_append(s, slots, k_new, v_new, k, v, layout: PageLayout, copies=None, 
     pages that ``copies`` (int32 [B, 3]) names.  One layer (``k_new`` [B, N, Hkv,
     d], ``k`` [num_pages, Hkv, page_rows, d]) or all of them (both with layers in
     front, ``layout`` of one layer's cache but with the scales of all)."""
-    device = torch.cuda.current_device() if k_new.is_cuda else None
+    device = _device_of(k_new)
     B_, Hkv, d = s.batch, s.num_kv_heads, s.head_dim
     layers = k_new.shape[0] if k_new.dim() == 5 else None
     if slots.dim() != 2:
@@ -904,7 +920,7 @@ def paged_append(s, slots, k_new, v_new, k, v, layout: PageLayout, copies=None, 
     _check(lib().dsa_paged_append(
         C.byref(s), n, slots.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), C.byref(rows),
         layers or 1, k.data_ptr(), v.data_ptr(), C.byref(layout), k.stride(0) if layers else 0,
-        _ptr(copies), _stream(stream)), "dsa_paged_append")
+        _ptr(copies), _stream_on(stream, device)), "dsa_paged_append")
 
 
 def paged_attention(p, s, pages: Pages, q, k, v, layout: PageLayout, decode_pos, sm_scale, out,
@@ -912,7 +928,7 @@ def paged_attention(p, s, pages: Pages, q, k, v, layout: PageLayout, decode_pos,
     """Attention of one token per request (``q`` bf16 [B, Hq, d]) over its pages;
     ``out`` [B, Hq, d] in fp32 or bf16.  Diagonal mode takes the step's plan, and
     the window logits fp32 [B, Hq, cap] where the selection is to read them."""
-    device = torch.cuda.current_device() if q.is_cuda else None
+    device = _device_of(q)
     B_, shape = s.batch, (s.batch, s.num_q_heads, s.head_dim)
     _need_dense(q, "q", torch.bfloat16, shape, device)
     _need_pages(pages, device, B_, "paged_attention")
@@ -934,7 +950,7 @@ def paged_attention(p, s, pages: Pages, q, k, v, layout: PageLayout, decode_pos,
         C.byref(p), C.byref(s), pages.ref, q.data_ptr(), k.data_ptr(), v.data_ptr(),
         C.byref(layout), decode_pos.data_ptr(), _ptr(plan_buf), sm_scale, out.data_ptr(), out_type,
         _ptr(window_logits), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
-        _stream(stream)), "dsa_paged_attention")
+        _stream_on(stream, device)), "dsa_paged_attention")
 
 
 def beam_workspace_bytes(batch: int, beams: int, vocab: int) -> int:
@@ -946,7 +962,7 @@ def beam_select(logits, score, next_score, parent, token, workspace, stream=None
     fp32 or bf16 (rows dense and evenly apart), ``score`` fp32 [B, beams]; out:
     ``next_score`` fp32 (may be ``score``), ``parent`` and ``token`` int32, all
     [B, beams]; parents as ``page_reorder`` takes them, flattened."""
-    device = torch.cuda.current_device() if logits.is_cuda else None
+    device = _device_of(logits)
     if logits.dim() != 3:
         raise ValueError(f"logits must be [B, beams, V], got {tuple(logits.shape)}")
     batch, beams, vocab = logits.shape
@@ -969,7 +985,7 @@ def beam_select(logits, score, next_score, parent, token, workspace, stream=None
     _check(lib().dsa_beam_select(
         batch, beams, vocab, logits.data_ptr(), row, kind, score.data_ptr(), next_score.data_ptr(),
         parent.data_ptr(), token.data_ptr(), _ptr(workspace),
-        0 if workspace is None else workspace.nbytes, _stream(stream)), "dsa_beam_select")
+        0 if workspace is None else workspace.nbytes, _stream_on(stream, device)), "dsa_beam_select")
 
 
 # ---- buffers (torch allocations) and views --------------------------------------

@@ -27,19 +27,42 @@ __device__ __forceinline__ int key_place(uint64_t k) { return ~static_cast<int>(
 
 __device__ __forceinline__ uint64_t wave_max_u64(uint64_t x) { return ~wave_min_u64(~x); }
 
+// Sum over the wave by DPP and lane swaps, as wave_allreduce.
+template <typename Get>
+__device__ __forceinline__ double add_f64(double x, Get get) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = get(static_cast<uint32_t>(u)), hi = get(static_cast<uint32_t>(u >> 32));
+  return x + __builtin_bit_cast(double, (static_cast<uint64_t>(hi) << 32) | lo);
+}
+template <int OFF>
+__device__ __forceinline__ double add_swapped(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  float lo0, lo1, hi0, hi1;
+  xor_pair<OFF>(__uint_as_float(static_cast<uint32_t>(u)), lo0, lo1);
+  xor_pair<OFF>(__uint_as_float(static_cast<uint32_t>(u >> 32)), hi0, hi1);
+  auto join = [](float hi, float lo) {
+    return __builtin_bit_cast(double, (static_cast<uint64_t>(__float_as_uint(hi)) << 32) |
+                                          __float_as_uint(lo));
+  };
+  return join(hi0, lo0) + join(hi1, lo1);
+}
 __device__ __forceinline__ double wave_sum_f64(double x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o, 64);
-  return x;
+  x = add_f64(x, [](uint32_t y) { return dpp_i<kDppQuadSwap1>(y); });
+  x = add_f64(x, [](uint32_t y) { return dpp_i<kDppQuadSwap2>(y); });
+  x = add_f64(x, [](uint32_t y) { return dpp_i<kDppHalfMirror>(y); });
+  x = add_f64(x, [](uint32_t y) { return dpp_i<kDppRowMirror>(y); });
+  return add_swapped<32>(add_swapped<16>(x));
 }
 
-// Lane's key among the first n lanes' (all different but for 0): how many are larger.
-__device__ __forceinline__ int key_rank(uint64_t key, int n) {
+// How many of the n keys of a list in LDS are larger than `key`; n a multiple of 4.
+__device__ __forceinline__ int key_rank(uint64_t key, const uint64_t* list, int n) {
   int rank = 0;
-  for (int j = 0; j < n; ++j) {
-    const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(key >> 32), j);
-    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(key), j);
-    rank += ((static_cast<uint64_t>(hi) << 32) | lo) > key;
+  for (int j = 0; j < n; j += 4) {
+    uint64_t k[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k[i] = list[j + i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) rank += k[i] > key;
   }
   return rank;
 }
@@ -47,16 +70,21 @@ __device__ __forceinline__ int key_rank(uint64_t key, int n) {
 // A workgroup takes R values per thread of a row: their maximum, the sum of their
 // exponentials (fours in fp32, the rest in fp64), and their W largest in order.
 //
-// A wave's W largest are at least its W-th largest of the lanes' own maxima, and
-// few values are: those go into a list, where each is placed by the larger ones' number.
-// With more than 64 of them (equal values) the largest are taken out one at a time.
+// The W largest are not below the W-th largest of the maxima of the workgroup's 32
+// groups of eight lanes, and few values are (about 10 of 8192 for eight beams, 22 for
+// sixteen): those go into a list, where each is placed by the larger ones' number.
+// With more than 64 of them (equal values) every wave takes its largest out one at a
+// time.
 template <bool BF16, int R>
 __global__ __launch_bounds__(kBeamThreads) void beam_row_kernel(BeamArgs a) {
   constexpr int VL = BF16 ? 8 : 4, NV = R / VL;  // values of a load, loads
-  __shared__ float top_s[kBeamWaves];
+  constexpr int kGroups = kBeamThreads / 8;
+  static_assert(kGroups >= DSA_MAX_BEAMS && kGroups <= 64 && kBeamWaves * DSA_MAX_BEAMS <= 64,
+                "a lane each");
+  __shared__ __attribute__((aligned(16))) float top_s[kGroups];
   __shared__ double sum_s[kBeamWaves];
-  __shared__ uint64_t list_s[kBeamWaves][64];
-  __shared__ uint64_t best_s[64];
+  __shared__ __attribute__((aligned(16))) uint64_t list_s[64];
+  __shared__ int n_s;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int chunk = blockIdx.x % a.chunks, row = blockIdx.x / a.chunks;
   // Pieces of VL values, which begin at any value: a row's sums do not depend on where it
@@ -103,10 +131,24 @@ __global__ __launch_bounds__(kBeamThreads) void beam_row_kernel(BeamArgs a) {
   float mine = -__builtin_inff();
 #pragma unroll
   for (int i = 0; i < R; ++i) mine = fmaxf(mine, x[i]);
-  float top = wave_max(mine);
-  if (lane == 0) top_s[wave] = top;
+  mine = fmaxf(mine, dpp<kDppQuadSwap1>(mine));
+  mine = fmaxf(mine, dpp<kDppQuadSwap2>(mine));
+  mine = fmaxf(mine, dpp<kDppHalfMirror>(mine));
+  if ((lane & 7) == 0) top_s[threadIdx.x >> 3] = mine;
+  if (threadIdx.x < 64) list_s[threadIdx.x] = 0;
+  if (threadIdx.x == 0) n_s = 0;
   __syncthreads();
-  for (int w = 0; w < kBeamWaves; ++w) top = fmaxf(top, top_s[w]);
+  const float group = lane < kGroups ? top_s[lane] : -__builtin_inff();
+  const float top = wave_max(group);
+  int larger = 0;
+#pragma unroll
+  for (int j = 0; j < kGroups; ++j) {
+    const float y = top_s[j];
+    larger += y > group || (y == group && j < lane);
+  }
+  const uint64_t at_w = __ballot(lane < kGroups && larger == a.W - 1);  // one lane
+  const float least = fmaxf(__shfl(group, __builtin_ctzll(at_w), 64), -3.402823466e38f);
+
   // A chunk of -infinities adds nothing; a NaN or +infinity makes the sum a NaN.
   double sum = 0.;
   const float base = top > -__builtin_inff() ? top : 0.f;
@@ -120,35 +162,16 @@ __global__ __launch_bounds__(kBeamThreads) void beam_row_kernel(BeamArgs a) {
   sum = wave_sum_f64(sum);
   if (lane == 0) sum_s[wave] = sum;
 
-  // The W-th largest of the lanes' maxima.
-  float least = -__builtin_inff(), left = mine;
-  for (int k = 0; k < a.W; ++k) {
-    least = wave_max(left);
-    if (lane == __builtin_ctzll(__ballot(left == least))) left = -__builtin_inff();
-  }
-  int n = 0;
-  uint64_t* list = list_s[wave];
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    const bool in = x[i] >= least && x[i] > -__builtin_inff();
-    const uint64_t some = __ballot(in);
-    if (some) {
-      const int at = n + __popcll(some & ((uint64_t(1) << lane) - 1));
-      if (in && at < 64) list[at] = beam_key(x[i], place(i));
-      n += __popcll(some);
+  for (int i = 0; i < R; ++i)
+    if (x[i] >= least) {
+      const int at = atomicAdd(&n_s, 1);
+      if (at < 64) list_s[at] = beam_key(x[i], place(i));
     }
-  }
-  fence_wave();
-  uint64_t best = 0;  // lane i: the i-th
-  if (n <= 64) {
-    const uint64_t key = lane < n ? list[lane] : 0;
-    const int rank = key_rank(key, n);
-    fence_wave();
-    if (lane < n && rank < a.W) list[rank] = key;
-    fence_wave();
-    best = lane < min(n, a.W) ? list[lane] : 0;
-  } else {
-    uint64_t under = ~uint64_t{0};
+  __syncthreads();
+  int n = n_s;
+  if (n > 64) {
+    uint64_t best = 0, under = ~uint64_t{0};  // lane i: the wave's i-th
     for (int k = 0; k < a.W; ++k) {
       uint64_t most = 0;
 #pragma unroll
@@ -159,13 +182,14 @@ __global__ __launch_bounds__(kBeamThreads) void beam_row_kernel(BeamArgs a) {
       under = wave_max_u64(most);
       if (lane == k) best = under;
     }
+    __syncthreads();  // all have read n_s, and the list ends
+    if (lane < a.W) list_s[wave * a.W + lane] = best;
+    __syncthreads();
+    n = kBeamWaves * a.W;
   }
-  if (lane < a.W) best_s[wave * a.W + lane] = best;
-  __syncthreads();
   if (wave) return;
-  const int all = kBeamWaves * a.W;  // at most 64
-  const uint64_t key = lane < all ? best_s[lane] : 0;
-  const int rank = key_rank(key, all);
+  const uint64_t key = lane < n ? list_s[lane] : 0;
+  const int rank = key_rank(key, list_s, (n + 3) & ~3);
   uint64_t* to = a.cands + static_cast<int64_t>(blockIdx.x) * a.W;
   const int some = __popcll(__ballot(key != 0));
   if (key && rank < a.W) to[rank] = key;
@@ -178,23 +202,51 @@ __global__ __launch_bounds__(kBeamThreads) void beam_row_kernel(BeamArgs a) {
   }
 }
 
-// A workgroup per request, a wave per beam: the wave joins its chunks, all take the
-// best of the beams' W * W candidates, a thread each.
+// A candidate of the last steps: its score, and its beam and token in 28 bits.
+struct BeamCand {
+  double z;
+  int place;
+};
+__device__ __forceinline__ BeamCand beam_cand(double off, int w, uint64_t key) {
+  const double z = off + static_cast<double>(key_value(key));
+  const bool ok = key && z > -__builtin_inf();  // not so for a NaN
+  return {ok ? z : -__builtin_inf(), ok ? w << 24 | key_place(key) : 0x7fffffff};
+}
+// How many of n candidates come before each of them, into rank[n] (zeros): the workgroup's
+// threads share the comparisons.
+__device__ __forceinline__ void cand_ranks(const double* z, const int* place, int n, int* rank) {
+  const int tid = threadIdx.x, i = tid % n, parts = blockDim.x / n;
+  const double zi = z[i];
+  const int at = place[i];
+  int before = 0;
+  if (tid < parts * n)
+    for (int j = tid / n; j < n; j += parts) before += z[j] > zi || (z[j] == zi && place[j] < at);
+  if (before) atomicAdd(rank + i, before);
+}
+
+// A workgroup per request, a wave per beam.  The wave joins its chunks' sums and finds
+// its W best chunks, by the first of their sorted keys; of all beams' the W best
+// chunks hold the W best candidates.  A thread each, ranked by how many come before.
 __global__ __launch_bounds__(64 * DSA_MAX_BEAMS) void beam_pick_kernel(BeamArgs a) {
-  __shared__ double score_s[DSA_MAX_BEAMS * DSA_MAX_BEAMS];
-  __shared__ int64_t place_s[DSA_MAX_BEAMS * DSA_MAX_BEAMS];
+  constexpr int kAll = DSA_MAX_BEAMS * DSA_MAX_BEAMS;
+  __shared__ double z_s[kAll];
+  __shared__ int place_s[kAll], chunk_s[kAll], best_s[DSA_MAX_BEAMS];
+  __shared__ double off_s[DSA_MAX_BEAMS];
+  __shared__ int rank_s[2][kAll], some_s;
+  __shared__ __attribute__((aligned(16))) uint64_t head_s[DSA_MAX_BEAMS][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b = blockIdx.x, n = a.W * a.W;
   const int64_t beam = static_cast<int64_t>(b) * a.W + wave, part = beam * a.chunks;
-  const double none = -__builtin_inf();
-  const float old = a.score[beam];
-
-  // The first chunks, and the first keys, a lane each.
   const uint64_t* keys = a.cands + part * a.W;
-  const int held = a.chunks * a.W;
-  uint64_t k0 = lane < held ? keys[lane] : 0, k1 = lane + 64 < held ? keys[lane + 64] : 0;
-  float t0 = lane < a.chunks ? a.tops[part + lane] : -__builtin_inff();
-  const double s0 = lane < a.chunks ? a.sums[part + lane] : 0.;
+  const float old = a.score[beam];
+  const bool one = lane < a.chunks;
+  const float t0 = one ? a.tops[part + lane] : -__builtin_inff();
+  const double s0 = one ? a.sums[part + lane] : 0.;
+  const uint64_t k0 = one ? keys[static_cast<int64_t>(lane) * a.W] : 0;
+  if (tid < DSA_MAX_BEAMS) best_s[tid] = -1;
+  if (tid < n) rank_s[0][tid] = rank_s[1][tid] = 0;
+  if (tid == 0) some_s = 0;
+
   float top = t0;
   for (int c = lane + 64; c < a.chunks; c += 64) top = fmaxf(top, a.tops[part + c]);
   top = wave_max(top);
@@ -205,41 +257,75 @@ __global__ __launch_bounds__(64 * DSA_MAX_BEAMS) void beam_pick_kernel(BeamArgs 
   for (int c = lane + 64; c < a.chunks; c += 64) sum += scaled(a.tops[part + c], a.sums[part + c]);
   sum = wave_sum_f64(sum);
   const double off = static_cast<double>(old) - (static_cast<double>(top) + log(sum));
+  if (lane == 0) off_s[wave] = off;
 
-  // The beam's W largest logits, one at a time.
-  uint64_t under = ~uint64_t{0}, best = 0;
-  for (int k = 0; k < a.W; ++k) {
-    uint64_t most = k0 < under ? k0 : 0;
-    most = k1 < under && k1 > most ? k1 : most;
-    for (int e = lane + 128; e < held; e += 64) {
-      const uint64_t key = keys[e];
-      most = key < under && key > most ? key : most;
-    }
-    under = wave_max_u64(most);
-    if (lane == k) best = under;
-  }
+  // The beam's best chunks (keys are all different but for 0, which is none).
+  const int mine = wave * a.W;
   if (lane < a.W) {
-    const double z = off + static_cast<double>(key_value(best));
-    score_s[wave * a.W + lane] = best && z > none ? z : none;
-    place_s[wave * a.W + lane] = static_cast<int64_t>(wave) * a.V + key_place(best);
+    z_s[mine + lane] = -__builtin_inf();
+    place_s[mine + lane] = 0x7fffffff;
+    chunk_s[mine + lane] = -1;
+  }
+  fence_wave();
+  if (a.chunks <= 64) {
+    head_s[wave][lane] = k0;
+    fence_wave();
+    const int rank = key_rank(k0, head_s[wave], (a.chunks + 3) & ~3);
+    if (k0 && rank < a.W) {
+      const BeamCand c = beam_cand(off, wave, k0);
+      z_s[mine + rank] = c.z;
+      place_s[mine + rank] = c.place;
+      chunk_s[mine + rank] = mine / a.W * a.chunks + lane;
+    }
+  } else {
+    uint64_t under = ~uint64_t{0};
+    for (int k = 0; k < a.W; ++k) {
+      uint64_t most = 0;
+      int at = -1;
+      for (int c = lane; c < a.chunks; c += 64) {
+        const uint64_t key = keys[static_cast<int64_t>(c) * a.W];
+        if (key < under && key > most) {
+          most = key;
+          at = c;
+        }
+      }
+      under = wave_max_u64(most);
+      if (under && most == under) {
+        const BeamCand c = beam_cand(off, wave, most);
+        z_s[mine + k] = c.z;
+        place_s[mine + k] = c.place;
+        chunk_s[mine + k] = mine / a.W * a.chunks + at;
+      }
+    }
   }
   __syncthreads();
+  cand_ranks(z_s, place_s, n, rank_s[0]);
+  __syncthreads();
+  if (tid < n && z_s[tid] > -__builtin_inf() && rank_s[0][tid] < a.W)
+    best_s[rank_s[0][tid]] = chunk_s[tid];
+  __syncthreads();
+  if (tid < n) {  // the best chunks' keys
+    const int chunk = best_s[tid / a.W], w = chunk < 0 ? 0 : chunk / a.chunks;
+    const uint64_t key = chunk < 0 ? 0
+                                   : a.cands[(static_cast<int64_t>(b) * a.W * a.chunks + chunk) * a.W +
+                                             tid % a.W];
+    const BeamCand c = beam_cand(off_s[w], w, key);
+    z_s[tid] = c.z;
+    place_s[tid] = c.place;
+    if (c.z > -__builtin_inf()) atomicAdd(&some_s, 1);
+  }
+  __syncthreads();
+  cand_ranks(z_s, place_s, n, rank_s[1]);
+  __syncthreads();
   if (tid >= n) return;
-  const double z = score_s[tid];
-  const int64_t at = place_s[tid];
-  int rank = 0, some = 0;
-  for (int j = 0; j < n; ++j) {
-    const double y = score_s[j];
-    rank += y > z || (y == z && place_s[j] < at);
-    some += y > none;
-  }
+  const int rank = rank_s[1][tid];
   const int64_t to = static_cast<int64_t>(b) * a.W;
-  if (z > none && rank < a.W) {
-    a.next[to + rank] = static_cast<float>(z);
-    a.parent[to + rank] = b * a.W + static_cast<int>(at / a.V);
-    a.token[to + rank] = static_cast<int>(at % a.V);
+  if (z_s[tid] > -__builtin_inf() && rank < a.W) {
+    a.next[to + rank] = static_cast<float>(z_s[tid]);
+    a.parent[to + rank] = b * a.W + (place_s[tid] >> 24);
+    a.token[to + rank] = place_s[tid] & 0xffffff;
   }
-  if (tid >= some && tid < a.W) {
+  if (tid >= some_s && tid < a.W) {  // where there are fewer
     a.next[to + tid] = -__builtin_inff();
     a.parent[to + tid] = -1;
     a.token[to + tid] = -1;

@@ -87,7 +87,9 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
       if (page != -1) row[i] = -1;
     }
   }
-  __threadfence();  // the counts have changed before anyone reads them
+  // The counts have changed (in the L2, where all of them are read) before anyone
+  // reads them.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
 
   for (int b = group; b < a.B; b += kUpdateThreads / 16) {
