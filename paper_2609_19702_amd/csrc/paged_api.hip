@@ -61,9 +61,9 @@ dsa_status paged_derive(const dsa_params* p, const dsa_shape* s, Derived* d, Pag
 // 20.0, 24.7 and 24.8).  Up to 896 rows, three or four tiles per wave, are not split:
 // the second kernel costs more (20 pairs, 696 rows, d = 64: 7.0 us whole, 8.8 in
 // three; 32 pairs, 832 rows, d = 128: 10.6 and 10.2 in four, but 3 us less from the
-// host).  2048 rows at most, for their places in LDS.
+// host).  4096 rows at most, for their places in LDS.
 PagedLaunch paged_launch(const Derived& d) {
-  constexpr int64_t kWhole = 14, kLeast = 4, kMost = 32;  // units of 64 rows
+  constexpr int64_t kWhole = 14, kLeast = 4, kMost = 64;  // units of 64 rows
   PagedLaunch l{};
   const int64_t pairs = static_cast<int64_t>(d.B) * d.Hkv;
   const int64_t units = (int64_t{d.rows_max} + 63) / 64;

@@ -25,16 +25,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {  // nearest ev
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
 }
 
-// 16 bytes of each lane straight into LDS, one lane's after the other from `to` on.
-__device__ __forceinline__ void load_lds16(const uint8_t* p, unsigned char* to) {
-  __builtin_amdgcn_global_load_lds(
-      (const __attribute__((address_space(1))) void*)p, (__attribute__((address_space(3))) void*)to,
-      16, 0, 2);  // 2: non-temporal
-}
-// All of the wave's loads have arrived; all of its LDS reads.
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
 // Eight E4M3 values as bf16, which every one of them is.
 __device__ __forceinline__ bf16x8 widen_e4m3(uint32_t a, uint32_t b) {
   auto two = [](uint32_t w, auto high) {
@@ -80,9 +70,6 @@ struct PagedWork {
 
 // The workgroup's rows, their places in memory (a row left out reads the first one)
 // and which of them there are, 32 to a word; false for a split behind the last row.
-// The first rows' entries of the table, and of the plan, are on their way before it
-// is known how long the request is: those of its prompt and of dense mode are
-// the ones, all others are read again.
 __device__ __forceinline__ bool paged_work(const PagedArgs& a, int lane, int wave, int waves,
                                            int64_t* place, uint32_t* mask, PagedWork& w) {
   const int pairs = a.B * a.Hkv, pair = blockIdx.x % pairs;
@@ -90,16 +77,13 @@ __device__ __forceinline__ bool paged_work(const PagedArgs& a, int lane, int wav
   w.b = pair / a.Hkv;
   w.h = pair % a.Hkv;
   w.first = w.s * a.C;
-  const bool planned = a.mode == DSA_MODE_DIAGONAL;
-  const int32_t* idx = planned ? a.idx + static_cast<size_t>(pair) * a.cap : nullptr;
-  const int32_t* table = a.table + static_cast<int64_t>(w.b) * a.M;
-  const int guess = w.first + wave * 64 + lane;
-  const int page0 = table[min(guess >> a.lg, a.M - 1)];
-  const int kept0 = planned ? idx[min(max(guess - a.Lp, 0), a.cap - 1)] : 0;
   w.r = paged_rows(a, w.b, pair);
   w.splits = (w.r.n + a.C - 1) / a.C;
   w.rows = min(w.r.n - w.first, a.C);
   if (w.s > 0 && w.rows <= 0) return false;
+  const bool planned = a.mode == DSA_MODE_DIAGONAL;
+  const int32_t* idx = planned ? a.idx + static_cast<size_t>(pair) * a.cap : nullptr;
+  const int32_t* table = a.table + static_cast<int64_t>(w.b) * a.M;
   for (int i0 = wave * 64; i0 < w.rows; i0 += waves * 64) {
     const int i = i0 + lane;
     int64_t at = 0;
@@ -107,14 +91,11 @@ __device__ __forceinline__ bool paged_work(const PagedArgs& a, int lane, int wav
     if (i < w.rows) {
       const int e = w.first + i, j = e - w.r.front;
       int row = e;
-      if (j >= 0 && planned) {
-        const int kept = i0 == wave * 64 && w.r.front == a.Lp ? kept0 : idx[j];
-        row = w.r.front + min(max(kept, 0), w.r.t);
-      } else if (j >= 0 && a.mode == DSA_MODE_WINDOW) {
+      if (j >= 0 && planned)
+        row = w.r.front + min(max(idx[j], 0), w.r.t);
+      else if (j >= 0 && a.mode == DSA_MODE_WINDOW)
         row = w.r.front + (j < a.Ns ? j : max(w.r.t - a.W + 1, a.Ns) + j - a.Ns);
-      }
-      const int entry = row >> a.lg;
-      const int page = entry >= a.M ? -1 : row == guess ? page0 : table[entry];
+      const int entry = row >> a.lg, page = entry < a.M ? table[entry] : -1;
       ok = static_cast<unsigned>(page) < static_cast<unsigned>(a.pool);
       if (ok) at = page * a.sp + (row & ((1 << a.lg) - 1)) * a.sr;
     }
@@ -141,7 +122,8 @@ __device__ __forceinline__ void paged_finish(const PagedArgs& a, const PagedWork
       O = fmaf(p[d], f, O);
     }
     if (w.splits > 1) {
-      float* to = a.part + (static_cast<size_t>(blockIdx.x) * G + g) * (D + 2);
+      float* to = a.part + ((static_cast<size_t>(w.s) * a.B * a.Hkv + w.b * a.Hkv + w.h) * G + g) *
+                             (D + 2);
       to[d] = O;
       if (d == 0) {
         to[D] = M;
@@ -202,7 +184,8 @@ __host__ __device__ constexpr uint32_t paged_vt_bytes() {
 }
 template <bool FP8, int D>
 __host__ __device__ constexpr uint32_t paged_lds(int C, int waves, int G) {
-  return C * 8u + ((C / 8 + 15) & ~15) + waves * (paged_vt_bytes<FP8, D>() + G * (D + 2) * 4u);
+  const uint32_t vt = paged_vt_bytes<FP8, D>(), red = G * (D + 2) * 4;
+  return C * 8u + ((C / 8 + 15) & ~15) + G * D * 2 + waves * (vt > red ? vt : red);
 }
 
 // A tile of a wave as loaded.
@@ -228,7 +211,7 @@ struct PagedTile {
 // weight is taken apart into TERMS bf16 ones: three hold all of its 24 bits, for
 // fp32 outputs; two are off by 2^-18 at most, a thousandth of a bf16 output's step.
 template <bool FP8, int D, int TERMS>
-__global__ __launch_bounds__(512) void paged_kernel(PagedArgs a) {
+__global__ __launch_bounds__(512, FP8 || D == 64 ? 4 : 2) void paged_kernel(PagedArgs a) {
   using T = PagedTile<FP8, D>;
   constexpr int EPL = T::EPL, KPL = T::KPL, LPR = T::LPR, RPI = T::RPI, NV = T::NV, NK = T::NK;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -238,25 +221,22 @@ __global__ __launch_bounds__(512) void paged_kernel(PagedArgs a) {
   const int pair = blockIdx.x % (a.B * a.Hkv), h = pair % a.Hkv, b = pair / a.Hkv, G = a.G;
   int64_t* place = reinterpret_cast<int64_t*>(lds);
   uint32_t* mask = reinterpret_cast<uint32_t*>(lds + a.C * 8);
-  unsigned char* vts = lds + a.C * 8 + ((a.C / 8 + 15) & ~15);
+  unsigned char* qs = lds + a.C * 8 + ((a.C / 8 + 15) & ~15);
+  unsigned char* vts = qs + G * D * 2;
   unsigned char* vt = vts + wave * paged_vt_bytes<FP8, D>();
-  float* red = reinterpret_cast<float*>(vts + waves * paged_vt_bytes<FP8, D>());
+  float* red = reinterpret_cast<float*>(vts);  // the waves' sums, after their last tiles
 
-  bf16x8 q[NK];
-#pragma unroll
-  for (int i = 0; i < NK; ++i) {
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (lr < G)
-      x = *reinterpret_cast<const uint4*>(a.q + (static_cast<size_t>(b) * a.Hq + h * G + lr) * D +
-                                          32 * KPL * (i / KPL) + EPL * lq + 8 * (i % KPL));
-    q[i] = __builtin_bit_cast(bf16x8, x);
-  }
+  // Queries of heads past the group are any; nothing of theirs comes out.
+  const uint16_t* qg = a.q + (static_cast<size_t>(b) * a.Hq + h * G) * D;
+  if (threadIdx.x < G * D / 8)
+    reinterpret_cast<uint4*>(qs)[threadIdx.x] = reinterpret_cast<const uint4*>(qg)[threadIdx.x];
   PagedWork work;
   if (!paged_work(a, lane, wave, waves, place, mask, work)) return;
   const float ks = FP8 && a.ks ? a.ks[h] : 1.f, vs = FP8 && a.vs ? a.vs[h] : 1.f;
   const float sl = a.scale * ks, sl2 = a.scale_log2 * ks;
   __syncthreads();
 
+  const unsigned char* qat = qs + ((lr & (G - 1)) * D + EPL * lq) * 2;
   const uint8_t* kb = a.k + h * a.sh + 16 * lq;
   const uint8_t* vb = a.v + h * a.sh + 16 * col;
   float m = kLowest, l = 0.f;  // of head lr, over the rows that this lane holds
@@ -278,16 +258,16 @@ __global__ __launch_bounds__(512) void paged_kernel(PagedArgs a) {
   };
 
   auto compute = [&](int t0, T& t) {
-    f32x4 sc[2];
+    f32x4 sc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      sc[hf] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < NK; ++i) {
+      const bf16x8 q = *reinterpret_cast<const bf16x8*>(qat + 64 * KPL * (i / KPL) + 16 * (i % KPL));
 #pragma unroll
-      for (int i = 0; i < NK; ++i)
-        sc[hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(to_bf16<FP8>(t.k[hf][i / KPL], i % KPL),
-                                                         q[i], sc[hf], 0, 0, 0);
+      for (int hf = 0; hf < 2; ++hf)
+        sc[hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(to_bf16<FP8>(t.k[hf][i / KPL], i % KPL), q,
+                                                         sc[hf], 0, 0, 0);
     }
-    const uint32_t there = __builtin_amdgcn_readfirstlane(t.there);
+    const uint32_t there = __builtin_amdgcn_readfirstlane(t.there), mine = there >> (4 * lq);
     if (a.wlog && lr < G) {
       float* to = a.wlog + (static_cast<size_t>(b) * a.Hq + h * G + lr) * a.cap;
 #pragma unroll
@@ -296,25 +276,30 @@ __global__ __launch_bounds__(512) void paged_kernel(PagedArgs a) {
         for (int j = 0; j < 4; ++j) {
           const int e = 16 * hf + 4 * lq + j, i = work.first + t0 + e;
           if (i >= work.r.front && i < work.first + work.rows)
-            to[i - work.r.front] = (there >> e) & 1 ? sc[hf][j] * sl : -__builtin_inff();
+            to[i - work.r.front] = (mine >> (16 * hf + j)) & 1 ? sc[hf][j] * sl : -__builtin_inff();
         }
     }
     float z[2][4], mx = kLowest;
-    if (there == 0xffffffffu) {
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
+    for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[hf][j] = sc[hf][j] * sl2;
-    } else {
+      for (int j = 0; j < 4; ++j) z[hf][j] = sc[hf][j] * sl2;
+    if (there != 0xffffffffu) {
       // What is left out is 0 in the product with V, whatever the memory holds.
+      const uint32_t rows = there >> rg;
 #pragma unroll
-      for (int u = 0; u < NV; ++u)
-        if (!((there >> (u * RPI + rg)) & 1)) t.v[u] = make_uint4(0, 0, 0, 0);
+      for (int u = 0; u < NV; ++u) {
+        const uint32_t keep = 0u - ((rows >> (u * RPI)) & 1);
+        t.v[u].x &= keep;
+        t.v[u].y &= keep;
+        t.v[u].z &= keep;
+        t.v[u].w &= keep;
+      }
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          z[hf][j] = (there >> (16 * hf + 4 * lq + j)) & 1 ? sc[hf][j] * sl2 : -__builtin_inff();
+          if (!((mine >> (16 * hf + j)) & 1)) z[hf][j] = -__builtin_inff();
     }
     // V rows in the order of the weights: those of lanes 16 * g .. are eight in turn.
 #pragma unroll
@@ -409,6 +394,7 @@ __global__ __launch_bounds__(512) void paged_kernel(PagedArgs a) {
     xor_pair<32>(l, x1, x2);
     l = x1 + x2;
   }
+  __syncthreads();  // the tiles are done with
   float* mine = red + wave * G * (D + 2);
 #pragma unroll
   for (int c = 0; c < D / 16; ++c)
