@@ -19,9 +19,11 @@ __device__ __forceinline__ uint64_t beam_key(float x, int place) {
              ? (static_cast<uint64_t>(ordered_bits(x)) << 32) | static_cast<uint32_t>(~place)
              : 0;
 }
-__device__ __forceinline__ float key_value(uint64_t k) {
-  const uint32_t u = static_cast<uint32_t>(k >> 32);
+__device__ __forceinline__ float from_ordered(uint32_t u) {
   return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ float key_value(uint64_t k) {
+  return from_ordered(static_cast<uint32_t>(k >> 32));
 }
 __device__ __forceinline__ int key_place(uint64_t k) { return ~static_cast<int>(k); }
 
@@ -71,7 +73,7 @@ __device__ __forceinline__ int key_rank(uint64_t key, const uint64_t* list, int 
 // exponentials (fours in fp32, the rest in fp64), and their W largest in order.
 //
 // The W largest are not below the W-th largest of the maxima of the workgroup's 32
-// groups of eight lanes, and few values are (about 10 of 8192 for eight beams, 22 for
+// groups of eight lanes (here cut to 27 bits, with the group's number below), and few values are (about 10 of 8192 for eight beams, 22 for
 // sixteen): those go into a list, where each is placed by the larger ones' number.
 // With more than 64 of them (equal values) every wave takes its largest out one at a
 // time.
@@ -79,9 +81,10 @@ template <bool BF16, int R>
 __global__ __launch_bounds__(kBeamThreads) void beam_row_kernel(BeamArgs a) {
   constexpr int VL = BF16 ? 8 : 4, NV = R / VL;  // values of a load, loads
   constexpr int kGroups = kBeamThreads / 8;
-  static_assert(kGroups >= DSA_MAX_BEAMS && kGroups <= 64 && kBeamWaves * DSA_MAX_BEAMS <= 64,
+  static_assert(kGroups >= DSA_MAX_BEAMS && kGroups == 32 && kBeamWaves * DSA_MAX_BEAMS <= 64,
                 "a lane each");
-  __shared__ __attribute__((aligned(16))) float top_s[kGroups];
+  __shared__ float top_s[kGroups];
+  __shared__ __attribute__((aligned(16))) uint32_t order_s[kGroups];
   __shared__ double sum_s[kBeamWaves];
   __shared__ __attribute__((aligned(16))) uint64_t list_s[64];
   __shared__ int n_s;
@@ -91,95 +94,110 @@ __global__ __launch_bounds__(kBeamThreads) void beam_row_kernel(BeamArgs a) {
   // lies, so equal rows tie.
   const uint8_t* start = static_cast<const uint8_t*>(a.x) + row * a.stride * (16 / VL);
   const int first = chunk * a.per, end = min(first + a.per, (a.V + VL - 1) / VL);
-  float x[R];
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
+  auto load = [&](int k) {
     const int piece = first + k * kBeamThreads + threadIdx.x, v = piece * VL;
-    const bool whole = piece < end && v + VL <= a.V;
-    u32x4 w = {0, 0, 0, 0};
-    if (whole)
-      w = __builtin_nontemporal_load(
-          reinterpret_cast<const Piece*>(start + static_cast<int64_t>(v) * (16 / VL)));
-    if constexpr (BF16) {
-      float f[8];
-      unpack8(make_uint4(w.x, w.y, w.z, w.w), f);
+    if (piece < end && v + VL <= a.V)
+      return static_cast<u32x4>(__builtin_nontemporal_load(
+          reinterpret_cast<const Piece*>(start + static_cast<int64_t>(v) * (16 / VL))));
+    u32x4 w;  // the row's end, value by value, and what lies behind
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[8 * k + i] = f[i];
-    } else {
-      x[4 * k] = __uint_as_float(w.x);
-      x[4 * k + 1] = __uint_as_float(w.y);
-      x[4 * k + 2] = __uint_as_float(w.z);
-      x[4 * k + 3] = __uint_as_float(w.w);
-    }
-    if (!whole) {  // the row's end, value by value, and what lies behind
-#pragma unroll
-      for (int i = 0; i < VL; ++i) {
-        x[VL * k + i] = -__builtin_inff();
-        if (piece < end && v + i < a.V) {
-          if constexpr (BF16)
-            x[VL * k + i] = bf16_lo(reinterpret_cast<const uint16_t*>(start)[v + i]);
-          else
-            x[VL * k + i] = reinterpret_cast<const float*>(start)[v + i];
-        }
+    for (int i = 0; i < VL; ++i) {
+      const bool there = piece < end && v + i < a.V;
+      if constexpr (BF16) {
+        const uint32_t u = there ? reinterpret_cast<const uint16_t*>(start)[v + i] : 0xff80u;
+        w[i / 2] = i & 1 ? w[i / 2] | u << 16 : u;
+      } else {
+        w[i] = there ? reinterpret_cast<const uint32_t*>(start)[v + i] : 0xff800000u;
       }
     }
-  }
-  auto place = [&](int i) {
-    return (first + i / VL * kBeamThreads + static_cast<int>(threadIdx.x)) * VL + i % VL;
+    return w;
+  };
+  auto value = [&](const u32x4& w, int i) {
+    if constexpr (BF16)
+      return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    else
+      return __uint_as_float(w[i]);
+  };
+  u32x4 w[NV];  // as they lie: half the registers for bf16, so more waves
+#pragma unroll
+  for (int k = 0; k < NV; ++k) w[k] = load(k);
+  auto place = [&](int k, int i) {
+    return (first + k * kBeamThreads + static_cast<int>(threadIdx.x)) * VL + i;
   };
 
-  float mine = -__builtin_inff();
+  float most[NV], mine = -__builtin_inff();
 #pragma unroll
-  for (int i = 0; i < R; ++i) mine = fmaxf(mine, x[i]);
+  for (int k = 0; k < NV; ++k) {
+    most[k] = value(w[k], 0);
+#pragma unroll
+    for (int i = 1; i < VL; ++i) most[k] = fmaxf(most[k], value(w[k], i));
+    mine = fmaxf(mine, most[k]);
+  }
   mine = fmaxf(mine, dpp<kDppQuadSwap1>(mine));
   mine = fmaxf(mine, dpp<kDppQuadSwap2>(mine));
   mine = fmaxf(mine, dpp<kDppHalfMirror>(mine));
-  if ((lane & 7) == 0) top_s[threadIdx.x >> 3] = mine;
+  if ((lane & 7) == 0) {
+    const int group = threadIdx.x >> 3;
+    top_s[group] = mine;
+    order_s[group] = (ordered_bits(mine) & ~(kGroups - 1u)) | group;
+  }
   if (threadIdx.x < 64) list_s[threadIdx.x] = 0;
   if (threadIdx.x == 0) n_s = 0;
   __syncthreads();
-  const float group = lane < kGroups ? top_s[lane] : -__builtin_inff();
-  const float top = wave_max(group);
-  int larger = 0;
+  const float top = wave_max(top_s[lane % kGroups]);
+  const uint32_t group = order_s[lane % kGroups];
+  int larger = 0;  // of the groups of half the lanes
+  const uint32_t* others = order_s + lane / kGroups * (kGroups / 2);
 #pragma unroll
-  for (int j = 0; j < kGroups; ++j) {
-    const float y = top_s[j];
-    larger += y > group || (y == group && j < lane);
-  }
-  const uint64_t at_w = __ballot(lane < kGroups && larger == a.W - 1);  // one lane
-  const float least = fmaxf(__shfl(group, __builtin_ctzll(at_w), 64), -3.402823466e38f);
+  for (int j = 0; j < kGroups / 2; ++j) larger += others[j] > group;
+  larger += __shfl_xor(larger, kGroups, 64);
+  const int at_w = __builtin_ctzll(__ballot(larger == a.W - 1));
+  const float least = fmaxf(from_ordered(__shfl(group, at_w, 64) & ~(kGroups - 1u)), -3.402823466e38f);
 
   // A chunk of -infinities adds nothing; a NaN or +infinity makes the sum a NaN.
   double sum = 0.;
   const float base = top > -__builtin_inff() ? top : 0.f;
 #pragma unroll
-  for (int i = 0; i < R; i += 4) {
-    float e[4];
+  for (int k = 0; k < NV; ++k) {
+    asm volatile("" : "+v"(w[k]));  // the values are widened once more, not kept
 #pragma unroll
-    for (int k = 0; k < 4; ++k) e[k] = fast_exp2((x[i + k] - base) * 1.4426950408889634f);
-    sum += static_cast<double>((e[0] + e[1]) + (e[2] + e[3]));
+    for (int i = 0; i < VL; i += 4) {
+      float e[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        e[j] = fast_exp2((value(w[k], i + j) - base) * 1.4426950408889634f);
+      sum += static_cast<double>((e[0] + e[1]) + (e[2] + e[3]));
+    }
   }
   sum = wave_sum_f64(sum);
   if (lane == 0) sum_s[wave] = sum;
 
 #pragma unroll
-  for (int i = 0; i < R; ++i)
-    if (x[i] >= least) {
-      const int at = atomicAdd(&n_s, 1);
-      if (at < 64) list_s[at] = beam_key(x[i], place(i));
+  for (int k = 0; k < NV; ++k)
+    if (most[k] >= least) {
+#pragma unroll
+      for (int i = 0; i < VL; ++i)
+        if (value(w[k], i) >= least) {
+          const int at = atomicAdd(&n_s, 1);
+          if (at < 64) list_s[at] = beam_key(value(w[k], i), place(k, i));
+        }
     }
   __syncthreads();
   int n = n_s;
   if (n > 64) {
     uint64_t best = 0, under = ~uint64_t{0};  // lane i: the wave's i-th
     for (int k = 0; k < a.W; ++k) {
-      uint64_t most = 0;
+      uint64_t next = 0;
+#pragma unroll 1
+      for (int q = 0; q < NV; ++q) {  // read again: rare, and no registers held for it
+        const u32x4 x = load(q);
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        const uint64_t key = beam_key(x[i], place(i));
-        most = key < under && key > most ? key : most;
+        for (int i = 0; i < VL; ++i) {
+          const uint64_t key = beam_key(value(x, i), place(q, i));
+          next = key < under && key > next ? key : next;
+        }
       }
-      under = wave_max_u64(most);
+      under = wave_max_u64(next);
       if (lane == k) best = under;
     }
     __syncthreads();  // all have read n_s, and the list ends
