@@ -766,9 +766,9 @@ DSA_API size_t dsa_paged_workspace_bytes(const dsa_params* p, const dsa_shape* s
  * Free pages are taken in the order of the pool from *d_cursor on and around, by
  * requests in order, a request's entries in order; *d_cursor becomes the page
  * after the last one taken.  Pages given back in this call can be taken in it;
- * shared ones that their last user left here cannot.  A request gets its pages where the needs of the
- * requests up to it add up to no more than there are free, or it needs none; else
- * it gets nothing, as with len + new_b > M * P.
+ * shared ones that their last user left here cannot.  A request gets its pages
+ * where the needs of the requests up to it add up to no more than there are free,
+ * or it needs none; else it gets nothing, as with len + new_b > M * P.
  *   p         prompt_len, mode, window, n_att and sinks are read; valid as for
  *             every call
  *   batch     B in [1, DSA_MAX_PAGED_BATCH]
@@ -883,7 +883,8 @@ DSA_API dsa_status dsa_paged_attention(const dsa_params* p, const dsa_shape* s,
  *   d_token        int32 [B][W], out
  *   d_ws, ws_bytes dsa_beam_workspace_bytes() bytes, 16-byte aligned; need not be
  *                  cleared
- * Sums of exponentials are kept in fp64, and scores compared in fp64.
+ * Exponentials are summed in fp64 (four at a time in fp32), and scores compared in
+ * fp64.  Equal rows have equal sums, wherever they lie.
  * Errors: INVALID_ARG, WORKSPACE, HIP.
  */
 #define DSA_MAX_BEAMS 16

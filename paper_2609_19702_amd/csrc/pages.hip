@@ -216,8 +216,8 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
       a.flags[b] = r.len < 0 ? 0
                              : (s.fits ? (pages ? 0 : DSA_PAGE_FLAG_NO_PAGES)
                                        : DSA_PAGE_FLAG_TOO_LONG);
-      const int pos = r.len + r.fresh - 1 - r.prompt;  // of rows that fit
-      a.pos[b] = ok && pos >= 0 ? pos : -1;
+      const int64_t pos = static_cast<int64_t>(r.len) + r.fresh - 1 - r.prompt;
+      a.pos[b] = ok && pos >= 0 ? static_cast<int>(pos) : -1;
       int32_t* told = a.copies + 3 * static_cast<int64_t>(b);
       told[0] = x;
       told[1] = y;
