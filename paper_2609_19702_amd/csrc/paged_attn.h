@@ -45,6 +45,10 @@ __device__ __forceinline__ bf16x8 to_bf16(const uint4& r, int half) {
     return __builtin_bit_cast(bf16x8, r);
 }
 
+// A quotient of uniform values is one too, which the compiler does not see: its vector
+// registers are then kept for all that follows from it.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // Rows of a request that its step attends: its prompt, then decode rows.
 struct PagedRows {
   int n, t, front;  // rows, decode position, prompt rows
@@ -72,10 +76,11 @@ struct PagedWork {
 // and which of them there are, 32 to a word; false for a split behind the last row.
 __device__ __forceinline__ bool paged_work(const PagedArgs& a, int lane, int wave, int waves,
                                            int64_t* place, uint32_t* mask, PagedWork& w) {
-  const int pairs = a.B * a.Hkv, pair = blockIdx.x % pairs;
-  w.s = blockIdx.x / pairs;
-  w.b = pair / a.Hkv;
-  w.h = pair % a.Hkv;
+  const int pairs = a.B * a.Hkv;
+  w.s = uniform(blockIdx.x / pairs);
+  const int pair = blockIdx.x - w.s * pairs;
+  w.b = uniform(pair / a.Hkv);
+  w.h = pair - w.b * a.Hkv;
   w.first = w.s * a.C;
   w.r = paged_rows(a, w.b, pair);
   w.splits = (w.r.n + a.C - 1) / a.C;
@@ -176,11 +181,12 @@ __device__ __forceinline__ void widen(const uint4& r, float (&f)[FP8 ? 16 : 8]) 
   }
 }
 
-// Dynamic LDS: places of the split's rows, which of them there are, a V tile per
-// wave, the waves' results.
+// Dynamic LDS: places of the split's rows, which of them there are, the queries, a V tile
+// per wave (its last row without the pad: that leaves room for two workgroups of 768 rows
+// and eight heads on a CU) and over the tiles the waves' results.
 template <bool FP8, int D>
 __host__ __device__ constexpr uint32_t paged_vt_bytes() {
-  return kTile * (FP8 ? D + 16 : 2 * (D + kPad));
+  return (kTile - 1) * (FP8 ? D + 16 : 2 * (D + kPad)) + (FP8 ? D : 2 * D);
 }
 template <bool FP8, int D>
 __host__ __device__ constexpr uint32_t paged_lds(int C, int waves, int G) {
@@ -211,14 +217,15 @@ struct PagedTile {
 // weight is taken apart into TERMS bf16 ones: three hold all of its 24 bits, for
 // fp32 outputs; two are off by 2^-18 at most, a thousandth of a bf16 output's step.
 template <bool FP8, int D, int TERMS>
-__global__ __launch_bounds__(512, FP8 || D == 64 ? 4 : 2) void paged_kernel(PagedArgs a) {
+__global__ __launch_bounds__(512, 4) void paged_kernel(PagedArgs a) {
   using T = PagedTile<FP8, D>;
   constexpr int EPL = T::EPL, KPL = T::KPL, LPR = T::LPR, RPI = T::RPI, NV = T::NV, NK = T::NK;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int lr = lane & 15, lq = lane >> 4, rg = lane / LPR, col = lane % LPR;
-  const int pair = blockIdx.x % (a.B * a.Hkv), h = pair % a.Hkv, b = pair / a.Hkv, G = a.G;
+  const int pair = uniform(blockIdx.x % (a.B * a.Hkv)), b = uniform(pair / a.Hkv);
+  const int h = pair - b * a.Hkv, G = a.G;
   int64_t* place = reinterpret_cast<int64_t*>(lds);
   uint32_t* mask = reinterpret_cast<uint32_t*>(lds + a.C * 8);
   unsigned char* qs = lds + a.C * 8 + ((a.C / 8 + 15) & ~15);
@@ -425,7 +432,7 @@ __global__ __launch_bounds__(512, 4) void paged_row_kernel(PagedArgs a) {
   uint32_t* mask = reinterpret_cast<uint32_t*>(lds + a.C * 8);
   float* red = reinterpret_cast<float*>(lds + a.C * 8 + ((a.C / 8 + 15) & ~15));
 
-  const int pair = blockIdx.x % (a.B * a.Hkv), h = pair % a.Hkv;
+  const int pair = uniform(blockIdx.x % (a.B * a.Hkv)), h = uniform(pair % a.Hkv);
   uint4 qr[EPL / 8];
 #pragma unroll
   for (int i = 0; i < EPL / 8; ++i)

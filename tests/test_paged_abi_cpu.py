@@ -137,7 +137,7 @@ def test_launches_cover_all_rows(mode, shape):
             continue
         rows = prompt + (grid[0] * grid[1] if mode == B.MODE_DENSE else min(13, grid[0] * grid[1]))
         i = B.paged_launch_info(p, s)
-        assert i.rows_per_split % 64 == 0 and i.rows_per_split <= 4096 and i.waves_per_group == 8
+        assert i.rows_per_split % 64 == 0 and i.rows_per_split <= 896 and i.waves_per_group == 8
         assert i.max_splits * i.rows_per_split >= rows > (i.max_splits - 1) * i.rows_per_split
         assert i.workgroups == shape[0] * shape[2] * i.max_splits
         assert (i.workspace_bytes > 0) == (i.max_splits > 1)
