@@ -122,6 +122,11 @@ class PageLayout(C.Structure):
                 ("stride_head", C.c_int64), ("stride_row", C.c_int64), ("d_k_scale", C.c_void_p),
                 ("d_v_scale", C.c_void_p), ("dtype", C.c_int32)]
 
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        if name != "_fits":  # what was looked at before is looked at again
+            super().__setattr__("_fits", None)
+
 
 class PagedLaunchInfo(C.Structure):
     _fields_ = [("rows_per_split", C.c_int32), ("max_splits", C.c_int32),
@@ -801,7 +806,6 @@ def page_layout(k: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                      KV_BF16 if k.dtype == torch.bfloat16 else KV_FP8_E4M3)
     out._held = (k_scale, v_scale)
     out.scales = min([x.numel() for x in out._held if x is not None], default=1 << 62)
-    out._fits = None  # the caches' values that _check_paged last let through
     return out
 
 
@@ -869,6 +873,7 @@ def page_reorder(pages: Pages, parent, stream=None):
 def _check_paged(s, k, v, layout, layers, device):
     """The caches against their layout, their scales and the shape."""
     shape, st, dtype = k.shape, k.stride(), k.dtype
+    # layout._fits: the caches' values that were last let through
     if (dtype is v.dtype and shape == v.shape and st == v.stride() and k.get_device() == device
             and v.get_device() == device
             and layout._fits == (dtype, shape, st, layers, s.num_kv_heads, s.head_dim, device)):

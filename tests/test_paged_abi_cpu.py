@@ -185,3 +185,20 @@ def test_binding_refuses():
         B.beam_select(x[0], *[None] * 5)
     with pytest.raises(ValueError, match="fp32 or bf16"):
         B.beam_select(x.half(), *[None] * 5)
+
+
+def test_a_changed_layout_is_looked_at_again():
+    s, k = B.make_shape(2, 8, 8, 64), torch.zeros(40, 8, 16, 64, dtype=torch.bfloat16)
+    at = B.page_layout(k)
+    for _ in range(2):
+        B._check_paged(s, k, k, at, None, k.get_device())
+    at.num_pages = 41
+    with pytest.raises(ValueError, match="does not hold 41 pages"):
+        B._check_paged(s, k, k, at, None, k.get_device())
+    at.num_pages, at.stride_row = 40, 128
+    with pytest.raises(ValueError, match="does not hold"):
+        B._check_paged(s, k, k, at, None, k.get_device())
+    at.stride_row = 64
+    B._check_paged(s, k, k, at, None, k.get_device())
+    with pytest.raises(ValueError, match="does not hold"):
+        B._check_paged(s, k[:39], k[:39], at, None, k.get_device())
