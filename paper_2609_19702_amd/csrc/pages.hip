@@ -40,7 +40,7 @@ __device__ __forceinline__ bool in_pool(int page, int pool) {
   return static_cast<unsigned>(page) < static_cast<unsigned>(pool);
 }
 
-// One workgroup, 16 lanes to a request.  Its parts, with a barrier after each:
+// One workgroup, LANES lanes to a request.  Its parts, with a barrier after each:
 //   1. lengths, new and prompt rows into LDS
 //   2. pages that ended or fell behind go back
 //   3. the pages that the new rows need are counted; an entry whose page is shared
@@ -49,14 +49,20 @@ __device__ __forceinline__ bool in_pool(int page, int pool) {
 //   5. free pages from the cursor on, 4096 looked at a time; the k-th goes to
 //      the request whose share of the sums k lies in, and waits in its slots
 //      (a request has a new row for every page that it needs)
-//   6. they go into the table, and slots come out
-// Bound by the way to memory and back, some 0.7 us for each part but 4: 5 us for one
-// request.
+//   6. they go into the table, and slots come out; more than a group's lanes of them
+//      in a part of their own, a wave to a request
+// Bound by the way to memory and back, some 0.5 us for each part but 4: 3.2 us for one
+// request; then by the rounds of groups: a new row each for 64, 128, 256, 1024 and 4096
+// requests takes 6.0, 6.2, 6.5, 13 and 39 us (with 16 lanes to each 6.0, 7.9, 12, 35 and
+// 127), so fewer lanes where there are many.
+template <int LANES>
 __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateArgs a) {
+  constexpr uint32_t kAll = (1u << LANES) - 1;  // a group's lanes in its ballot
   extern __shared__ PageReq req[];
   __shared__ int part[kLook][kUpdateWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int sub = tid & 15, group = tid >> 4, shift = lane & 48;  // shift: of a group's ballot
+  const int sub = tid % LANES, group = tid / LANES;
+  const int shift = lane - sub;  // of the group's ballot
   const int rows = 1 << a.lg;
 
   for (int b = tid; b < a.B; b += kUpdateThreads) {
@@ -71,7 +77,7 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
   }
   __syncthreads();
 
-  for (int b = group; b < a.B; b += kUpdateThreads / 16) {
+  for (int b = group; b < a.B; b += kUpdateThreads / LANES) {
     const PageReq r = req[b];
     int32_t* row = a.table + static_cast<int64_t>(b) * a.M;
     int lo = 0, hi = r.len < 0 ? a.M : 0;
@@ -81,7 +87,7 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
       lo = static_cast<int>(min((front + rows - 1) >> a.lg, static_cast<int64_t>(a.M)));
       hi = back > 0 ? static_cast<int>(min(back >> a.lg, static_cast<int64_t>(a.M))) : 0;
     }
-    for (int i = lo + sub; i < hi; i += 16) {
+    for (int i = lo + sub; i < hi; i += LANES) {
       const int page = row[i];
       if (in_pool(page, a.pool)) atomicSub(a.refs + page, 1);
       if (page != -1) row[i] = -1;
@@ -92,11 +98,11 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
 
-  for (int b = group; b < a.B; b += kUpdateThreads / 16) {
+  for (int b = group; b < a.B; b += kUpdateThreads / LANES) {
     const PageSpan s = page_span(a, req[b]);
     int32_t* row = a.table + static_cast<int64_t>(b) * a.M;
     int need = 0;
-    for (int i = s.e0 + sub; i - sub < s.e1; i += 16) {
+    for (int i = s.e0 + sub; i - sub < s.e1; i += LANES) {
       int want = 0;  // what the entry becomes, if anything
       if (i < s.e1) {
         const int page = row[i];
@@ -106,7 +112,7 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
           want = -2 - page;
         if (want && want != page) row[i] = want;
       }
-      need += __popc(static_cast<uint32_t>(__ballot(want != 0) >> shift) & 0xffffu);
+      need += __popc(static_cast<uint32_t>(__ballot(want != 0) >> shift) & kAll);
     }
     if (sub == 0) req[b].upto = need;
   }
@@ -169,7 +175,7 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
   }
   found = min(found, total);
 
-  for (int b = group; b < a.B; b += kUpdateThreads / 16) {
+  for (int b = group; b < a.B; b += kUpdateThreads / LANES) {
     const PageReq r = req[b];
     const PageSpan s = page_span(a, r);
     const int need = r.upto - (b ? req[b - 1].upto : 0);
@@ -179,9 +185,9 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
     int x = -1, y = -1;  // the first entry's old and new page, where rows are copied
     int last = 0;        // the last page that the request is given
     int got = -1;        // page of entry e0 + sub
-    for (int i = s.e0 + sub, rank = 0; i - sub < s.e1; i += 16) {
+    for (int i = s.e0 + sub, rank = 0; i - sub < s.e1; i += LANES) {
       int now = i < s.e1 ? row[i] : 0;
-      const uint32_t mask = static_cast<uint32_t>(__ballot(now < 0) >> shift) & 0xffffu;
+      const uint32_t mask = static_cast<uint32_t>(__ballot(now < 0) >> shift) & kAll;
       if (now < 0) {
         const int old = -2 - now;  // the shared page, or -1
         now = old;
@@ -224,15 +230,27 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
       told[2] = x >= 0 ? r.len & (rows - 1) : -1;
     }
     // What waited in the slots has been read: they become the rows' places.
-    fence_wave();
     const int n = ok ? r.fresh : 0;
-    const bool few = s.e1 - s.e0 <= 16;
-    for (int i = sub; i - sub < n; i += 16) {
-      const int at = r.len + min(i, n - 1), e = at >> a.lg;
-      const int held = __shfl(got, shift + ((e - s.e0) & 15), 64);
-      if (i < n) slots[i] = ((few ? held : row[e]) << a.lg) + (at & (rows - 1));
+    if (a.N > LANES) {
+      if (sub == 0) req[b].fresh = n;
+      continue;
     }
-    for (int i = n + sub; i < a.N; i += 16) slots[i] = -1;
+    fence_wave();
+    const int at = (n ? r.len : 0) + sub, e = at >> a.lg;
+    const int held = __shfl(got, shift + ((e - s.e0) & (LANES - 1)), 64);
+    if (sub < a.N) slots[sub] = sub < n ? (held << a.lg) + (at & (rows - 1)) : -1;
+  }
+  if (a.N <= LANES) return;
+  __syncthreads();
+  for (int b = wave; b < a.B; b += kUpdateWaves) {
+    const int len = req[b].len, n = req[b].fresh;
+    const int32_t* row = a.table + static_cast<int64_t>(b) * a.M;
+    int32_t* slots = a.slots + static_cast<int64_t>(b) * a.N;
+    for (int i = lane; i < a.N; i += 64) {
+      int slot = -1;
+      if (i < n) slot = (row[(len + i) >> a.lg] << a.lg) + ((len + i) & (rows - 1));
+      slots[i] = slot;
+    }
   }
 }
 
@@ -356,7 +374,14 @@ void append_grid(const PagedAppendArgs& a, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_page_update(const PageUpdateArgs& a, hipStream_t st) {
-  page_update_kernel<<<dim3(1), dim3(kUpdateThreads), a.B * sizeof(PageReq), st>>>(a);
+  const dim3 one(1), block(kUpdateThreads);
+  const size_t lds = a.B * sizeof(PageReq);
+  if (a.B <= kUpdateThreads / 16)
+    page_update_kernel<16><<<one, block, lds, st>>>(a);
+  else if (a.B <= kUpdateThreads / 8)
+    page_update_kernel<8><<<one, block, lds, st>>>(a);
+  else
+    page_update_kernel<4><<<one, block, lds, st>>>(a);
   return hipGetLastError();
 }
 

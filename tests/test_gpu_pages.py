@@ -208,6 +208,27 @@ def test_many_requests(batch):
     assert users(t) == t.refs
 
 
+@pytest.mark.parametrize("page", [1, 2, 16])
+@pytest.mark.parametrize("most", [1, 3, 4, 5, 8, 9, 16, 17, 65])
+@pytest.mark.parametrize("batch", [64, 65, 128, 129, 300])
+def test_few_and_many_slots(batch, most, page):
+    """Every number of lanes to a request, with as many slots as lanes and one more."""
+    rng = random.Random(batch * most + page)
+    width = 120 // page + 1
+    t = Tables(batch, page, width, pool=batch * width * 3 // 4, most=most, prompt=9, cursor=3)
+    length = [rng.randrange(-1, 30) for _ in range(batch)]
+    for i in range(4):
+        new = [rng.choice([0, 1, most, most, rng.randrange(most + 1)]) for _ in range(batch)]
+        flags = t.step(length, new)[3]
+        assert users(t) == t.refs
+        length = [-1 if flags[b] or rng.random() < 0.1 else max(n, 0) + (new[b] if n >= 0 else 0)
+                  for b, n in enumerate(length)]
+        if i == 1:
+            parent = [rng.randrange(batch) if rng.random() < 0.2 else b for b in range(batch)]
+            t.reorder(parent)
+            length = [length[b] for b in parent]
+
+
 def test_a_long_row_and_a_large_pool():
     t = Tables(3, 16, 2000, pool=50000, most=20000, prompt=0, cursor=49000)
     t.refs[5:40000] = [1] * 39995  # others' pages
