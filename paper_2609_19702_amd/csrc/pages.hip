@@ -258,7 +258,8 @@ constexpr int kReorderThreads = 512;
 constexpr int kReorderMost = 2048;  // entries that a workgroup holds, about
 
 // A workgroup takes some columns of the table: all their entries into LDS, then
-// every row its parent's.  Bound by the way to memory and back.
+// every row its parent's.  Bound by the way to memory and back: 2.2 us for four rows of 53
+// entries, 4.5 for 256.
 __global__ __launch_bounds__(kReorderThreads) void page_reorder_kernel(PageReorderArgs a,
                                                                       int lg_cols) {
   extern __shared__ int32_t held[];  // [B][cols]
@@ -322,7 +323,11 @@ __device__ __forceinline__ uint4 fp8_codes(const uint4& a, const uint4& b, float
 }
 
 // 16 bytes of a K row and of its V row in the cache per thread.  The first `blocks`
-// workgroups of a (layer, request) take new rows, the others rows of its copy.
+// workgroups of a (layer, request) take new rows, the others rows of its copy.  Bound by
+// memory: 32 prompts of 256 rows at most in 8 layers of 8 heads, d = 128, bf16 to fp8,
+// 66.5 us or 4.6 TB/s of a copy's 5.0; a row and half a page copied for 32 requests in 30
+// layers of 32 heads, 42 us or 4.1 TB/s.  Two or four rows a thread, or a workgroup's
+// copies row by row, were within 2%.
 template <bool FP8, int D>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a, int blocks,
                                                            int copy_blocks) {
