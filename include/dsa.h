@@ -848,7 +848,7 @@ DSA_API dsa_status dsa_paged_append(const dsa_shape* s, int32_t most_new, const 
  *   d_q              bf16 [B][Hq][d]
  *   d_decode_pos     int32 [B], as for dsa_plan (t < 0: an unused slot, zeros out)
  *   d_plan           plan of the same step in diagonal mode (else not read)
- *   sm_scale         any finite value
+ *   sm_scale         within +-2^126
  *   d_out            [B][Hq][d] in out_type (DSA_OUT_FP32, DSA_OUT_BF16)
  *   d_window_logits  NULL, or fp32 [B][Hq][cap] in diagonal mode, as for
  *                    dsa_decode_attention; a row without a page has -infinity

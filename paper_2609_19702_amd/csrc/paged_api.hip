@@ -234,7 +234,7 @@ DSA_API dsa_status dsa_paged_attention(const dsa_params* p, const dsa_shape* s,
   if (layout->page_rows != pages->page_rows) return DSA_ERR_INVALID_ARG;
   if (!d_q || !d_k || !d_v || !d_decode_pos || !d_out) return DSA_ERR_INVALID_ARG;
   if (out_type != DSA_OUT_FP32 && out_type != DSA_OUT_BF16) return DSA_ERR_INVALID_ARG;
-  if (!std::isfinite(sm_scale)) return DSA_ERR_INVALID_ARG;
+  if (!(std::fabs(sm_scale) <= 0x1p126f)) return DSA_ERR_INVALID_ARG;  // times log2(e), too
   const bool diagonal = d.mode == DSA_MODE_DIAGONAL;
   if (diagonal ? !d_plan : d_window_logits != nullptr) return DSA_ERR_INVALID_ARG;
   for (const void* x : {d_q, d_k, d_v, static_cast<const void*>(d_out)})

@@ -114,6 +114,11 @@ def test_attention_refuses(bad):
     assert attend(**bad) == B.ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("scale", [2.0 ** 126 * 1.0001, -2.0 ** 127, 3e38])
+def test_attention_refuses_scales_whose_scores_would_overflow(scale):
+    assert attend(scale=scale) == B.ERR_INVALID_ARG
+
+
 def test_attention_asks_for_its_workspace():
     p, s = B.make_params(32, 64, 64, 64, 13, B.MODE_DENSE), B.make_shape(1, 8, 8, 128)
     g = pages(max_pages=300)
