@@ -49,7 +49,7 @@ dsa_status paged_derive(const dsa_params* p, const dsa_shape* s, Derived* d, Pag
   const dsa_status st = derive(p, s, d);
   if (st != DSA_OK) return st;
   *l = paged_launch(*d);
-  return l->workgroups > kInt ? DSA_ERR_INVALID_ARG : DSA_OK;
+  return l->workgroups > kInt || int64_t{d->B} * d->Hq > kInt - 4 ? DSA_ERR_INVALID_ARG : DSA_OK;
 }
 
 }  // namespace

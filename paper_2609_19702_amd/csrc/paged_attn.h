@@ -545,32 +545,36 @@ __global__ __launch_bounds__(512, 4) void paged_row_kernel(PagedArgs a) {
 // turns, four splits at a time.  Two dependent ways to memory: 4.0 us for three splits of
 // 768 heads, 4.5 for six of 1024.
 template <int D>
-__global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a, int each) {
+__global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a, int each, int most) {
   constexpr int N = D / 64;
   __shared__ float red[4][D + 2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t at = each > 1 ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * 4 + wave;
-  if (at >= static_cast<int64_t>(a.B) * a.Hq) return;
-  const int b = static_cast<int>(at / a.Hq), hq = static_cast<int>(at % a.Hq);
-  const int h = hq / a.G, g = hq % a.G;
-  const int pair = b * a.Hkv + h, splits = (paged_rows(a, b, pair).n + a.C - 1) / a.C;
-  if (splits < 2) return;
+  const int at = uniform(each > 1 ? blockIdx.x : blockIdx.x * 4 + wave);
+  if (at >= a.B * a.Hq) return;
+  const int b = uniform(at / a.Hq), hq = at - b * a.Hq, h = uniform(hq / a.G), g = hq - h * a.G;
+  const int pair = b * a.Hkv + h;
   const int64_t step = static_cast<int64_t>(a.B) * a.Hkv * a.G * (D + 2);
   const float* p = a.part + (static_cast<size_t>(pair) * a.G + g) * (D + 2);
-  float M = kLowest, L = 0.f, O[N] = {};
-  for (int x0 = each > 1 ? 4 * wave : 0; x0 < splits; x0 += 4 * each) {
-    float mx[4], lx[4], ox[4][N];
+  float mx[4], lx[4], ox[4][N];
+  auto load = [&](int x0) {
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      const float* px = p + min(x0 + x, splits - 1) * step;
+      const float* px = p + min(x0 + x, most - 1) * step;
       mx[x] = px[D];
       lx[x] = px[D + 1];
 #pragma unroll
       for (int i = 0; i < N; ++i) ox[x][i] = px[lane + 64 * i];
     }
+  };
+  int x0 = each > 1 ? 4 * wave : 0;
+  load(x0);  // on their way before it is known how many there are
+  const int splits = (paged_rows(a, b, pair).n + a.C - 1) / a.C;
+  if (splits < 2) return;
+  float M = kLowest, L = 0.f, O[N] = {};
+  while (x0 < splits) {
     float top = M;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) top = fmaxf(top, mx[x]);
+    for (int x = 0; x < 4; ++x) top = x0 + x < splits ? fmaxf(top, mx[x]) : top;
     const float f = fast_exp2(M - top);
     M = top;
     L *= f;
@@ -584,6 +588,8 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a, int eac
 #pragma unroll
       for (int i = 0; i < N; ++i) O[i] = fmaf(ox[x][i], fx, O[i]);
     }
+    x0 += 4 * each;
+    if (x0 < splits) load(x0);
   }
   if (each > 1) {
     red[wave][D] = M;
@@ -607,7 +613,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a, int eac
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const float y = L == 0.f ? 0.f : O[i] * vs / L;
-    const size_t to = at * D + lane + 64 * i;
+    const size_t to = static_cast<size_t>(at) * D + lane + 64 * i;
     if (a.f32)
       static_cast<float*>(a.out)[to] = y;
     else
@@ -631,7 +637,7 @@ hipError_t launch_paged(const PagedLaunch& l, const PagedArgs& a, hipStream_t st
     const int64_t rows = static_cast<int64_t>(a.B) * a.Hq;
     const int each = l.S > 4 ? 4 : 1;
     paged_combine_kernel<D><<<dim3(static_cast<uint32_t>(each > 1 ? rows : (rows + 3) / 4)), dim3(256), 0,
-                              st>>>(a, each);
+                              st>>>(a, each, l.S);
   }
   return hipGetLastError();
 }
