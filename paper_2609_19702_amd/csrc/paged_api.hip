@@ -55,18 +55,20 @@ dsa_status paged_derive(const dsa_params* p, const dsa_shape* s, Derived* d, Pag
 }  // namespace
 
 // Eight waves to a workgroup.  Up to 896 rows, three or four tiles per wave, are not
-// split: the second kernel costs more (20 pairs, 696 rows, d = 64: 7.0 us whole, 8.8 in
-// three; 32 pairs, 832 rows, d = 128: 10.6 and 10.2 in four, but 3 us less from the
-// host).  Longer ones are split into 256 to 768 rows, as many as give each CU a
-// workgroup: few pairs get more (per layer, replayed, at 256, 512 and 128 workgroups in
-// all: one request of 8 heads and 9472 rows at most, fp8, d = 128, 12.8, 13.7 and 14.9
-// us).  From 512 rows on in whole tiles for all waves (24 requests of 4 heads and 1105
-// rows: 21.4 us in splits of 512, 22.8 in two of 576).  With 768 rows two workgroups
-// share a CU, and requests of other lengths end together (16 requests of 32 heads, 200
-// to 4300 rows, d = 128, in 768, 1024, 2048 and 4096 rows: 102, 103, 109 and 117 us; fp8
-// 57, 58, 61 and 66; 32 of 8 heads with four queries each 70, 79, 81 and 77).  All of
-// 2304 rows, 56 us for the whole requests' 54; 8 of 8 heads with eight queries each, up
-// to 9472 rows, 49 for the 46 of 2048 rows.
+// split: the second kernel costs more (per layer, replayed: 20 pairs, 696 rows, d = 64, 7.0
+// us whole and 8.3 in three; 160 such 9.0 and 10.7; 512 pairs, 832 rows, d = 128, 28.4 and
+// 30.4; but 32 of these 10.5 and 9.8).  Longer ones are split into 256 to 768 rows, as many
+// as give each CU a workgroup: few pairs get more (at 256, 512 and 128 workgroups in all:
+// four requests of 8 heads and 4300 rows at most, fp8, d = 128, 13.2, 15.2 and 15.0 us; one
+// of 9472 11.7, 11.7 and 12.9).  From 512 rows on in whole tiles for all waves (the four
+// requests 13.2 in splits of 512 rows, 13.8 in those of 576), but halves stay halves (24
+// requests of 4 heads and 1105 rows, 19.2 in two, 20.5 in three; 16 of 8 heads 19.7 and
+// 20.7; though 12 of 8, d = 64, 18.8 and 17.4).  With 768 rows two workgroups share a CU,
+// and requests of other lengths end together (16 requests of 32 heads, 200 to 4300 rows,
+// d = 128, in 512, 768, 1024, 2048 and 4096 rows: 100, 101, 103, 108 and 117 us; fp8 59,
+// 56, 57, 60 and 66; 32 of 8 heads with four queries each 71, 69, 78, 81 and 77).  All of
+// 2304 rows, 56 us for the whole requests' 55; 8 of 8 heads with eight queries each, up to
+// 9472 rows, 48 for the 45 of 2048 rows.
 PagedLaunch paged_launch(const Derived& d) {
   constexpr int64_t kWhole = 14, kLeast = 4, kMost = 12;  // units of 64 rows
   PagedLaunch l{};
@@ -74,7 +76,7 @@ PagedLaunch paged_launch(const Derived& d) {
   const int64_t units = (int64_t{d.rows_max} + 63) / 64;
   const int64_t want = std::max<int64_t>(1, 256 / pairs);
   int64_t per = (units + want - 1) / want;
-  if (per >= 8) per &= ~int64_t{3};
+  if (per >= 8 && want > 2) per &= ~int64_t{3};
   per = units <= kWhole ? units : std::clamp<int64_t>(per, kLeast, kMost);
   l.C = static_cast<int>(per * 64);
   l.S = static_cast<int>((units + per - 1) / per);
