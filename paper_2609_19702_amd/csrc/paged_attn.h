@@ -219,7 +219,7 @@ struct PagedTile {
 // The queries are read from LDS each time and the waves' sums lie over their V tiles: with
 // 128 registers and 768 rows, two workgroups share a CU.  Bound by memory and by how evenly
 // the CUs end: 32 requests of 8 heads, 2304 rows each, d = 128, four queries a head, 56 us
-// or 5.4 TB/s of reads (bf16); of 200 to 4300 rows, 70 us and 4.3, fp8 40 and 3.8, where the
+// or 5.4 TB/s of reads (bf16); of 200 to 4300 rows, 69 us and 4.4, fp8 42 and 3.6, where the
 // matrix cores are busy for 9% of the time.
 template <bool FP8, int D, int TERMS>
 __global__ __launch_bounds__(512, 4) void paged_kernel(PagedArgs a) {
@@ -542,8 +542,7 @@ __global__ __launch_bounds__(512, 4) void paged_row_kernel(PagedArgs a) {
 }
 
 // Joins the splits of a (request, query head): `each` waves of a workgroup for one, by
-// turns, four splits at a time.  Two dependent ways to memory: 4.0 us for three splits of
-// 768 heads, 4.5 for six of 1024.
+// turns, four splits at a time.  3.9 us for two splits of 768 heads, 4.5 for six of 1024.
 template <int D>
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a, int each, int most) {
   constexpr int N = D / 64;
