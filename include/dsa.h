@@ -758,8 +758,8 @@ DSA_API size_t dsa_paged_workspace_bytes(const dsa_params* p, const dsa_shape* s
  * (rows 0 .. len - 1 hold tokens) and new_b = d_new[b] new rows:
  *   - len < 0: the slot is unused; its pages go back to the pool.
  *   - Else the pages whose rows all lie in [prompt_b + S, len - W + 1) do: no step
- *     from here on attends them (W = N_r in diagonal and N_att - S in window mode;
- *     none in dense mode, S = 0).
+ *     from here on attends them, unless a later call's length is below this one's
+ *     (W = N_r in diagonal and N_att - S in window mode; none in dense mode, S = 0).
  *   - Rows len .. len + new_b - 1 get pages: an entry that names none, and one
  *     whose page other entries name too, takes the next free page.  (The shared
  *     page stays with its other users, or goes back after its last.)
