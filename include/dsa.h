@@ -884,7 +884,8 @@ DSA_API dsa_status dsa_paged_attention(const dsa_params* p, const dsa_shape* s,
  *   d_ws, ws_bytes dsa_beam_workspace_bytes() bytes, 16-byte aligned; need not be
  *                  cleared
  * Exponentials are summed in fp64 (four at a time in fp32), and scores compared in
- * fp64.  Equal rows have equal sums, wherever they lie.
+ * fp64, as (x[v] - max x) + (d_score[b][w] - log of the sum): however large the logits
+ * are, only their differences round.  Equal rows have equal sums, wherever they lie.
  * Errors: INVALID_ARG, WORKSPACE, HIP.
  */
 #define DSA_MAX_BEAMS 16

@@ -121,12 +121,13 @@ def attention(q, k, v, scale):
 
 
 def beam(logits, score):
-    """``(score, w, v)`` of the best candidates of one request, ``[W, V]`` fp64."""
+    """``(score, w, v)`` of the best candidates of one request, ``[W, V]`` fp64.  The
+    maximum is taken from a logit before anything is added, so that large logits round
+    nothing away."""
     beams, vocab = logits.shape
     with np.errstate(all="ignore"):
-        top = logits.max(1, keepdims=True)
-        lse = top + np.log(np.exp(logits - top).sum(1, keepdims=True))
-        z = (score[:, None] + (logits - lse)).reshape(-1)
+        x = logits - logits.max(1, keepdims=True)
+        z = (x + (score[:, None] - np.log(np.exp(x).sum(1, keepdims=True)))).reshape(-1)
     ok = z > -math.inf  # a NaN is none either
     at = np.flatnonzero(ok)
     at = at[np.lexsort((at, -z[at]))][:beams]

@@ -228,8 +228,10 @@ struct BeamCand {
   double z;
   int place;
 };
-__device__ __forceinline__ BeamCand beam_cand(double off, int w, uint64_t key) {
-  const double z = off + static_cast<double>(key_value(key));
+// A value's distance to its row's maximum comes first: large logits (`off` is the beam's score less
+// the log of its sum) would round the rest away.
+__device__ __forceinline__ BeamCand beam_cand(float top, double off, int w, uint64_t key) {
+  const double z = (static_cast<double>(key_value(key)) - static_cast<double>(top)) + off;
   const bool ok = key && z > -__builtin_inf();  // not so for a NaN
   return {ok ? z : -__builtin_inf(), ok ? w << 24 | key_place(key) : 0x7fffffff};
 }
@@ -255,6 +257,7 @@ __global__ __launch_bounds__(64 * DSA_MAX_BEAMS) void beam_pick_kernel(BeamArgs 
   __shared__ double z_s[kAll];
   __shared__ int place_s[kAll], chunk_s[kAll], best_s[DSA_MAX_BEAMS];
   __shared__ double off_s[DSA_MAX_BEAMS];
+  __shared__ float top_s[DSA_MAX_BEAMS];
   __shared__ int rank_s[2][kAll], some_s;
   __shared__ __attribute__((aligned(16))) uint64_t head_s[DSA_MAX_BEAMS][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -279,8 +282,11 @@ __global__ __launch_bounds__(64 * DSA_MAX_BEAMS) void beam_pick_kernel(BeamArgs 
   double sum = scaled(t0, s0);
   for (int c = lane + 64; c < a.chunks; c += 64) sum += scaled(a.tops[part + c], a.sums[part + c]);
   sum = wave_sum_f64(sum);
-  const double off = static_cast<double>(old) - (static_cast<double>(top) + log(sum));
-  if (lane == 0) off_s[wave] = off;
+  const double off = static_cast<double>(old) - log(sum);
+  if (lane == 0) {
+    off_s[wave] = off;
+    top_s[wave] = top;
+  }
 
   // The beam's best chunks (keys are all different but for 0, which is none).
   const int mine = wave * a.W;
@@ -295,7 +301,7 @@ __global__ __launch_bounds__(64 * DSA_MAX_BEAMS) void beam_pick_kernel(BeamArgs 
     fence_wave();
     const int rank = key_rank(k0, head_s[wave], (a.chunks + 3) & ~3);
     if (k0 && rank < a.W) {
-      const BeamCand c = beam_cand(off, wave, k0);
+      const BeamCand c = beam_cand(top, off, wave, k0);
       z_s[mine + rank] = c.z;
       place_s[mine + rank] = c.place;
       chunk_s[mine + rank] = mine / a.W * a.chunks + lane;
@@ -314,7 +320,7 @@ __global__ __launch_bounds__(64 * DSA_MAX_BEAMS) void beam_pick_kernel(BeamArgs 
       }
       under = wave_max_u64(most);
       if (under && most == under) {
-        const BeamCand c = beam_cand(off, wave, most);
+        const BeamCand c = beam_cand(top, off, wave, most);
         z_s[mine + k] = c.z;
         place_s[mine + k] = c.place;
         chunk_s[mine + k] = mine / a.W * a.chunks + at;
@@ -332,7 +338,7 @@ __global__ __launch_bounds__(64 * DSA_MAX_BEAMS) void beam_pick_kernel(BeamArgs 
     const uint64_t key = chunk < 0 ? 0
                                    : a.cands[(static_cast<int64_t>(b) * a.W * a.chunks + chunk) * a.W +
                                              tid % a.W];
-    const BeamCand c = beam_cand(off_s[w], w, key);
+    const BeamCand c = beam_cand(top_s[w], off_s[w], w, key);
     z_s[tid] = c.z;
     place_s[tid] = c.place;
     if (c.z > -__builtin_inf()) atomicAdd(&some_s, 1);
