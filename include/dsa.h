@@ -885,7 +885,8 @@ DSA_API dsa_status dsa_paged_attention(const dsa_params* p, const dsa_shape* s,
  *                  cleared
  * Exponentials are summed in fp64 (four at a time in fp32), and scores compared in
  * fp64, as (x[v] - max x) + (d_score[b][w] - log of the sum): however large the logits
- * are, only their differences round.  Equal rows have equal sums, wherever they lie.
+ * are, only their differences round.  Where that makes scores of one beam equal, the
+ * larger logit comes first.  Equal rows have equal sums, wherever they lie.
  * Errors: INVALID_ARG, WORKSPACE, HIP.
  */
 #define DSA_MAX_BEAMS 16

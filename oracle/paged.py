@@ -130,5 +130,6 @@ def beam(logits, score):
         z = (x + (score[:, None] - np.log(np.exp(x).sum(1, keepdims=True)))).reshape(-1)
     ok = z > -math.inf  # a NaN is none either
     at = np.flatnonzero(ok)
-    at = at[np.lexsort((at, -z[at]))][:beams]
+    # equal scores: the lower beam, its larger logit (rounding makes scores equal), the lower token
+    at = at[np.lexsort((at, -logits.reshape(-1)[at], at // vocab, -z[at]))][:beams]
     return [(z[i], int(i) // vocab, int(i) % vocab) for i in at]

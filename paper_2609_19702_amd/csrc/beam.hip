@@ -25,7 +25,6 @@ __device__ __forceinline__ float from_ordered(uint32_t u) {
 __device__ __forceinline__ float key_value(uint64_t k) {
   return from_ordered(static_cast<uint32_t>(k >> 32));
 }
-__device__ __forceinline__ int key_place(uint64_t k) { return ~static_cast<int>(k); }
 
 __device__ __forceinline__ uint64_t wave_max_u64(uint64_t x) { return ~wave_min_u64(~x); }
 
@@ -223,27 +222,37 @@ __global__ __launch_bounds__(kBeamThreads) void beam_row_kernel(BeamArgs a) {
   }
 }
 
-// A candidate of the last steps: its score, and its beam and token in 28 bits.
+// A candidate of the last steps: its score, and what decides between equal ones, larger ones
+// first: beam, logit and token (4, 32 and 24 bits, beam and token counted from above).  A
+// beam's scores grow with its logits but for their rounding, so its candidates come as its
+// keys do.
 struct BeamCand {
   double z;
-  int place;
+  uint64_t tie;
 };
 // A value's distance to its row's maximum comes first: large logits (`off` is the beam's score less
 // the log of its sum) would round the rest away.
 __device__ __forceinline__ BeamCand beam_cand(float top, double off, int w, uint64_t key) {
   const double z = (static_cast<double>(key_value(key)) - static_cast<double>(top)) + off;
   const bool ok = key && z > -__builtin_inf();  // not so for a NaN
-  return {ok ? z : -__builtin_inf(), ok ? w << 24 | key_place(key) : 0x7fffffff};
+  const uint64_t tie = (static_cast<uint64_t>(DSA_MAX_BEAMS - 1 - w) << 56) | ((key >> 32) << 24) |
+                       (key & 0xffffff);
+  return {ok ? z : -__builtin_inf(), ok ? tie : 0};
 }
+__device__ __forceinline__ int cand_beam(uint64_t tie) {
+  return DSA_MAX_BEAMS - 1 - static_cast<int>(tie >> 56);
+}
+__device__ __forceinline__ int cand_token(uint64_t tie) { return ~static_cast<int>(tie) & 0xffffff; }
+
 // How many of n candidates come before each of them, into rank[n] (zeros): the workgroup's
 // threads share the comparisons.
-__device__ __forceinline__ void cand_ranks(const double* z, const int* place, int n, int* rank) {
+__device__ __forceinline__ void cand_ranks(const double* z, const uint64_t* tie, int n, int* rank) {
   const int tid = threadIdx.x, i = tid % n, parts = blockDim.x / n;
   const double zi = z[i];
-  const int at = place[i];
+  const uint64_t at = tie[i];
   int before = 0;
   if (tid < parts * n)
-    for (int j = tid / n; j < n; j += parts) before += z[j] > zi || (z[j] == zi && place[j] < at);
+    for (int j = tid / n; j < n; j += parts) before += z[j] > zi || (z[j] == zi && tie[j] > at);
   if (before) atomicAdd(rank + i, before);
 }
 
@@ -255,7 +264,8 @@ __device__ __forceinline__ void cand_ranks(const double* z, const int* place, in
 __global__ __launch_bounds__(64 * DSA_MAX_BEAMS) void beam_pick_kernel(BeamArgs a) {
   constexpr int kAll = DSA_MAX_BEAMS * DSA_MAX_BEAMS;
   __shared__ double z_s[kAll];
-  __shared__ int place_s[kAll], chunk_s[kAll], best_s[DSA_MAX_BEAMS];
+  __shared__ uint64_t tie_s[kAll];
+  __shared__ int chunk_s[kAll], best_s[DSA_MAX_BEAMS];
   __shared__ double off_s[DSA_MAX_BEAMS];
   __shared__ float top_s[DSA_MAX_BEAMS];
   __shared__ int rank_s[2][kAll], some_s;
@@ -292,7 +302,7 @@ __global__ __launch_bounds__(64 * DSA_MAX_BEAMS) void beam_pick_kernel(BeamArgs 
   const int mine = wave * a.W;
   if (lane < a.W) {
     z_s[mine + lane] = -__builtin_inf();
-    place_s[mine + lane] = 0x7fffffff;
+    tie_s[mine + lane] = 0;
     chunk_s[mine + lane] = -1;
   }
   fence_wave();
@@ -303,7 +313,7 @@ __global__ __launch_bounds__(64 * DSA_MAX_BEAMS) void beam_pick_kernel(BeamArgs 
     if (k0 && rank < a.W) {
       const BeamCand c = beam_cand(top, off, wave, k0);
       z_s[mine + rank] = c.z;
-      place_s[mine + rank] = c.place;
+      tie_s[mine + rank] = c.tie;
       chunk_s[mine + rank] = mine / a.W * a.chunks + lane;
     }
   } else {
@@ -322,13 +332,13 @@ __global__ __launch_bounds__(64 * DSA_MAX_BEAMS) void beam_pick_kernel(BeamArgs 
       if (under && most == under) {
         const BeamCand c = beam_cand(top, off, wave, most);
         z_s[mine + k] = c.z;
-        place_s[mine + k] = c.place;
+        tie_s[mine + k] = c.tie;
         chunk_s[mine + k] = mine / a.W * a.chunks + at;
       }
     }
   }
   __syncthreads();
-  cand_ranks(z_s, place_s, n, rank_s[0]);
+  cand_ranks(z_s, tie_s, n, rank_s[0]);
   __syncthreads();
   if (tid < n && z_s[tid] > -__builtin_inf() && rank_s[0][tid] < a.W)
     best_s[rank_s[0][tid]] = chunk_s[tid];
@@ -340,19 +350,19 @@ __global__ __launch_bounds__(64 * DSA_MAX_BEAMS) void beam_pick_kernel(BeamArgs 
                                              tid % a.W];
     const BeamCand c = beam_cand(top_s[w], off_s[w], w, key);
     z_s[tid] = c.z;
-    place_s[tid] = c.place;
+    tie_s[tid] = c.tie;
     if (c.z > -__builtin_inf()) atomicAdd(&some_s, 1);
   }
   __syncthreads();
-  cand_ranks(z_s, place_s, n, rank_s[1]);
+  cand_ranks(z_s, tie_s, n, rank_s[1]);
   __syncthreads();
   if (tid >= n) return;
   const int rank = rank_s[1][tid];
   const int64_t to = static_cast<int64_t>(b) * a.W;
   if (z_s[tid] > -__builtin_inf() && rank < a.W) {
     a.next[to + rank] = static_cast<float>(z_s[tid]);
-    a.parent[to + rank] = b * a.W + (place_s[tid] >> 24);
-    a.token[to + rank] = place_s[tid] & 0xffffff;
+    a.parent[to + rank] = b * a.W + cand_beam(tie_s[tid]);
+    a.token[to + rank] = cand_token(tie_s[tid]);
   }
   if (tid >= some_s && tid < a.W) {  // where there are fewer
     a.next[to + tid] = -__builtin_inff();
