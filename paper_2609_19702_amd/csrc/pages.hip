@@ -135,16 +135,18 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
 
   int found = 0;
   if (total > 0) {
-    const int c = a.cursor[0] % a.pool, start = c < 0 ? c + a.pool : c;
-    for (int i0 = 0; i0 < a.pool && found < total; i0 += kLook * kUpdateThreads) {
+    // Unsigned: a place on from the cursor is below twice the pool, so below 2^32.
+    const uint32_t pool = a.pool;
+    const int c = a.cursor[0] % a.pool;
+    const uint32_t start = c < 0 ? c + a.pool : c;
+    for (uint32_t i0 = 0; i0 < pool && found < total; i0 += kLook * kUpdateThreads) {
       int page[kLook], rank[kLook];
       bool free[kLook];
 #pragma unroll
       for (int k = 0; k < kLook; ++k) {
-        const int i = i0 + k * kUpdateThreads + tid;
-        page[k] = start + min(i, a.pool - 1);
-        page[k] = page[k] >= a.pool ? page[k] - a.pool : page[k];
-        free[k] = load_ref(a.refs + page[k]) == 0 && i < a.pool;
+        const uint32_t i = i0 + k * kUpdateThreads + tid, at = start + min(i, pool - 1);
+        page[k] = static_cast<int>(at >= pool ? at - pool : at);
+        free[k] = load_ref(a.refs + page[k]) == 0 && i < pool;
       }
 #pragma unroll
       for (int k = 0; k < kLook; ++k) {

@@ -1,0 +1,69 @@
+"""Tables and pools of the largest sizes that the calls take: places of 31 bits."""
+
+import pytest
+import torch
+
+from paper_2609_19702_amd import binding as B
+from tests.paged_util import DEV, ints
+
+pytestmark = pytest.mark.gpu
+
+MOST = (1 << 31) - 1
+
+
+def filled(n, value):
+    return torch.full((n,), value, dtype=torch.int32, device=DEV)
+
+
+class Pool:
+    """Two requests over a pool of one-row pages."""
+
+    def __init__(self, refs, cursor, width=8):
+        self.p = B.make_params(0, 64, 64, 1, 1, B.MODE_DENSE)
+        self.pages = B.make_pages(1, torch.full((2, width), -1, dtype=torch.int32, device=DEV), refs,
+                                  ints([cursor]))
+        self.slots = torch.full((2, width), 7, dtype=torch.int32, device=DEV)
+        self.pos, self.flags = ints([7, 7]), ints([7, 7])
+        self.copies = torch.full((2, 3), 7, dtype=torch.int32, device=DEV)
+
+    def update(self, lengths, new):
+        B.page_update(self.p, self.pages, ints(lengths), ints(new), self.slots, self.pos,
+                      self.copies, self.flags)
+        return self.flags.tolist()
+
+
+@pytest.mark.parametrize("pool,cursor", [(MOST, MOST - 1), (MOST, MOST - 3), (MOST, 1 << 30),
+                                         (MOST, -2), (MOST, MOST), (MOST - 4095, MOST - 4096),
+                                         ((1 << 30) + 1, 1 << 30), ((1 << 30) + 4099, (1 << 30) + 7)])
+def test_a_large_pool_is_searched_around(pool, cursor):
+    """From the cursor on, past the pool's end to its beginning."""
+    refs = filled(pool, 0)
+    start = cursor % pool if cursor >= 0 else (cursor + pool) % pool
+    busy = [(start + i) % pool for i in (0, 2, 5)]
+    refs[torch.tensor(busy, device=DEV)] = 9
+    free = [(start + i) % pool for i in range(12) if i not in (0, 2, 5)]
+    x = Pool(refs, cursor)
+    assert x.update([0, 0], [4, 3]) == [0, 0]
+    assert x.slots.tolist() == [free[:4] + [-1] * 4, free[4:7] + [-1] * 5]
+    assert x.pages.table.tolist() == x.slots.tolist()
+    assert x.pages.cursor.item() == (free[6] + 1) % pool
+    at = torch.tensor(free[:7], device=DEV)
+    assert (refs[at] == 1).all() and (refs[torch.tensor(busy, device=DEV)] == 9).all()
+    refs[at] = 0
+    refs[torch.tensor(busy, device=DEV)] = 0
+    assert not refs.any()
+
+
+@pytest.mark.parametrize("pool", [MOST, (1 << 30) + 3])
+def test_the_last_pages_that_a_large_pool_is_searched_for(pool):
+    """All but the two before the cursor, and one at the pool's end, are taken."""
+    refs = filled(pool, 1)
+    cursor = (1 << 30) - 5
+    refs[pool - 1] = refs[cursor - 1] = refs[cursor - 2] = 0
+    x = Pool(refs, cursor)
+    assert x.update([0, 0], [1, 2]) == [0, 0]
+    assert x.pages.table[:, :2].tolist() == [[pool - 1, -1], [cursor - 2, cursor - 1]]
+    assert x.pages.cursor.item() == cursor
+    assert (refs == 1).all()
+    assert x.update([1, 2], [1, 1]) == [1, 1]  # none is left
+    assert x.slots.tolist() == [[-1] * 8] * 2 and x.pages.cursor.item() == cursor
