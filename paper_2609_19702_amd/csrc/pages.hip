@@ -1,5 +1,7 @@
 // Page tables: pages for new rows and back, requests that go on from others'
 // pages, and the new K/V rows' way into their slots.
+#include <algorithm>
+
 #include "device.h"
 #include "paged.h"
 
@@ -258,32 +260,41 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
 
 constexpr int kReorderThreads = 512;
 constexpr int kReorderMost = 2048;  // entries that a workgroup holds, about
+constexpr uint32_t kReorderGroups = 1 << 20;  // of a launch, whose threads are below 2^32
 
 // A workgroup takes some columns of the table: all their entries into LDS, then
-// every row its parent's.  Bound by the way to memory and back: 2.2 us for four rows of 53
-// entries, 4.5 for 256.
+// every row its parent's; then others, where there are more of them than workgroups.  Bound by
+// the way to memory and back: 2.2 us for four rows of 53 entries, 4.5 for 256.
 __global__ __launch_bounds__(kReorderThreads) void page_reorder_kernel(PageReorderArgs a,
-                                                                      int lg_cols) {
+                                                                      int lg_cols, uint32_t groups) {
   extern __shared__ int32_t held[];  // [B][cols]
-  const int cols = 1 << lg_cols, first = blockIdx.x << lg_cols;
+  const int cols = 1 << lg_cols;
+  const uint32_t M = a.M;  // columns are below M + cols, so below 2^32
   const int n = a.B << lg_cols;
-  for (int e = threadIdx.x; e < n; e += kReorderThreads) {
-    const int i = first + (e & (cols - 1));
-    held[e] = i < a.M ? a.table[static_cast<int64_t>(e >> lg_cols) * a.M + i] : -1;
-  }
-  int parent = threadIdx.x < n ? a.parent[threadIdx.x >> lg_cols] : 0;
-  __syncthreads();
-  for (int e = threadIdx.x; e < n; e += kReorderThreads) {
-    const int b = e >> lg_cols, i = first + (e & (cols - 1));
-    if (e != static_cast<int>(threadIdx.x)) parent = a.parent[b];
-    if (i >= a.M || parent == b) continue;
-    const int old = held[e];
-    const bool there = static_cast<unsigned>(parent) < static_cast<unsigned>(a.B);
-    const int page = there ? held[(parent << lg_cols) + (e & (cols - 1))] : -1;
-    if (page == old) continue;
-    if (in_pool(page, a.pool)) atomicAdd(a.refs + page, 1);
-    if (in_pool(old, a.pool)) atomicSub(a.refs + old, 1);
-    a.table[static_cast<int64_t>(b) * a.M + i] = page;
+  for (uint32_t group = blockIdx.x;;) {
+    const uint32_t first = group << lg_cols;
+    for (int e = threadIdx.x; e < n; e += kReorderThreads) {
+      const uint32_t i = first + (e & (cols - 1));
+      held[e] = i < M ? a.table[static_cast<int64_t>(e >> lg_cols) * a.M + i] : -1;
+    }
+    int parent = threadIdx.x < n ? a.parent[threadIdx.x >> lg_cols] : 0;
+    __syncthreads();
+    for (int e = threadIdx.x; e < n; e += kReorderThreads) {
+      const int b = e >> lg_cols;
+      const uint32_t i = first + (e & (cols - 1));
+      if (e != static_cast<int>(threadIdx.x)) parent = a.parent[b];
+      if (i >= M || parent == b) continue;
+      const int old = held[e];
+      const bool there = static_cast<unsigned>(parent) < static_cast<unsigned>(a.B);
+      const int page = there ? held[(parent << lg_cols) + (e & (cols - 1))] : -1;
+      if (page == old) continue;
+      if (in_pool(page, a.pool)) atomicAdd(a.refs + page, 1);
+      if (in_pool(old, a.pool)) atomicSub(a.refs + old, 1);
+      a.table[static_cast<int64_t>(b) * a.M + i] = page;
+    }
+    group += gridDim.x;
+    if (group >= groups) return;
+    __syncthreads();  // all have read what the next columns replace
   }
 }
 
@@ -395,8 +406,9 @@ hipError_t launch_page_update(const PageUpdateArgs& a, hipStream_t st) {
 hipError_t launch_page_reorder(const PageReorderArgs& a, hipStream_t st) {
   int lg = 0;
   while (lg < 4 && (a.B << (lg + 1)) <= kReorderMost && (1 << lg) < a.M) ++lg;
-  const int groups = (a.M + (1 << lg) - 1) >> lg;
-  page_reorder_kernel<<<dim3(groups), dim3(kReorderThreads), (a.B << lg) * 4, st>>>(a, lg);
+  const uint32_t groups = (static_cast<uint32_t>(a.M) + (1 << lg) - 1) >> lg;
+  const dim3 grid(std::min(groups, kReorderGroups));
+  page_reorder_kernel<<<grid, dim3(kReorderThreads), (a.B << lg) * 4, st>>>(a, lg, groups);
   return hipGetLastError();
 }
 

@@ -67,3 +67,34 @@ def test_the_last_pages_that_a_large_pool_is_searched_for(pool):
     assert (refs == 1).all()
     assert x.update([1, 2], [1, 1]) == [1, 1]  # none is left
     assert x.slots.tolist() == [[-1] * 8] * 2 and x.pages.cursor.item() == cursor
+
+
+@pytest.mark.parametrize("batch,width", [(1, MOST), (2, MOST // 2), (1, MOST - 15), (3, 70000001),
+                                         (130, 9000001)])
+def test_long_rows_of_a_table(batch, width):
+    """More columns than a launch has workgroups for, the last ones of 31 bits."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    table = torch.empty((batch, width), dtype=torch.int32, device=DEV)
+    table.fill_(-1)
+    at = torch.randint(0, width, (batch, 5000), generator=g, device=DEV)
+    at[:, :3] = torch.tensor([0, width - 1, width - 2], device=DEV)
+    table.scatter_(1, at, torch.randint(0, 100, at.shape, generator=g, device=DEV,
+                                        dtype=torch.int32))
+    refs = filled(100, 1 << 20)
+    pages = B.make_pages(1, table, refs)
+    for parent in ([batch - 1 - b for b in range(batch)], [-1] + [0] * (batch - 1)):
+        want = torch.full((batch, 5000), -1, dtype=torch.int32, device=DEV)
+        here = torch.stack([table[p].gather(0, at[b]) if p >= 0 else want[b]
+                            for b, p in enumerate(parent)])
+        count = [int((table[p] >= 0).sum()) if p >= 0 else 0 for p in parent]
+        users = torch.zeros(100, dtype=torch.int64, device=DEV)
+        for p in parent:
+            if p >= 0:
+                users += torch.bincount(table[p][table[p] >= 0], minlength=100)
+        for b in range(batch):
+            users -= torch.bincount(table[b][table[b] >= 0], minlength=100)
+        before = refs.long()
+        B.page_reorder(pages, ints(parent))
+        assert torch.equal(table.gather(1, at), here)
+        assert [int((table[b] >= 0).sum()) for b in range(batch)] == count
+        assert torch.equal(refs.long(), before + users)
