@@ -23,9 +23,11 @@ struct PageReq {
   int len, fresh, prompt, upto;
 };
 
-// Its entries of new rows, [e0, e1); fits: it is in use, and its rows have entries.
+// Its entries of new rows, [e0, e1), counted without signs as they are everywhere (a step of a
+// group's lanes past the last of 2^31 - 1 has no place below 0); fits: it is in use, and its
+// rows have entries.
 struct PageSpan {
-  int e0, e1;
+  uint32_t e0, e1;
   bool fits;
 };
 __device__ __forceinline__ PageSpan page_span(const PageUpdateArgs& a, const PageReq& r) {
@@ -34,7 +36,7 @@ __device__ __forceinline__ PageSpan page_span(const PageUpdateArgs& a, const Pag
   s.fits = r.len >= 0 && end <= static_cast<int64_t>(a.M) << a.lg;
   const bool some = s.fits && r.fresh > 0;
   s.e0 = some ? r.len >> a.lg : 0;
-  s.e1 = some ? static_cast<int>((end + (1 << a.lg) - 1) >> a.lg) : 0;
+  s.e1 = some ? static_cast<uint32_t>((end + (1 << a.lg) - 1) >> a.lg) : 0;
   return s;
 }
 
@@ -63,8 +65,9 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
   extern __shared__ PageReq req[];
   __shared__ int part[kLook][kUpdateWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int sub = tid % LANES, group = tid / LANES;
-  const int shift = lane - sub;  // of the group's ballot
+  const uint32_t sub = tid % LANES;
+  const int group = tid / LANES;
+  const int shift = lane - static_cast<int>(sub);  // of the group's ballot
   const int rows = 1 << a.lg;
 
   for (int b = tid; b < a.B; b += kUpdateThreads) {
@@ -82,14 +85,14 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
   for (int b = group; b < a.B; b += kUpdateThreads / LANES) {
     const PageReq r = req[b];
     int32_t* row = a.table + static_cast<int64_t>(b) * a.M;
-    int lo = 0, hi = r.len < 0 ? a.M : 0;
+    uint32_t lo = 0, hi = r.len < 0 ? a.M : 0;
     if (r.len >= 0 && a.W > 0) {
       const int64_t front = static_cast<int64_t>(r.prompt) + a.S;
       const int64_t back = static_cast<int64_t>(r.len) - a.W + 1;
-      lo = static_cast<int>(min((front + rows - 1) >> a.lg, static_cast<int64_t>(a.M)));
-      hi = back > 0 ? static_cast<int>(min(back >> a.lg, static_cast<int64_t>(a.M))) : 0;
+      lo = static_cast<uint32_t>(min((front + rows - 1) >> a.lg, static_cast<int64_t>(a.M)));
+      hi = back > 0 ? static_cast<uint32_t>(min(back >> a.lg, static_cast<int64_t>(a.M))) : 0;
     }
-    for (int i = lo + sub; i < hi; i += LANES) {
+    for (uint32_t i = lo + sub; i < hi; i += LANES) {
       const int page = row[i];
       if (in_pool(page, a.pool)) atomicSub(a.refs + page, 1);
       if (page != -1) row[i] = -1;
@@ -104,7 +107,7 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
     const PageSpan s = page_span(a, req[b]);
     int32_t* row = a.table + static_cast<int64_t>(b) * a.M;
     int need = 0;
-    for (int i = s.e0 + sub; i - sub < s.e1; i += LANES) {
+    for (uint32_t i = s.e0 + sub; i - sub < s.e1; i += LANES) {
       int want = 0;  // what the entry becomes, if anything
       if (i < s.e1) {
         const int page = row[i];
@@ -189,7 +192,8 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
     int x = -1, y = -1;  // the first entry's old and new page, where rows are copied
     int last = 0;        // the last page that the request is given
     int got = -1;        // page of entry e0 + sub
-    for (int i = s.e0 + sub, rank = 0; i - sub < s.e1; i += LANES) {
+    int rank = 0;
+    for (uint32_t i = s.e0 + sub; i - sub < s.e1; i += LANES) {
       int now = i < s.e1 ? row[i] : 0;
       const uint32_t mask = static_cast<uint32_t>(__ballot(now < 0) >> shift) & kAll;
       if (now < 0) {
@@ -240,9 +244,10 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
       continue;
     }
     fence_wave();
-    const int at = (n ? r.len : 0) + sub, e = at >> a.lg;
-    const int held = __shfl(got, shift + ((e - s.e0) & (LANES - 1)), 64);
-    if (sub < a.N) slots[sub] = sub < n ? (held << a.lg) + (at & (rows - 1)) : -1;
+    const uint32_t at = (n ? r.len : 0) + sub, e = at >> a.lg;
+    const int held = __shfl(got, shift + static_cast<int>((e - s.e0) & (LANES - 1)), 64);
+    if (static_cast<int>(sub) < a.N)
+      slots[sub] = static_cast<int>(sub) < n ? (held << a.lg) + static_cast<int>(at & (rows - 1)) : -1;
   }
   if (a.N <= LANES) return;
   __syncthreads();
@@ -250,9 +255,12 @@ __global__ __launch_bounds__(kUpdateThreads) void page_update_kernel(PageUpdateA
     const int len = req[b].len, n = req[b].fresh;
     const int32_t* row = a.table + static_cast<int64_t>(b) * a.M;
     int32_t* slots = a.slots + static_cast<int64_t>(b) * a.N;
-    for (int i = lane; i < a.N; i += 64) {
+    for (int64_t i = lane; i < a.N; i += 64) {
       int slot = -1;
-      if (i < n) slot = (row[(len + i) >> a.lg] << a.lg) + ((len + i) & (rows - 1));
+      if (i < n) {
+        const int at = len + static_cast<int>(i);
+        slot = (row[at >> a.lg] << a.lg) + (at & (rows - 1));
+      }
       slots[i] = slot;
     }
   }

@@ -98,3 +98,51 @@ def test_long_rows_of_a_table(batch, width):
         assert torch.equal(table.gather(1, at), here)
         assert [int((table[b] >= 0).sum()) for b in range(batch)] == count
         assert torch.equal(refs.long(), before + users)
+
+
+@pytest.mark.parametrize("page,width", [(1, MOST), (1, MOST - 1), (2, MOST // 2), (16, MOST // 16)])
+def test_the_last_rows_of_the_longest_table(page, width):
+    """Requests of close to 2^31 rows, with few and many slots."""
+    table = torch.full((1, width), -1, dtype=torch.int32, device=DEV)
+    p = B.make_params(0, 64, 64, 1, 1, B.MODE_DENSE)
+    for most in (1, 16, 17, 65):
+        for new in {1, 3, most}:
+            new = min(new, most)
+            length = width * page - new
+            entries = list(range(length // page, width))
+            refs = filled(100, 0)
+            pages = B.make_pages(page, table, refs, ints([7]))
+            slots = torch.full((1, most), 7, dtype=torch.int32, device=DEV)
+            pos, copies, flags = ints([7]), ints([[7, 7, 7]]), ints([7])
+
+            def update(at, n):
+                B.page_update(p, pages, ints([at]), ints([n]), slots, pos, copies, flags)
+
+            update(length, new)
+            got = [7 + i for i in range(len(entries))]
+            assert table[0, entries[0]:].tolist() == got and flags.item() == 0
+            assert pos.item() == length + new - 1 and copies.tolist() == [[-1] * 3]
+            want = [got[r // page - entries[0]] * page + r % page
+                    for r in range(length, length + new)]
+            assert slots.tolist() == [want + [-1] * (most - new)]
+            assert refs.nonzero().view(-1).tolist() == got and (refs <= 1).all()
+            update(length, new + 1)  # clamped to the slots, or a row too many
+            assert flags.item() == (B.PAGE_FLAG_TOO_LONG if new < most else 0)
+            update(MOST, 1)
+            assert flags.item() == B.PAGE_FLAG_TOO_LONG
+            update(width * page, 0)
+            assert flags.item() == 0 and slots.tolist() == [[-1] * most]
+            table[0, entries[0]:] = -1
+    assert not (table != -1).any()
+
+
+def test_slots_past_31_bits_of_bytes():
+    """As many slots as a call takes: those past the new rows hold -1."""
+    most = MOST
+    slots = torch.full((1, most), 7, dtype=torch.int32, device=DEV)
+    table = torch.full((1, 9), -1, dtype=torch.int32, device=DEV)
+    pos, copies, flags = ints([7]), ints([[7, 7, 7]]), ints([7])
+    p = B.make_params(0, 64, 64, 1, 1, B.MODE_DENSE)
+    B.page_update(p, B.make_pages(4, table, filled(9, 0), ints([0])), ints([0]), ints([30]), slots,
+                  pos, copies, flags)
+    assert slots[0, :30].tolist() == list(range(30)) and (slots[0, 30:] == -1).all()
