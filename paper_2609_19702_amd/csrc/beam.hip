@@ -91,7 +91,8 @@ __global__ __launch_bounds__(kBeamThreads) void beam_row_kernel(BeamArgs a) {
   __shared__ __attribute__((aligned(16))) uint64_t list_s[64];
   __shared__ int n_s;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int chunk = blockIdx.x % a.chunks, row = blockIdx.x / a.chunks;
+  const uint32_t part = a.first + blockIdx.x;
+  const int chunk = part % a.chunks, row = part / a.chunks;
   // Pieces of VL values, which begin at any value: a row's sums do not depend on where it
   // lies, so equal rows tie.
   const uint8_t* start = static_cast<const uint8_t*>(a.x) + row * a.stride * (16 / VL);
@@ -210,15 +211,15 @@ __global__ __launch_bounds__(kBeamThreads) void beam_row_kernel(BeamArgs a) {
   if (wave) return;
   const uint64_t key = lane < n ? list_s[lane] : 0;
   const int rank = key_rank(key, list_s, (n + 3) & ~3);
-  uint64_t* to = a.cands + static_cast<int64_t>(blockIdx.x) * a.W;
+  uint64_t* to = a.cands + static_cast<int64_t>(part) * a.W;
   const int some = __popcll(__ballot(key != 0));
   if (key && rank < a.W) to[rank] = key;
   if (lane >= some && lane < a.W) to[lane] = 0;
   if (lane == 0) {
     double s = 0.;
     for (int w = 0; w < kBeamWaves; ++w) s += sum_s[w];
-    a.sums[blockIdx.x] = s;
-    a.tops[blockIdx.x] = top;
+    a.sums[part] = s;
+    a.tops[part] = top;
   }
 }
 
@@ -390,15 +391,19 @@ BeamLaunch beam_launch(int B, int W, int V, bool bf16) {
   return l;
 }
 
-hipError_t launch_beam(const BeamArgs& a, hipStream_t st) {
-  const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.B) * a.W * a.chunks));
-  const dim3 block(kBeamThreads);
-  if (a.bf16)
-    a.many ? beam_row_kernel<true, kMany><<<grid, block, 0, st>>>(a)
-           : beam_row_kernel<true, kFew><<<grid, block, 0, st>>>(a);
-  else
-    a.many ? beam_row_kernel<false, kMany><<<grid, block, 0, st>>>(a)
-           : beam_row_kernel<false, kFew><<<grid, block, 0, st>>>(a);
+hipError_t launch_beam(BeamArgs a, hipStream_t st) {
+  const int64_t parts = static_cast<int64_t>(a.B) * a.W * a.chunks;
+  const hipError_t e = launch_parts(parts, kBeamThreads, [&](uint32_t first, dim3 grid) {
+    const dim3 block(kBeamThreads);
+    a.first = first;
+    if (a.bf16)
+      a.many ? beam_row_kernel<true, kMany><<<grid, block, 0, st>>>(a)
+             : beam_row_kernel<true, kFew><<<grid, block, 0, st>>>(a);
+    else
+      a.many ? beam_row_kernel<false, kMany><<<grid, block, 0, st>>>(a)
+             : beam_row_kernel<false, kFew><<<grid, block, 0, st>>>(a);
+  });
+  if (e != hipSuccess) return e;
   beam_pick_kernel<<<dim3(a.B), dim3(64 * a.W), 0, st>>>(a);
   return hipGetLastError();
 }

@@ -2,9 +2,24 @@
 // argument blocks and launchers.
 #pragma once
 
+#include <algorithm>
+
 #include "internal.h"
 
 namespace dsa {
+
+// A launch holds fewer than 2^32 threads: `launch(first, grid)` for every part of `groups`
+// workgroups, the first of which is workgroup `first` of them all.
+template <typename Launch>
+hipError_t launch_parts(int64_t groups, int threads, Launch launch) {
+  const int64_t most = ((int64_t{1} << 32) - 1) / threads;
+  for (int64_t first = 0; first < groups; first += most) {
+    launch(static_cast<uint32_t>(first), dim3(static_cast<uint32_t>(std::min(most, groups - first))));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 
 struct PageUpdateArgs {
   const int32_t* length;
@@ -40,6 +55,7 @@ struct PagedAppendArgs {
   const float* ks;
   const float* vs;
   int layers, B, N, Hkv, D, pool, lg;
+  uint32_t first;  // workgroup of the launch's first
 };
 
 struct PagedArgs {
@@ -63,6 +79,7 @@ struct PagedArgs {
   int M, pool, lg;
   int C;    // rows of a split
   int f32;  // output in fp32
+  uint32_t first;  // workgroup of the launch's first
 };
 
 // Launch of dsa_paged_attention.
@@ -85,6 +102,7 @@ struct BeamArgs {
   uint64_t* cands;  // [B * W][chunks][W] the largest values and their places
   int B, W, V, chunks, per;  // per: 16-byte pieces of a row that a workgroup takes
   bool bf16, many;
+  uint32_t first;  // workgroup of the launch's first
 };
 struct BeamLaunch {
   int per, chunks;
@@ -100,6 +118,6 @@ hipError_t launch_paged_bf16(const Derived& d, const PagedLaunch& l, const Paged
                              hipStream_t st);
 hipError_t launch_paged_fp8(const Derived& d, const PagedLaunch& l, const PagedArgs& a,
                             hipStream_t st);
-hipError_t launch_beam(const BeamArgs& a, hipStream_t st);
+hipError_t launch_beam(BeamArgs a, hipStream_t st);
 
 }  // namespace dsa

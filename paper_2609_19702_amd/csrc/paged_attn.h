@@ -77,8 +77,9 @@ struct PagedWork {
 __device__ __forceinline__ bool paged_work(const PagedArgs& a, int lane, int wave, int waves,
                                            int64_t* place, uint32_t* mask, PagedWork& w) {
   const int pairs = a.B * a.Hkv;
-  w.s = uniform(blockIdx.x / pairs);
-  const int pair = blockIdx.x - w.s * pairs;
+  const uint32_t group = a.first + blockIdx.x;
+  w.s = uniform(group / pairs);
+  const int pair = group - w.s * pairs;
   w.b = uniform(pair / a.Hkv);
   w.h = pair - w.b * a.Hkv;
   w.first = w.s * a.C;
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(512, 4) void paged_kernel(PagedArgs a) {
 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int lr = lane & 15, lq = lane >> 4, rg = lane / LPR, col = lane % LPR;
-  const int pair = uniform(blockIdx.x % (a.B * a.Hkv)), b = uniform(pair / a.Hkv);
+  const int pair = uniform((a.first + blockIdx.x) % (a.B * a.Hkv)), b = uniform(pair / a.Hkv);
   const int h = pair - b * a.Hkv, G = a.G;
   int64_t* place = reinterpret_cast<int64_t*>(lds);
   uint32_t* mask = reinterpret_cast<uint32_t*>(lds + a.C * 8);
@@ -439,7 +440,7 @@ __global__ __launch_bounds__(512, 4) void paged_row_kernel(PagedArgs a) {
   uint32_t* mask = reinterpret_cast<uint32_t*>(lds + a.C * 8);
   float* red = reinterpret_cast<float*>(lds + a.C * 8 + ((a.C / 8 + 15) & ~15));
 
-  const int pair = uniform(blockIdx.x % (a.B * a.Hkv)), h = uniform(pair % a.Hkv);
+  const int pair = uniform((a.first + blockIdx.x) % (a.B * a.Hkv)), h = uniform(pair % a.Hkv);
   uint4 qr[EPL / 8];
 #pragma unroll
   for (int i = 0; i < EPL / 8; ++i)
@@ -548,7 +549,8 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a, int eac
   constexpr int N = D / 64;
   __shared__ float red[4][D + 2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int at = uniform(each > 1 ? blockIdx.x : blockIdx.x * 4 + wave);
+  const uint32_t group = a.first + blockIdx.x;
+  const int at = uniform(each > 1 ? group : group * 4 + wave);
   if (at >= a.B * a.Hq) return;
   const int b = uniform(at / a.Hq), hq = at - b * a.Hq, h = uniform(hq / a.G), g = hq - h * a.G;
   const int pair = b * a.Hkv + h;
@@ -621,24 +623,27 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a, int eac
 }
 
 template <bool FP8, int D>
-hipError_t launch_paged(const PagedLaunch& l, const PagedArgs& a, hipStream_t st) {
-  const dim3 grid(static_cast<uint32_t>(l.workgroups)), block(64 * l.waves);
-  const uint32_t lds = paged_lds<FP8, D>(l.C, l.waves, a.G);
-  if (a.G == 1) {
-    const uint32_t row_lds = l.C * 8u + ((l.C / 8 + 15) & ~15) + l.waves * (D + 2) * 4u;
-    paged_row_kernel<FP8, D, FP8 ? 4 : 8><<<grid, block, row_lds, st>>>(a);
-  } else if (a.f32) {
-    paged_kernel<FP8, D, 3><<<grid, block, lds, st>>>(a);
-  } else {
-    paged_kernel<FP8, D, 2><<<grid, block, lds, st>>>(a);
-  }
-  if (l.S > 1) {
-    const int64_t rows = static_cast<int64_t>(a.B) * a.Hq;
-    const int each = l.S > 4 ? 4 : 1;
-    paged_combine_kernel<D><<<dim3(static_cast<uint32_t>(each > 1 ? rows : (rows + 3) / 4)), dim3(256), 0,
-                              st>>>(a, each, l.S);
-  }
-  return hipGetLastError();
+hipError_t launch_paged(const PagedLaunch& l, PagedArgs a, hipStream_t st) {
+  const dim3 block(64 * l.waves);
+  const hipError_t e = launch_parts(l.workgroups, 64 * l.waves, [&](uint32_t first, dim3 grid) {
+    const uint32_t lds = paged_lds<FP8, D>(l.C, l.waves, a.G);
+    a.first = first;
+    if (a.G == 1) {
+      const uint32_t row_lds = l.C * 8u + ((l.C / 8 + 15) & ~15) + l.waves * (D + 2) * 4u;
+      paged_row_kernel<FP8, D, FP8 ? 4 : 8><<<grid, block, row_lds, st>>>(a);
+    } else if (a.f32) {
+      paged_kernel<FP8, D, 3><<<grid, block, lds, st>>>(a);
+    } else {
+      paged_kernel<FP8, D, 2><<<grid, block, lds, st>>>(a);
+    }
+  });
+  if (e != hipSuccess || l.S == 1) return e;
+  const int64_t rows = static_cast<int64_t>(a.B) * a.Hq;
+  const int each = l.S > 4 ? 4 : 1;
+  return launch_parts(each > 1 ? rows : (rows + 3) / 4, 256, [&](uint32_t first, dim3 grid) {
+    a.first = first;
+    paged_combine_kernel<D><<<grid, dim3(256), 0, st>>>(a, each, l.S);
+  });
 }
 
 }  // namespace

@@ -354,8 +354,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a, in
                                                            int copy_blocks) {
   constexpr int chunks = D * (FP8 ? 1 : 2) / 16;
   const int per = blocks + copy_blocks;
-  const int lb = blockIdx.x / per, b = lb % a.B, layer = lb / a.B;
-  const int block = blockIdx.x % per;
+  const uint32_t group = a.first + blockIdx.x;
+  const int lb = group / per, b = lb % a.B, layer = lb / a.B;
+  const int block = group % per;
   const int rows = 1 << a.lg;
   const unsigned at = (block < blocks ? block : block - blocks) * 256u + threadIdx.x;
   const int c = at % chunks, h = at / chunks % static_cast<unsigned>(a.Hkv);
@@ -389,12 +390,15 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a, in
 }
 
 template <bool FP8, int D>
-void append_grid(const PagedAppendArgs& a, hipStream_t st) {
+hipError_t append_grid(PagedAppendArgs a, hipStream_t st) {
   const int64_t row = static_cast<int64_t>(a.Hkv) * (D * (FP8 ? 1 : 2) / 16);
   const int blocks = static_cast<int>((a.N * row + 255) / 256);
   const int copies = a.copies ? static_cast<int>(((row << a.lg) + 255) / 256) : 0;
-  const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(blocks + copies) * a.layers * a.B));
-  paged_append_kernel<FP8, D><<<grid, dim3(256), 0, st>>>(a, blocks, copies);
+  const int64_t groups = (int64_t{blocks} + copies) * a.layers * a.B;
+  return launch_parts(groups, 256, [&](uint32_t first, dim3 grid) {
+    a.first = first;
+    paged_append_kernel<FP8, D><<<grid, dim3(256), 0, st>>>(a, blocks, copies);
+  });
 }
 
 }  // namespace
@@ -422,10 +426,8 @@ hipError_t launch_page_reorder(const PageReorderArgs& a, hipStream_t st) {
 
 hipError_t launch_paged_append(const PagedAppendArgs& a, int dtype, hipStream_t st) {
   if (dtype == DSA_KV_FP8_E4M3)
-    a.D == 64 ? append_grid<true, 64>(a, st) : append_grid<true, 128>(a, st);
-  else
-    a.D == 64 ? append_grid<false, 64>(a, st) : append_grid<false, 128>(a, st);
-  return hipGetLastError();
+    return a.D == 64 ? append_grid<true, 64>(a, st) : append_grid<true, 128>(a, st);
+  return a.D == 64 ? append_grid<false, 64>(a, st) : append_grid<false, 128>(a, st);
 }
 
 }  // namespace dsa
