@@ -773,7 +773,8 @@ DSA_API size_t dsa_paged_workspace_bytes(const dsa_params* p, const dsa_shape* s
  *             every call
  *   batch     B in [1, DSA_MAX_PAGED_BATCH]
  *   pages     all fields but d_prompt required
- *   d_length  int32 [B]; not changed (a program adds d_new when its step is done)
+ *   d_length  int32 [B]; not changed (when its step is done a program adds d_new to
+ *             the lengths of 0 and more whose flags are 0: the others got no rows)
  *   d_new     int32 [B], clamped to [0, most_new]; NULL: 1 each
  *   most_new  N >= 1, B * N < 2^31
  *   d_slots   int32 [B][N], out: page * P + row in the page of row len + i; -1 for
@@ -796,8 +797,9 @@ DSA_API dsa_status dsa_page_update(const dsa_params* p, int32_t batch, const dsa
  * Request b goes on from the rows of request d_parent[b]: row b of the table
  * becomes what row d_parent[b] was, for all b at once, and d_refs follows.  No row
  * is moved; dsa_page_update gives a request that writes into a shared page its
- * own.  A parent outside [0, B) leaves the request without pages.  (Lengths,
- * prompt lengths and selection states are the caller's to reorder.)
+ * own.  A parent outside [0, B) leaves the request without pages: its slot is unused
+ * and its length -1 from here on (with another, dsa_page_update would give it a page).
+ * (Lengths, prompt lengths and selection states are the caller's to reorder.)
  *   batch     B in [1, DSA_MAX_PAGED_BATCH]
  *   pages     d_table and d_refs required
  *   d_parent  int32 [B]
