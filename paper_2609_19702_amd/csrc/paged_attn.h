@@ -136,7 +136,7 @@ __device__ __forceinline__ void paged_finish(const PagedArgs& a, const PagedWork
         to[D + 1] = L;
       }
     } else {
-      const float y = L == 0.f ? 0.f : O * vs / L;
+      const float y = L == 0.f ? 0.f : O / L * vs;  // O * vs can pass fp32 where y does not
       const size_t to = (static_cast<size_t>(w.b) * a.Hq + w.h * G + g) * D + d;
       if (a.f32)
         static_cast<float*>(a.out)[to] = y;
@@ -613,7 +613,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a, int eac
   const float vs = a.vs ? a.vs[h] : 1.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const float y = L == 0.f ? 0.f : O[i] * vs / L;
+    const float y = L == 0.f ? 0.f : O[i] / L * vs;
     const size_t to = static_cast<size_t>(at) * D + lane + 64 * i;
     if (a.f32)
       static_cast<float*>(a.out)[to] = y;
