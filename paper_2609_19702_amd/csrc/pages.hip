@@ -309,13 +309,13 @@ __global__ __launch_bounds__(kReorderThreads) void page_reorder_kernel(PageReord
 // bf16 values over a scale, within +-448 (NaN stays NaN), in three operations where the
 // compiler's division takes ten: Markstein's correction.  With y the rounded reciprocal of s and
 // q = x * y rounded, q + (x - q * s) * y by fma is x / s rounded to nearest, unless that lies
-// within 2^-21 of a unit in the last place of the middle between two fp32 values (q is off by 1.5 units at
-// most; nothing is below 2^-138).  E4M3 codes could differ where, besides, one of the two is a border
-// between codes, of five bits: with integers X, S and b of 8, 24 and 5 bits that is
-// |X 2^k - S (b 2^20 +- 1)| <= 16 with k >= 39, which leaves S = 2^24 - 1 and b = 16, the border
-// 2^-10, and there the steps round as the quotient does.  So the codes are the division's.
-// Quotients past 1024 end at 448 by either, those below 2^-12 at a zero of their sign;
-// scales far from 1 are divided by.
+// within 2^-21 of a unit in the last place of the middle between two fp32 values (q is off by
+// 1.5 units at most; nothing is below 2^-138).  E4M3 codes could differ where, besides, one of
+// the two is a border between codes, of five bits: with integers X, S and b of 8, 24 and 5 bits
+// that is |X 2^k - S (b 2^20 +- 1)| <= 16 with k >= 39, which leaves S = 2^24 - 1 and b = 16,
+// the border 2^-10, and there the steps round as the quotient does.  So the codes are the
+// division's.  Quotients past 1024 end at 448 by either, those below 2^-12 at a zero of their
+// sign; scales far from 1 are divided by.
 __device__ __forceinline__ void over_scale(const uint4& x, float s, float (&f)[8]) {
   unpack8(x, f);
   const float y = 1.f / s, size = fabsf(s);
